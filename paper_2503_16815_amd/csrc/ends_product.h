@@ -1,0 +1,318 @@
+// The matrix product that the head's operators are made of:  C[m][n] = sum_k A[m][k] B[n][k], both
+// operands with their k elements next to each other, 16-bit elements, 32-bit sums.  What happens
+// to C is the epilogue's business (it is never stored as it is): softmax statistics, the loss's
+// derivative, or a sum into a gradient.
+//
+// A workgroup of eight wavefronts owns a tile of C.  Both operands' tiles go from memory to LDS without
+// passing registers, 64 elements of k at a time, the next ones while the current ones are multiplied.
+// The 16-byte pieces of a row are permuted by the row's number, so that the sixteen rows that a wavefront
+// reads together lie in different banks.
+//
+// 32-bit operands come as three 16-bit arrays whose sum they are (8 bits of the significand in
+// each); the six products of those arrays that matter at 24 bits are summed one after the other.
+#pragma once
+#include "ends.h"
+
+namespace deft {
+
+constexpr int kStep = 64;            // elements of k per step
+constexpr int kStepBytes = kStep * 2;
+
+enum Epilogue { kSoftmax = 0, kDerivative = 1, kSums = 2, kGradient = 3 };
+
+struct ProductArgs {
+    const void *a, *b;
+    int64_t a_ld, b_ld;              // elements between rows
+    int64_t a_plane, b_plane;        // elements between the three arrays of a 32-bit operand
+    int m, n;                        // rows of a and of b
+    const int *n_dev;                // rows of b that count, where the device knows it, or NULL
+    int k;                           // a multiple of kStep
+    const int *k_dev;                // or the rows of another operand, rounded up to kStep
+    int splits;                      // of k, over blockIdx.y
+    float scale;
+    // kSoftmax, kDerivative: m counts rows of the vocabulary from m_first on, n packed positions
+    int m_first;
+    const int *label;                // [n]
+    float2 *parts;                   // [n][parts_ld]: each tile's softmax sum of the position
+    int parts_ld;
+    float *z_label;                  // [n]
+    const float *lse;                // [n]
+    const float *row_grad;           // [n]
+    const float *t_scale;            // the power of two that d_t is scaled with
+    float d_scale;                   // the one that d is scaled with
+    void *d, *d_t;                   // [n][d_ld], [m][d_t_ld]
+    int64_t d_ld, d_t_ld, d_plane, d_t_plane;
+    // kSums: sums[split][n][m]; kGradient: out[n][m]
+    float *sums;
+    int64_t sums_ld, sums_split;
+    int add;
+    void *out;
+    int64_t out_ld;
+};
+
+template <typename T> struct Mfma;
+template <> struct Mfma<f16> {
+    typedef f16 operand __attribute__((ext_vector_type(8)));
+    static __device__ __forceinline__ f32x4 run(operand a, operand b, f32x4 c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+    }
+};
+template <> struct Mfma<bf16> {
+    typedef bf16 operand __attribute__((ext_vector_type(8)));
+    static __device__ __forceinline__ f32x4 run(operand a, operand b, f32x4 c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+    }
+};
+
+// A float as a sum of three bf16: the first two cut off (so that they are exact and cannot
+// overflow), the last rounded.  What is not finite stays in the first.
+__device__ __forceinline__ void split3(float x, bf16 (&p)[3])
+{
+    const auto cut = [](float f) { return __uint_as_float(__float_as_uint(f) & 0xffff0000u); };
+    const bool finite = (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u;
+    const float first = finite ? cut(x) : x;
+    const float rest = finite ? x - first : 0.0f;
+    const float second = cut(rest);
+    p[0] = (bf16)first;
+    p[1] = (bf16)second;
+    p[2] = (bf16)(rest - second);
+}
+
+// Four rows' values of four neighbouring lanes, two to a word: lane q of the four gets row q's.
+__device__ __forceinline__ uint2 transpose4(unsigned x01, unsigned x23)
+{
+    const int q = threadIdx.x & 3;
+    const unsigned far = __builtin_amdgcn_update_dpp(0u, q < 2 ? x23 : x01, 0x4E, 0xf, 0xf, true);   // from lane ^ 2
+    const unsigned a = q < 2 ? x01 : far, b = q < 2 ? far : x23;
+    const bool odd = q & 1;
+    const unsigned lo = __builtin_amdgcn_perm(b, a, 0x05040100u), hi = __builtin_amdgcn_perm(b, a, 0x07060302u);
+    const unsigned got = __builtin_amdgcn_update_dpp(0u, odd ? lo : hi, 0xB1, 0xf, 0xf, true);       // from lane ^ 1
+    const unsigned left = odd ? got : lo, right = odd ? hi : got;
+    return make_uint2(__builtin_amdgcn_perm(right, left, 0x05040100u), __builtin_amdgcn_perm(right, left, 0x07060302u));
+}
+
+__device__ __forceinline__ unsigned pack2(f16 a, f16 b)
+{
+    return (unsigned)__builtin_bit_cast(unsigned short, a) | (unsigned)__builtin_bit_cast(unsigned short, b) << 16;
+}
+__device__ __forceinline__ unsigned pack2(bf16 a, bf16 b)
+{
+    return (unsigned)__builtin_bit_cast(unsigned short, a) | (unsigned)__builtin_bit_cast(unsigned short, b) << 16;
+}
+
+// T: element type of the operands.  O: type of the gradient that kGradient writes.  WM x WN wavefronts of MT x NT
+// tiles of 16 x 16.  SPLIT: operands are three arrays each.
+template <typename T, typename O, int E, int WM, int WN, int MT, int NT, bool SPLIT>
+__global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p)
+{
+    constexpr int kThreads = WM * WN * kWave, TM = WM * MT * 16, TN = WN * NT * 16;
+    constexpr int kABytes = TM * kStepBytes, kStage = (TM + TN) * kStepBytes;
+    constexpr int kALoads = TM * 8 / kThreads, kBLoads = TN * 8 / kThreads;
+    static_assert(kALoads * kThreads == TM * 8 && kBLoads * kThreads == TN * 8, "whole loads");
+    typedef typename Mfma<T>::operand Operand;
+    extern __shared__ __align__(16) char lds[];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave / WN, wn = wave % WN;
+    const int tiles_m = (p.m + TM - 1) / TM;
+    const int tm = blockIdx.x % tiles_m, tn = blockIdx.x / tiles_m;
+    const int m0 = tm * TM, n0 = tn * TN;
+    const int n_rows = p.n_dev ? *p.n_dev : p.n;
+    if (n0 >= n_rows) return;
+
+    const int steps_all = (p.k_dev ? *p.k_dev + kStep - 1 : p.k) / kStep;
+    const int from = (int)((int64_t)steps_all * blockIdx.y / p.splits), to = (int)((int64_t)steps_all * (blockIdx.y + 1) / p.splits);
+    const int steps = to - from, total = SPLIT ? steps * 6 : steps;
+
+    // where this thread's 16-byte pieces come from (rows past the operand's last one read that one)
+    const char *a_base = static_cast<const char *>(p.a) + ((int64_t)m0 * p.a_ld + (int64_t)from * kStep) * 2;
+    const char *b_base = static_cast<const char *>(p.b) + ((int64_t)n0 * p.b_ld + (int64_t)from * kStep) * 2;
+    unsigned a_off[kALoads], b_off[kBLoads];
+#pragma unroll
+    for (int i = 0; i < kALoads; ++i) {
+        const int c = tid + i * kThreads, row = c >> 3;
+        a_off[i] = (unsigned)min(row, p.m - 1 - m0) * (unsigned)(p.a_ld * 2) + (((c & 7) ^ ((row >> 1) & 7)) << 4);
+    }
+#pragma unroll
+    for (int i = 0; i < kBLoads; ++i) {
+        const int c = tid + i * kThreads, row = c >> 3;
+        b_off[i] = (unsigned)min(row, p.n - 1 - n0) * (unsigned)(p.b_ld * 2) + (((c & 7) ^ ((row >> 1) & 7)) << 4);
+    }
+    // the six products of three arrays each that are kept, the smallest first
+    const auto load = [&](int step, int stage) {
+        int64_t a_at = 0, b_at = 0;
+        int s = step;
+        if (SPLIT) {
+            const int which = step / steps;
+            s = step - which * steps;
+            const int pa = (0x021010 >> (4 * (5 - which))) & 15, pb = (0x201100 >> (4 * (5 - which))) & 15;
+            a_at = pa * p.a_plane * 2;
+            b_at = pb * p.b_plane * 2;
+        }
+        const char *as = a_base + a_at + (int64_t)s * kStepBytes, *bs = b_base + b_at + (int64_t)s * kStepBytes;
+        char *to_lds = lds + stage * kStage + wave * (kWave * 16);
+#pragma unroll
+        for (int i = 0; i < kALoads; ++i)
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(as + a_off[i]),
+                                             (__attribute__((address_space(3))) void *)(to_lds + i * kThreads * 16), 16, 0, 0);
+#pragma unroll
+        for (int i = 0; i < kBLoads; ++i)
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(bs + b_off[i]),
+                                             (__attribute__((address_space(3))) void *)(to_lds + kABytes + i * kThreads * 16), 16, 0, 0);
+    };
+
+    f32x4 acc[MT][NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+
+    const int row16 = lane & 15, part = lane >> 4;
+    if (total > 0) load(0, 0);
+    for (int step = 0; step < total; ++step) {
+        __syncthreads();   // this step's tiles are there, and nobody reads the other stage any more
+        if (step + 1 < total) load(step + 1, (step + 1) & 1);
+        const char *at = lds + (step & 1) * kStage;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int q = half * 4 + part;
+            Operand a[MT], b[NT];
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                const int row = wm * MT * 16 + i * 16 + row16;
+                a[i] = *reinterpret_cast<const Operand *>(at + row * kStepBytes + ((q ^ ((row >> 1) & 7)) << 4));
+            }
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                const int row = wn * NT * 16 + j * 16 + row16;
+                b[j] = *reinterpret_cast<const Operand *>(at + kABytes + row * kStepBytes + ((q ^ ((row >> 1) & 7)) << 4));
+            }
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc[i][j] = Mfma<T>::run(a[i], b[j], acc[i][j]);
+        }
+    }
+
+    // acc[i][j][r] is C[m][n] at m = m_lane + i * 16 + r, n = n_lane + j * 16
+    const int m_lane = m0 + wm * MT * 16 + part * 4, n_lane = n0 + wn * NT * 16 + row16;
+
+    if constexpr (E == kSoftmax) {
+        __syncthreads();
+        float2 *joined = reinterpret_cast<float2 *>(lds);   // [WM][TN]
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            const int n = n_lane + j * 16;
+            const int label = n < n_rows ? p.label[n] - p.m_first - m_lane : -1;
+            SoftSum s = {-INFINITY, 0.0f};
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    acc[i][j][r] *= p.scale;
+                    if (m_lane + i * 16 + r < p.m) s.top = fmaxf(s.top, acc[i][j][r]);
+                    if (label == i * 16 + r) p.z_label[n] = acc[i][j][r];
+                }
+            s.top = fmaxf(s.top, __shfl_xor(s.top, 16));
+            s.top = fmaxf(s.top, __shfl_xor(s.top, 32));
+            const float top = s.top == -INFINITY ? -3.0e38f : s.top;   // (no row of the vocabulary here, or all -infinity)
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (m_lane + i * 16 + r < p.m) s.sum += __expf(acc[i][j][r] - top);
+            s.sum += __shfl_xor(s.sum, 16);
+            s.sum += __shfl_xor(s.sum, 32);
+            if (part == 0) joined[wm * TN + wn * NT * 16 + j * 16 + row16] = make_float2(top, s.sum);
+        }
+        __syncthreads();
+        for (int i = tid; i < TN && n0 + i < n_rows; i += kThreads) {
+            SoftSum s = {joined[i].x, joined[i].y};
+#pragma unroll
+            for (int w = 1; w < WM; ++w) s = soft_join(s, SoftSum{joined[w * TN + i].x, joined[w * TN + i].y});
+            p.parts[(int64_t)(n0 + i) * p.parts_ld + p.m_first / TM + tm] = make_float2(s.top, s.sum);
+        }
+    } else if constexpr (E == kDerivative) {
+        const float t_scale = *p.t_scale;
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            const int n = n_lane + j * 16;
+            const bool in = n < n_rows;
+            const int label = in ? p.label[n] - p.m_first - m_lane : -1;
+            const float lse = in ? p.lse[n] : 0.0f, g = in ? p.row_grad[n] * t_scale : 0.0f;
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                float d[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float q = __expf(acc[i][j][r] * p.scale - lse) - (label == i * 16 + r ? 1.0f : 0.0f);
+                    d[r] = in && m_lane + i * 16 + r < p.m ? q : 0.0f;
+                }
+                const int m = m_lane + i * 16, first = m - part * 4;   // `first` of the tile's sixteen rows
+                T *to_d = static_cast<T *>(p.d) + (int64_t)n * p.d_ld + m;
+                T *to_t = static_cast<T *>(p.d_t) + (int64_t)(first + part * 4 + (lane & 3)) * p.d_t_ld + (n & ~3);
+                if constexpr (SPLIT) {
+                    bf16 x[4][3], y[4][3];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        split3(d[r] * p.d_scale, x[r]);
+                        split3(d[r] * g, y[r]);
+                    }
+#pragma unroll
+                    for (int s = 0; s < 3; ++s) {
+                        *reinterpret_cast<uint2 *>(to_d + s * p.d_plane) =
+                            make_uint2(pack2(x[0][s], x[1][s]), pack2(x[2][s], x[3][s]));
+                        *reinterpret_cast<uint2 *>(to_t + s * p.d_t_plane) =
+                            transpose4(pack2(y[0][s], y[1][s]), pack2(y[2][s], y[3][s]));
+                    }
+                } else {
+                    *reinterpret_cast<uint2 *>(to_d) = make_uint2(pack2((T)(d[0] * p.d_scale), (T)(d[1] * p.d_scale)),
+                                                                  pack2((T)(d[2] * p.d_scale), (T)(d[3] * p.d_scale)));
+                    *reinterpret_cast<uint2 *>(to_t) =
+                        transpose4(pack2((T)(d[0] * g), (T)(d[1] * g)), pack2((T)(d[2] * g), (T)(d[3] * g)));
+                }
+            }
+        }
+    } else if constexpr (E == kSums) {
+        float *sums = p.sums + blockIdx.y * p.sums_split;
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            const int n = n_lane + j * 16;
+            if (n >= n_rows) continue;
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                const int m = m_lane + i * 16;   // (sums_ld is a multiple of 4, so m < p.m leaves room for four)
+                if (m >= p.m) continue;
+                f32x4 *to_sum = reinterpret_cast<f32x4 *>(sums + (int64_t)n * p.sums_ld + m);
+                *to_sum = p.add ? *to_sum + acc[i][j] : acc[i][j];
+            }
+        }
+    } else {
+        const float alpha = p.scale / *p.t_scale;
+        typedef O O4 __attribute__((ext_vector_type(4), aligned(sizeof(O))));
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            const int n = n_lane + j * 16;
+            if (n >= n_rows) continue;
+            O *row = static_cast<O *>(p.out) + (int64_t)n * p.out_ld;
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                const int m = m_lane + i * 16;
+                if (m + 4 <= p.m) {
+                    O4 x = {};
+                    if (p.add) x = *reinterpret_cast<const O4 *>(row + m);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) x[r] = (O)((p.add ? (float)x[r] : 0.0f) + alpha * acc[i][j][r]);
+                    *reinterpret_cast<O4 *>(row + m) = x;
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (m + r < p.m) row[m + r] = (O)((p.add ? (float)row[m + r] : 0.0f) + alpha * acc[i][j][r]);
+                }
+            }
+        }
+    }
+}
+
+}  // namespace deft
