@@ -32,6 +32,21 @@ __device__ __forceinline__ float wave_sum(float x)
     return x;
 }
 
+// 16 bytes of a row, at any address that its elements may have
+template <typename T> struct Vec;
+template <> struct Vec<float> {
+    typedef float type __attribute__((ext_vector_type(4), aligned(4)));
+    static constexpr int n = 4;
+};
+template <> struct Vec<f16> {
+    typedef f16 type __attribute__((ext_vector_type(8), aligned(2)));
+    static constexpr int n = 8;
+};
+template <> struct Vec<bf16> {
+    typedef bf16 type __attribute__((ext_vector_type(8), aligned(2)));
+    static constexpr int n = 8;
+};
+
 // A running softmax sum: the largest value so far and the sum of exp(value - largest).  -infinity
 // adds nothing to it; a NaN or +infinity makes the sum NaN, as the definition does.
 struct SoftSum {

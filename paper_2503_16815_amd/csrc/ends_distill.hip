@@ -3,27 +3,17 @@
 //   p = softmax(t / T) over the entries that the teacher kept,  q = softmax(z / T) over the vocabulary
 //   loss = T^2 sum_k p_k (log p_k - log q_{i_k}),   dz = g T (q - p scattered to its indices)
 //
-// A workgroup owns a row.  Bound by the row's bytes: one read for the loss, one more write for the gradient.
+// Bound by the row's bytes: one read for the loss, one more write for the gradient.  A row of up to 256 KB
+// stays in the registers of one workgroup of 1024 lanes from its one read to the gradient's write
+// (131072 16-bit logits take 64 registers a lane).  The workgroup goes on from row to row, and each
+// 16 bytes of the next row are asked for as soon as the gradient of the present row's has been stored,
+// so memory is idle only during the row's two reductions.  Rows that are longer are read once more.
 #include "ends.h"
 
 namespace deft {
 namespace {
 
 constexpr int kThreads = 512, kWaves = kThreads / kWave;
-
-template <typename T> struct Vec;   // 16 bytes of a row, at any address that its elements may have
-template <> struct Vec<float> {
-    typedef float type __attribute__((ext_vector_type(4), aligned(4)));
-    static constexpr int n = 4;
-};
-template <> struct Vec<f16> {
-    typedef f16 type __attribute__((ext_vector_type(8), aligned(2)));
-    static constexpr int n = 8;
-};
-template <> struct Vec<bf16> {
-    typedef bf16 type __attribute__((ext_vector_type(8), aligned(2)));
-    static constexpr int n = 8;
-};
 
 // Sum over the workgroup; every thread gets it.  `room` is read until the next barrier.
 __device__ __forceinline__ float block_sum(float x, float *room)
@@ -155,15 +145,202 @@ __global__ void __launch_bounds__(kThreads) distill_kernel(deft_distill_t a)
         if (index[k] >= 0) grad[index[k]] = (T)fixed[j & 1];
 }
 
+// ---- rows that stay in registers -------------------------------------------------------------
+
+constexpr int kMarkBits = 1 << 17;   // of the map that shows whether an index occurs twice
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+
+__device__ __forceinline__ SoftSum soft_join2(SoftSum a, SoftSum b)   // with powers of two
+{
+    const float top = fmaxf(a.top, b.top);
+    return {top, (a.top == top ? a.sum : a.sum * exp2_of(a.top - top)) + (b.top == top ? b.sum : b.sum * exp2_of(b.top - top))};
+}
+
+__device__ __forceinline__ SoftSum wave_join2(SoftSum s, int from)
+{
+    for (int d = from; d > 0; d >>= 1) s = soft_join2(s, SoftSum{__shfl_xor(s.top, d), __shfl_xor(s.sum, d)});
+    return s;
+}
+
+// Each lane holds NV vectors of the row, kRowThreads vectors apart, and one of its last `vocab % n` elements; the
+// k-th lane the teacher's k-th entry.  Logits are scaled by log2(e) / T as they are used.
+template <typename T, int kRowThreads, int NV, bool GRAD>
+__global__ void __launch_bounds__(kRowThreads, 4) distill_row_kernel(deft_distill_t a)
+{
+    constexpr int kRowWaves = kRowThreads / kWave;
+    typedef typename Vec<T>::type V;
+    constexpr int n = Vec<T>::n;
+    __shared__ unsigned mark[kMarkBits / 32];
+    __shared__ SoftSum student[kRowWaves], teacher[kRowWaves];
+    __shared__ int flags[kRowWaves], twice[2];
+    __shared__ float part[kRowWaves];
+    __shared__ int same_index[kRowThreads];
+    __shared__ float same_prob[kRowThreads];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const float c = kLog2e / a.temperature;
+    const int whole = a.vocab / n * n, rest = a.vocab - whole;
+    const T *const logits = static_cast<const T *>(a.logits);
+    for (int i = tid; i < kMarkBits / 32; i += kRowThreads) mark[i] = 0;
+    if (tid < 2) twice[tid] = 0;
+
+    V x[NV];
+    T last = (T)0.0f;
+    const auto load = [&](int64_t row, int j) {
+        const int at = (j * kRowThreads + tid) * n;
+        if (at < whole) x[j] = *reinterpret_cast<const V *>(logits + row * a.logits_stride + at);
+    };
+    const auto entry = [&](int64_t row, int &index, float &u) {
+        index = -1;
+        u = -INFINITY;
+        if (row < a.n_rows && tid < a.top_k) {
+            index = a.teacher_index[row * a.top_k + tid];
+            u = a.teacher_logit[row * a.top_k + tid];
+        }
+    };
+    int index, next_index;
+    float u, next_u;
+    entry(blockIdx.x, index, u);
+    bool kept = __syncthreads_or(index != -1);
+    if (kept) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) load(blockIdx.x, j);
+        if (tid < rest) last = logits[(int64_t)blockIdx.x * a.logits_stride + whole + tid];
+    }
+
+    int odd = 0;
+    for (int64_t row = blockIdx.x; row < a.n_rows; row += gridDim.x, odd ^= 1) {
+        const int64_t next = row + gridDim.x;
+        const bool in = index >= 0 && index < a.vocab;
+        float z_at = 0.0f;   // the logit at this lane's entry
+        if (in) z_at = (float)logits[row * a.logits_stride + index] * c;
+        entry(next, next_index, next_u);
+        if (in) {
+            const unsigned bit = 1u << (index & 31);
+            if (atomicOr(&mark[(index % kMarkBits) >> 5], bit) & bit) twice[odd] = 1;
+        }
+        SoftSum s = {-INFINITY, 0.0f}, t = {in ? u * c : -INFINITY, 0.0f};
+        if (kept) {
+            // -3e38 in the place of -infinity: exp2(-infinity - that) is 0, and a NaN stays one
+            float top = tid < rest ? (float)last * c : -3.0e38f;
+            top = fmaxf(top, -3.0e38f);
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+                if ((j * kRowThreads + tid) * n < whole) {
+#pragma unroll
+                    for (int i = 0; i < n; ++i) top = fmaxf(top, (float)x[j][i] * c);
+                }
+            s.top = top;
+            if (tid < rest) s.sum = exp2_of(__builtin_fmaf((float)last, c, -top));
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+                if ((j * kRowThreads + tid) * n < whole) {
+#pragma unroll
+                    for (int i = 0; i < n; ++i) s.sum += exp2_of(__builtin_fmaf((float)x[j][i], c, -top));
+                }
+            s = wave_join2(s, 32);
+            if (in) t.sum = t.top == -INFINITY ? 0.0f : exp2_of(t.top - t.top);   // (1, or the NaN that the entry is)
+            t = wave_join2(t, 32);
+        }
+        const int flag = (__any(index != -1 && !in) ? 1 : 0) | (__any(next_index != -1) ? 2 : 0);
+        if (lane == 0) {
+            student[wave] = s;
+            teacher[wave] = t;
+            flags[wave] = flag;
+        }
+        __syncthreads();
+        s = wave_join2(student[lane & (kRowWaves - 1)], kRowWaves / 2);
+        t = wave_join2(teacher[lane & (kRowWaves - 1)], kRowWaves / 2);
+        const int all = flags[lane & (kRowWaves - 1)];
+        const bool outside = __any(all & 1), next_kept = __any(all & 2);
+        const bool bad = kept && (outside || s.sum == 0.0f || t.sum == 0.0f), ok = kept && !bad;
+        const float lse = s.top + __log2f(s.sum);
+        float p = 0.0f, by = 0.0f;
+        if (in && ok) {
+            const float v = u * c - t.top;
+            p = exp2_of(v) / t.sum;
+            if (p > 0.0f || p != p) by = p * (v - __log2f(t.sum) - (z_at - lse)) * kLn2;
+        }
+        by = wave_sum(by);
+        if (lane == 0) part[wave] = by;
+        float g = 0.0f, fixed = 0.0f;
+        if (GRAD && ok) {
+            g = a.row_grad[row] * a.temperature;
+            if (twice[odd]) {   // an index that occurs twice counts with the sum of its entries
+                same_index[tid] = in ? index : -1;
+                same_prob[tid] = p;
+                __syncthreads();
+                p = 0.0f;
+                for (int k = 0; k < a.top_k; ++k) p += same_index[k] == index ? same_prob[k] : 0.0f;
+            }
+            fixed = g * (exp2_of(z_at - lse) - p);
+        }
+        if (in) mark[(index % kMarkBits) >> 5] = 0;
+        if (tid == 0) twice[odd ^ 1] = 0;
+
+        T *grad = GRAD ? static_cast<T *>(a.grad_logits) + row * a.grad_stride : nullptr;
+        if (GRAD && tid < rest) grad[whole + tid] = ok ? (T)(g * exp2_of(__builtin_fmaf((float)last, c, -lse))) : (T)0.0f;
+        if (next_kept && tid < rest) last = logits[next * a.logits_stride + whole + tid];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int at = (j * kRowThreads + tid) * n;
+            if (GRAD && at < whole) {
+                V y = {};
+                if (ok) {
+#pragma unroll
+                    for (int i = 0; i < n; ++i) y[i] = (T)(g * exp2_of(__builtin_fmaf((float)x[j][i], c, -lse)));
+                }
+                *reinterpret_cast<V *>(grad + at) = y;
+            }
+            if (next_kept) load(next, j);
+        }
+        if (GRAD) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the stores above come before those below
+        __syncthreads();
+        if (GRAD && in && ok) grad[index] = (T)fixed;
+        if (tid == 0) {
+            float loss = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kRowWaves; ++w) loss += part[w];
+            a.loss[row] = ok ? loss * a.temperature * a.temperature : 0.0f;
+            if (a.status) a.status[row] = bad ? DEFT_ERR_INVALID_ARG : DEFT_OK;
+        }
+        index = next_index;
+        u = next_u;
+        kept = next_kept;
+    }
+}
+
+template <typename T, int THREADS, int NV>
+hipError_t row_launch(const deft_distill_t &a, int compute_units, hipStream_t st)
+{
+    const int most = compute_units * (1024 / THREADS), blocks = a.n_rows < most ? a.n_rows : most;
+    if (a.grad_logits) distill_row_kernel<T, THREADS, NV, true><<<blocks, THREADS, 0, st>>>(a);
+    else distill_row_kernel<T, THREADS, NV, false><<<blocks, THREADS, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+// By the row's bytes alone (and by top_k, an entry a lane).  Up to 128 KB two workgroups of 512 lanes share a
+// compute unit, so that one's reductions fall into the other's reads and writes.
+template <typename T>
+hipError_t any_launch(const deft_distill_t &a, int compute_units, hipStream_t st)
+{
+    const int vectors = a.vocab / Vec<T>::n;
+    if (a.top_k <= 512 && vectors <= 512 * 4) return row_launch<T, 512, 4>(a, compute_units, st);
+    if (a.top_k <= 512 && vectors <= 512 * 8) return row_launch<T, 512, 8>(a, compute_units, st);
+    if (a.top_k <= 512 && vectors <= 512 * 16) return row_launch<T, 512, 16>(a, compute_units, st);
+    if (vectors <= 1024 * 16) return row_launch<T, 1024, 16>(a, compute_units, st);
+    distill_kernel<T><<<a.n_rows, kThreads, (size_t)a.top_k * 8, st>>>(a);
+    return hipGetLastError();
+}
+
 }  // namespace
 
-hipError_t distill_launch(int dtype, const deft_distill_t &a, int, hipStream_t st)
+hipError_t distill_launch(int dtype, const deft_distill_t &a, int compute_units, hipStream_t st)
 {
-    const size_t lds = (size_t)a.top_k * 8;
-    if (dtype == DEFT_F32) distill_kernel<float><<<a.n_rows, kThreads, lds, st>>>(a);
-    else if (dtype == DEFT_F16) distill_kernel<f16><<<a.n_rows, kThreads, lds, st>>>(a);
-    else distill_kernel<bf16><<<a.n_rows, kThreads, lds, st>>>(a);
-    return hipGetLastError();
+    if (dtype == DEFT_F32) return any_launch<float>(a, compute_units, st);
+    if (dtype == DEFT_F16) return any_launch<f16>(a, compute_units, st);
+    return any_launch<bf16>(a, compute_units, st);
 }
 
 }  // namespace deft
