@@ -13,33 +13,17 @@
 namespace deft {
 namespace {
 
-template <typename T> struct Vec;   // 16 bytes of a row, at any address that its elements may have
-template <> struct Vec<float> {
-    typedef float type __attribute__((ext_vector_type(4), aligned(4)));
-    static constexpr int n = 4;
-};
-template <> struct Vec<f16> {
-    typedef f16 type __attribute__((ext_vector_type(8), aligned(2)));
-    static constexpr int n = 8;
-};
-template <> struct Vec<bf16> {
-    typedef bf16 type __attribute__((ext_vector_type(8), aligned(2)));
-    static constexpr int n = 8;
-};
-
-// The elements at `at` .. `at` + n - 1 of a row of `width`, as floats; beyond the row they are 0.
+// The 16 bytes from element `at` of a row of `width` on; beyond the row they are 0.
 template <typename T>
-__device__ __forceinline__ void load_part(const T *row, int at, int width, float (&x)[Vec<T>::n])
+__device__ __forceinline__ typename Vec<T>::type load_part(const T *row, int at, int width)
 {
     constexpr int n = Vec<T>::n;
-    if (at + n <= width) {
-        const typename Vec<T>::type v = *reinterpret_cast<const typename Vec<T>::type *>(row + at);
+    if (at + n <= width) return *reinterpret_cast<const typename Vec<T>::type *>(row + at);
+    typename Vec<T>::type v = {};
 #pragma unroll
-        for (int i = 0; i < n; ++i) x[i] = (float)v[i];
-    } else {
-#pragma unroll
-        for (int i = 0; i < n; ++i) x[i] = at + i < width ? (float)row[at + i] : 0.0f;
-    }
+    for (int i = 0; i < n; ++i)
+        if (at + i < width) v[i] = row[at + i];
+    return v;
 }
 
 template <typename T>
@@ -72,9 +56,9 @@ __global__ void __launch_bounds__(256) embed_kernel(deft_embed_t e)
     for (int at = lane * n; at < e.hidden; at += kWave * n) {
         float x[n] = {};
         if (in) {
-            load_part<T>(from, at, e.hidden, x);
+            const typename Vec<T>::type v = load_part<T>(from, at, e.hidden);
 #pragma unroll
-            for (int i = 0; i < n; ++i) x[i] *= e.scale;
+            for (int i = 0; i < n; ++i) x[i] = e.scale * (float)v[i];
         }
         store_part<T>(out, at, e.hidden, x);
     }
@@ -187,12 +171,136 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(SortArgs a)
     }
 }
 
+// ---- up to 16384 rows: sorted by one workgroup -----------------------------------------------
+
+// A token number and its row fit one word (18 and 14 bits), sixteen words a lane.  Everything happens in
+// registers and LDS in one launch, which has the other compute units to itself: they clear the rows of the
+// table that no token points to.  (Measured on 16384 tokens of a vocabulary of 50257: the six launches of the
+// sort in memory 50 us and the clearing 21 us before it.)
+constexpr int kSmallThreads = 1024, kSmallWaves = 16, kSmallItems = 16, kSmall = kSmallThreads * kSmallItems;
+constexpr int kRowBits = 14, kSmallVocab = 1 << (32 - kRowBits);
+
+struct SmallArgs {
+    int n, vocab, hidden, digit_bits, passes;
+    const int32_t *tokens;
+    int32_t *keys, *rows;
+    void *table;
+    int64_t stride;
+};
+
+// What lanes of a wavefront wrote to LDS before is what they read behind it (its accesses are in order).
+__device__ __forceinline__ void in_wave()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+__device__ __forceinline__ void sort_small(const SmallArgs &a, unsigned *words, int (*count)[kDigits], int *wave_total)
+{
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int rounds = (a.n + kSmallThreads - 1) / kSmallThreads, first = wave * rounds * kWave + lane;
+    unsigned item[kSmallItems];
+    int rank[kSmallItems];
+#pragma unroll
+    for (int r = 0; r < kSmallItems; ++r) {
+        const int i = first + r * kWave;
+        if (r < rounds && i < a.n) {
+            const int t = a.tokens[i];
+            item[r] = (unsigned)(t >= 0 && t < a.vocab ? t : a.vocab) << kRowBits | (unsigned)i;
+        }
+    }
+    for (int pass = 0; pass < a.passes; ++pass) {
+        const int shift = kRowBits + pass * a.digit_bits, digits = 1 << a.digit_bits;
+        for (int d = lane; d < digits; d += kWave) count[wave][d] = 0;
+        in_wave();
+#pragma unroll
+        for (int r = 0; r < kSmallItems; ++r) {
+            if (r < rounds) {
+                const bool valid = first + r * kWave < a.n;
+                const int digit = (item[r] >> shift) & (digits - 1);
+                const uint64_t same = same_digit(digit, valid);
+                const int before = __popcll(same & ((1ull << lane) - 1));
+                const int base = valid ? count[wave][digit] : 0;
+                in_wave();   // every lane has read what the first of each digit now writes
+                rank[r] = base + before;
+                if (valid && before == 0) count[wave][digit] = base + __popcll(same);
+                in_wave();
+            }
+        }
+        __syncthreads();
+        // counts become the places of each wavefront's first item of a digit
+        int own = 0, x = 0;
+        if (tid < digits)
+            for (int w = 0; w < kSmallWaves; ++w) own += count[w][tid];
+        x = own;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int y = __shfl_up(x, d);
+            if (lane >= d) x += y;
+        }
+        if (lane == 63) wave_total[wave] = x;
+        __syncthreads();
+        if (tid < digits) {
+            int at = x - own;
+            for (int w = 0; w < wave; ++w) at += wave_total[w];
+            for (int w = 0; w < kSmallWaves; ++w) {
+                const int c = count[w][tid];
+                count[w][tid] = at;
+                at += c;
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kSmallItems; ++r)
+            if (r < rounds && first + r * kWave < a.n) words[count[wave][(item[r] >> shift) & (digits - 1)] + rank[r]] = item[r];
+        __syncthreads();
+        if (pass + 1 < a.passes) {
+#pragma unroll
+            for (int r = 0; r < kSmallItems; ++r)
+                if (r < rounds && first + r * kWave < a.n) item[r] = words[first + r * kWave];
+        }
+    }
+    for (int i = tid; i < a.n; i += kSmallThreads) {
+        a.keys[i] = (int32_t)(words[i] >> kRowBits);
+        a.rows[i] = (int32_t)(words[i] & ((1u << kRowBits) - 1));
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kSmallThreads) sort_small_kernel(SmallArgs a)
+{
+    __shared__ unsigned words[kSmall];
+    __shared__ int count[kSmallWaves][kDigits];
+    __shared__ int wave_total[kSmallWaves];
+    if (blockIdx.x == 0) {
+        sort_small(a, words, count, wave_total);
+        return;
+    }
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int share = blockIdx.x - 1, shares = gridDim.x - 1;
+    const int from = (int)((int64_t)a.vocab * share / shares), to = (int)((int64_t)a.vocab * (share + 1) / shares);
+    for (int i = tid; i < (to - from + 31) / 32; i += kSmallThreads) words[i] = 0;   // (fewer rows than kSmall bits)
+    __syncthreads();
+    for (int i = tid; i < a.n; i += kSmallThreads) {
+        const int t = a.tokens[i];
+        if (t >= from && t < to) atomicOr(&words[(t - from) >> 5], 1u << ((t - from) & 31));
+    }
+    __syncthreads();
+    constexpr int n = Vec<T>::n;
+    const float zero[n] = {};
+    for (int row = from + wave; row < to; row += kSmallWaves) {
+        if (words[(row - from) >> 5] >> ((row - from) & 31) & 1) continue;
+        T *to_row = static_cast<T *>(a.table) + (int64_t)row * a.stride;
+        for (int at = lane * n; at < a.hidden; at += kWave * n) store_part<T>(to_row, at, a.hidden, zero);
+    }
+}
+
 // ---- sums over the sorted rows --------------------------------------------------------------
 
-constexpr int kChunk = 32, kBatch = 8;
+constexpr int kBatch = 8, kJoin = 8;
 
 struct SumArgs {
-    int n, vocab, hidden, accumulate, chunks;
+    int n, vocab, hidden, accumulate, chunk, chunks;
     int lanes;            // threads that share a chunk: a power of two, 16 bytes of the row each
     float scale;
     const int32_t *keys, *rows;
@@ -200,8 +308,17 @@ struct SumArgs {
     int64_t grad_out_stride;
     void *grad_table;
     int64_t grad_table_stride;
-    float *partial;       // [chunks][2][hidden]: of the run that a chunk begins in, of the one it ends in
+    float *partial;       // [chunks][2][width]: of the run that a chunk begins in, of the one it ends in
+    int width;            // of a partial sum's row: hidden, rounded up to a lane's part
 };
+
+// Chunks of 16 rows keep 16384 tokens' rows on four workgroups per compute unit; longer lists have longer chunks, so
+// that a token with many rows leaves no more than a few thousand partial sums.
+int chunk_of(int n)
+{
+    const int c = (n + 1023) / 1024;
+    return c <= 16 ? 16 : c >= 256 ? 256 : (c + 7) / 8 * 8;
+}
 
 template <typename T>
 __device__ __forceinline__ void write_sum(const SumArgs &a, int token, int at, const float (&acc)[Vec<T>::n])
@@ -209,24 +326,22 @@ __device__ __forceinline__ void write_sum(const SumArgs &a, int token, int at, c
     constexpr int n = Vec<T>::n;
     T *row = static_cast<T *>(a.grad_table) + (int64_t)token * a.grad_table_stride;
     float x[n];
+#pragma unroll
+    for (int i = 0; i < n; ++i) x[i] = a.scale * acc[i];
     if (a.accumulate) {
-        load_part<T>(row, at, a.hidden, x);
+        const typename Vec<T>::type v = load_part<T>(row, at, a.hidden);
 #pragma unroll
-        for (int i = 0; i < n; ++i) x[i] += a.scale * acc[i];
-    } else {
-#pragma unroll
-        for (int i = 0; i < n; ++i) x[i] = a.scale * acc[i];
+        for (int i = 0; i < n; ++i) x[i] += (float)v[i];
     }
     store_part<T>(row, at, a.hidden, x);
 }
 
-template <typename T>
-__device__ __forceinline__ void write_partial(const SumArgs &a, int chunk, int which, int at, const float (&acc)[Vec<T>::n])
+template <int N>
+__device__ __forceinline__ void write_partial(const SumArgs &a, int chunk, int which, int at, const float (&acc)[N])
 {
-    float *p = a.partial + ((int64_t)chunk * 2 + which) * a.hidden;
+    float *p = a.partial + ((int64_t)chunk * 2 + which) * a.width + at;
 #pragma unroll
-    for (int i = 0; i < Vec<T>::n; ++i)
-        if (at + i < a.hidden) p[at + i] = acc[i];
+    for (int i = 0; i < N; i += 4) *reinterpret_cast<f32x4 *>(p + i) = f32x4{acc[i], acc[i + 1], acc[i + 2], acc[i + 3]};
 }
 
 template <typename T>
@@ -237,27 +352,31 @@ __global__ void __launch_bounds__(256) embed_sum_kernel(SumArgs a)
     const int chunk = blockIdx.x * per_block + threadIdx.x / a.lanes;
     const int at = (blockIdx.y * a.lanes + threadIdx.x % a.lanes) * n;
     if (chunk >= a.chunks || at >= a.hidden) return;
-    const int first = chunk * kChunk, last = min(first + kChunk, a.n);
+    const int first = chunk * a.chunk, last = min(first + a.chunk, a.n);
     int token = a.keys[first];
     bool from_left = first > 0 && a.keys[first - 1] == token;
     float acc[n] = {};
     for (int p = first; p < last; p += kBatch) {
-        int key[kBatch];
-        float x[kBatch][n];
+        int key[kBatch], row[kBatch];
+        typename Vec<T>::type x[kBatch];
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            const int i = min(p + j, last - 1);
+            key[j] = a.keys[i];
+            row[j] = a.rows[i];
+        }
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) {   // a batch's rows are on their way together
-            key[j] = p + j < last ? a.keys[p + j] : a.vocab;
-#pragma unroll
-            for (int i = 0; i < n; ++i) x[j][i] = 0.0f;
+            x[j] = typename Vec<T>::type{};
             if (key[j] < a.vocab)
-                load_part<T>(static_cast<const T *>(a.grad_out) + (int64_t)a.rows[p + j] * a.grad_out_stride, at, a.hidden, x[j]);
+                x[j] = load_part<T>(static_cast<const T *>(a.grad_out) + (int64_t)row[j] * a.grad_out_stride, at, a.hidden);
         }
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) {
             if (p + j >= last) break;
             if (key[j] != token) {
                 if (token < a.vocab) {
-                    if (from_left) write_partial<T>(a, chunk, 0, at, acc);
+                    if (from_left) write_partial(a, chunk, 0, at, acc);
                     else write_sum<T>(a, token, at, acc);
                 }
                 token = key[j];
@@ -266,13 +385,13 @@ __global__ void __launch_bounds__(256) embed_sum_kernel(SumArgs a)
                 for (int i = 0; i < n; ++i) acc[i] = 0.0f;
             }
 #pragma unroll
-            for (int i = 0; i < n; ++i) acc[i] += x[j][i];
+            for (int i = 0; i < n; ++i) acc[i] += (float)x[j][i];
         }
     }
     if (token >= a.vocab) return;
     const bool to_right = last < a.n && a.keys[last] == token;
-    if (from_left) write_partial<T>(a, chunk, 0, at, acc);
-    else if (to_right) write_partial<T>(a, chunk, 1, at, acc);
+    if (from_left) write_partial(a, chunk, 0, at, acc);
+    else if (to_right) write_partial(a, chunk, 1, at, acc);
     else write_sum<T>(a, token, at, acc);
 }
 
@@ -285,22 +404,35 @@ __global__ void __launch_bounds__(256) embed_join_kernel(SumArgs a)
     const int chunk = blockIdx.x * per_block + threadIdx.x / a.lanes;
     const int at = (blockIdx.y * a.lanes + threadIdx.x % a.lanes) * n;
     if (chunk >= a.chunks || at >= a.hidden) return;
-    const int first = chunk * kChunk, end = first + kChunk;
+    const int first = chunk * a.chunk, end = first + a.chunk;
     if (end >= a.n) return;
     const int token = a.keys[end - 1];
     if (token >= a.vocab || a.keys[end] != token) return;               // nothing goes on
     if (a.keys[first] == token && first > 0 && a.keys[first - 1] == token) return;   // it began further left
     float acc[n];
-    load_part<float>(a.partial + ((int64_t)chunk * 2 + 1) * a.hidden, at, a.hidden, reinterpret_cast<float(&)[4]>(acc[0]));
-    if (n == 8) load_part<float>(a.partial + ((int64_t)chunk * 2 + 1) * a.hidden, at + 4, a.hidden, reinterpret_cast<float(&)[4]>(acc[n - 4]));
-    for (int c = chunk + 1; c < a.chunks && a.keys[c * kChunk] == token; ++c) {
-        const float *p = a.partial + (int64_t)c * 2 * a.hidden;
+    const float *p = a.partial + ((int64_t)chunk * 2 + 1) * a.width + at;
 #pragma unroll
-        for (int k = 0; k < n; k += 4) {
-            float x[4];
-            load_part<float>(p, at + k, a.hidden, x);
+    for (int i = 0; i < n; ++i) acc[i] = p[i];
+    p = a.partial + at;
+    bool on = true;
+    for (int c = chunk + 1; on && c < a.chunks; c += kJoin) {   // several chunks' sums are on their way together
+        int key[kJoin];
+        f32x4 x[kJoin][n / 4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) acc[k + i] += x[i];
+        for (int j = 0; j < kJoin; ++j) {
+            const int from = min(c + j, a.chunks - 1);
+            key[j] = c + j < a.chunks ? a.keys[from * a.chunk] : -1;
+#pragma unroll
+            for (int k = 0; k < n / 4; ++k)
+                x[j][k] = *reinterpret_cast<const f32x4 *>(p + (int64_t)from * 2 * a.width + k * 4);
+        }
+#pragma unroll
+        for (int j = 0; j < kJoin; ++j) {
+            on = on && key[j] == token;
+            if (on) {
+#pragma unroll
+                for (int i = 0; i < n; ++i) acc[i] += x[j][i / 4][i % 4];
+            }
         }
     }
     write_sum<T>(a, token, at, acc);
@@ -341,42 +473,60 @@ Layout layout(int64_t rows, int64_t hidden)
     l.keys_b = take(rows * 4);
     l.rows_b = take(rows * 4);
     l.hist = take((rows + kSortBlock - 1) / kSortBlock * kDigits * 4);
-    l.partial = take((rows + kChunk - 1) / kChunk * 2 * hidden * 4);
+    const int64_t by_16 = (rows + 15) / 16, by_256 = (rows + 255) / 256;
+    const int64_t chunks = by_16 < 1024 ? by_16 : by_256 > 1024 ? by_256 : 1024;   // the most of any shorter list
+    l.partial = take(chunks * 2 * ((hidden + 7) / 8 * 8) * 4);
     l.bytes = at;
     return l;
 }
 
 template <typename T>
-hipError_t grad_launch(const EmbedPlan &plan, const deft_embed_grad_t &e, char *scratch, hipStream_t st)
+hipError_t grad_launch(const EmbedPlan &plan, const deft_embed_grad_t &e, char *scratch, int compute_units, hipStream_t st)
 {
     T *table = static_cast<T *>(e.grad_table);
-    if (!e.accumulate) {
-        const int blocks = (e.vocab + 3) / 4;
-        zero_rows_kernel<T><<<blocks < 4096 ? blocks : 4096, 256, 0, st>>>(table, e.grad_table_stride, e.vocab, e.hidden);
-    }
-    if (e.n_rows == 0) return hipGetLastError();
     const Layout l = layout(plan.max_rows, plan.max_hidden);
     int32_t *keys[2] = {reinterpret_cast<int32_t *>(scratch + l.keys_a), reinterpret_cast<int32_t *>(scratch + l.keys_b)};
     int32_t *rows[2] = {reinterpret_cast<int32_t *>(scratch + l.rows_a), reinterpret_cast<int32_t *>(scratch + l.rows_b)};
-    SortArgs s{};
-    s.n = e.n_rows;
-    s.vocab = e.vocab;
-    s.hist = reinterpret_cast<int32_t *>(scratch + l.hist);
-    s.blocks = (e.n_rows + kSortBlock - 1) / kSortBlock;
     const int bits = bits_of(e.vocab);
     int out = 0;
-    for (int shift = 0; shift < bits; shift += 8, out ^= 1) {
-        s.shift = shift;
-        s.tokens = shift == 0 ? e.tokens : nullptr;
-        s.keys_in = keys[out ^ 1];
-        s.rows_in = rows[out ^ 1];
-        s.keys_out = keys[out];
-        s.rows_out = rows[out];
-        sort_count_kernel<<<s.blocks, kSortThreads, 0, st>>>(s);
-        sort_scan_kernel<<<1, 1024, 0, st>>>(s.hist, s.blocks * kDigits);
-        sort_place_kernel<<<s.blocks, kSortThreads, 0, st>>>(s);
+    if (e.n_rows > 0 && e.n_rows <= kSmall && e.vocab < kSmallVocab) {
+        SmallArgs s{};
+        s.n = e.n_rows;
+        s.vocab = e.vocab;
+        s.hidden = e.hidden;
+        s.passes = (bits + 7) / 8;
+        s.digit_bits = (bits + s.passes - 1) / s.passes;
+        s.tokens = e.tokens;
+        s.keys = keys[0];
+        s.rows = rows[0];
+        s.table = table;
+        s.stride = e.grad_table_stride;
+        const int shares = e.accumulate ? 0 : e.vocab < compute_units - 1 ? e.vocab : compute_units - 1;
+        sort_small_kernel<T><<<1 + shares, kSmallThreads, 0, st>>>(s);
+    } else {
+        if (!e.accumulate) {
+            const int blocks = (e.vocab + 3) / 4;
+            zero_rows_kernel<T><<<blocks < 4096 ? blocks : 4096, 256, 0, st>>>(table, e.grad_table_stride, e.vocab, e.hidden);
+        }
+        if (e.n_rows == 0) return hipGetLastError();
+        SortArgs s{};
+        s.n = e.n_rows;
+        s.vocab = e.vocab;
+        s.hist = reinterpret_cast<int32_t *>(scratch + l.hist);
+        s.blocks = (e.n_rows + kSortBlock - 1) / kSortBlock;
+        for (int shift = 0; shift < bits; shift += 8, out ^= 1) {
+            s.shift = shift;
+            s.tokens = shift == 0 ? e.tokens : nullptr;
+            s.keys_in = keys[out ^ 1];
+            s.rows_in = rows[out ^ 1];
+            s.keys_out = keys[out];
+            s.rows_out = rows[out];
+            sort_count_kernel<<<s.blocks, kSortThreads, 0, st>>>(s);
+            sort_scan_kernel<<<1, 1024, 0, st>>>(s.hist, s.blocks * kDigits);
+            sort_place_kernel<<<s.blocks, kSortThreads, 0, st>>>(s);
+        }
+        out ^= 1;
     }
-    out ^= 1;
     SumArgs a{};
     a.n = e.n_rows;
     a.vocab = e.vocab;
@@ -390,7 +540,9 @@ hipError_t grad_launch(const EmbedPlan &plan, const deft_embed_grad_t &e, char *
     a.grad_table = e.grad_table;
     a.grad_table_stride = e.grad_table_stride;
     a.partial = reinterpret_cast<float *>(scratch + l.partial);
-    a.chunks = (e.n_rows + kChunk - 1) / kChunk;
+    a.width = (e.hidden + 7) / 8 * 8;
+    a.chunk = chunk_of(e.n_rows);
+    a.chunks = (e.n_rows + a.chunk - 1) / a.chunk;
     const int parts = (e.hidden + Vec<T>::n - 1) / Vec<T>::n;
     a.lanes = 8;
     while (a.lanes < parts && a.lanes < 256) a.lanes *= 2;
@@ -420,12 +572,13 @@ hipError_t embed_launch(int dtype, const deft_embed_t &e, hipStream_t st)
     return hipGetLastError();
 }
 
-hipError_t embed_grad_launch(const EmbedPlan &plan, int dtype, const deft_embed_grad_t &e, void *scratch, int, hipStream_t st)
+hipError_t embed_grad_launch(const EmbedPlan &plan, int dtype, const deft_embed_grad_t &e, void *scratch, int compute_units,
+                             hipStream_t st)
 {
     char *s = static_cast<char *>(scratch);
-    if (dtype == DEFT_F32) return grad_launch<float>(plan, e, s, st);
-    if (dtype == DEFT_F16) return grad_launch<f16>(plan, e, s, st);
-    return grad_launch<bf16>(plan, e, s, st);
+    if (dtype == DEFT_F32) return grad_launch<float>(plan, e, s, compute_units, st);
+    if (dtype == DEFT_F16) return grad_launch<f16>(plan, e, s, compute_units, st);
+    return grad_launch<bf16>(plan, e, s, compute_units, st);
 }
 
 }  // namespace deft
