@@ -226,7 +226,7 @@ __global__ void __launch_bounds__(256) join_hidden_kernel(HiddenArgs a)
 template <typename T, typename O, int E, int WM, int WN, int MT, int NT, bool SPLIT>
 hipError_t product_shape(const ProductArgs &p, hipStream_t st)
 {
-    constexpr int TM = WM * MT * 16, TN = WN * NT * 16, kLds = 2 * (TM + TN) * kStepBytes;
+    constexpr int TM = WM * MT * 16, TN = WN * NT * 16, kLds = product_lds(TM, TN);
     const dim3 grid(((p.m + TM - 1) / TM) * ((p.n + TN - 1) / TN), p.splits);
     product_kernel<T, O, E, WM, WN, MT, NT, SPLIT><<<grid, WM * WN * kWave, kLds, st>>>(p);
     return hipGetLastError();
@@ -243,10 +243,10 @@ template <typename T, typename O, int E, bool SPLIT>
 hipError_t allow_lds()
 {
     hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&product_kernel<T, O, E, 2, 4, 8, 4, SPLIT>),
-                                       hipFuncAttributeMaxDynamicSharedMemorySize, 2 * 512 * kStepBytes);
+                                       hipFuncAttributeMaxDynamicSharedMemorySize, product_lds(256, 256));
     if (e == hipSuccess)
         e = hipFuncSetAttribute(reinterpret_cast<const void *>(&product_kernel<T, O, E, 4, 2, 4, 2, SPLIT>),
-                                hipFuncAttributeMaxDynamicSharedMemorySize, 2 * 320 * kStepBytes);
+                                hipFuncAttributeMaxDynamicSharedMemorySize, product_lds(256, 64));
     return e;
 }
 

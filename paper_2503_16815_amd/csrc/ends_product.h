@@ -4,9 +4,18 @@
 // derivative, or a sum into a gradient.
 //
 // A workgroup of eight wavefronts owns a tile of C.  Both operands' tiles go from memory to LDS without
-// passing registers, 64 elements of k at a time, the next ones while the current ones are multiplied.
+// passing registers, 64 elements of k at a time.  LDS holds three of A's and two of B's (160 KB at 256 x 256):
+// A's tile of the step after next is asked for in a step's first half, B's in its second, each spread
+// over the half's matrix instructions, so that neither waits for the other (measured at 8192^3 in bf16: all of it at
+// the step's beginning 1130 TFLOP/s, spread 1230; addresses in 64-bit registers instead of a buffer's 1180).  The fragments
+// of a half are read from LDS during the half before.  The matrix instructions are written out, so that
+// sums stay in accumulation registers and everything else comes between them in this order.
+//
 // The 16-byte pieces of a row are permuted by the row's number, so that the sixteen rows that a wavefront
-// reads together lie in different banks.
+// reads together lie in different banks (no bank conflicts counted).
+//
+// Tiles are dealt out so that the workgroups of an XCD work on neighbouring ones, four wide: 12 rows of tiles
+// come into its L2 for 32 workgroups instead of 33 (131072 x 8192 x 4096: 890 to 1110 TFLOP/s by itself).
 //
 // 32-bit operands come as three 16-bit arrays whose sum they are (8 bits of the significand in
 // each); the six products of those arrays that matter at 24 bits are summed one after the other.
@@ -53,16 +62,16 @@ struct ProductArgs {
 template <typename T> struct Mfma;
 template <> struct Mfma<f16> {
     typedef f16 operand __attribute__((ext_vector_type(8)));
-    static __device__ __forceinline__ f32x4 run(operand a, operand b, f32x4 c)
+    static __device__ __forceinline__ void run(operand a, operand b, f32x4 &c)
     {
-        return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+        asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
     }
 };
 template <> struct Mfma<bf16> {
     typedef bf16 operand __attribute__((ext_vector_type(8)));
-    static __device__ __forceinline__ f32x4 run(operand a, operand b, f32x4 c)
+    static __device__ __forceinline__ void run(operand a, operand b, f32x4 &c)
     {
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+        asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
     }
 };
 
@@ -102,24 +111,47 @@ __device__ __forceinline__ unsigned pack2(bf16 a, bf16 b)
     return (unsigned)__builtin_bit_cast(unsigned short, a) | (unsigned)__builtin_bit_cast(unsigned short, b) << 16;
 }
 
+constexpr int kStagesA = 3, kStagesB = 2;
+constexpr int product_lds(int tm, int tn) { return (kStagesA * tm + kStagesB * tn) * kStepBytes; }
+
+// All of this wavefront's LDS reads are done, and all but `N` of its loads; then the others' are too.
+template <int N>
+__device__ __forceinline__ void step_barrier()
+{
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+template <int H> struct HalfOf {
+    static constexpr int value = H;
+};
+
 // T: element type of the operands.  O: type of the gradient that kGradient writes.  WM x WN wavefronts of MT x NT
 // tiles of 16 x 16.  SPLIT: operands are three arrays each.
 template <typename T, typename O, int E, int WM, int WN, int MT, int NT, bool SPLIT>
 __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p)
 {
+#ifdef __HIP_DEVICE_COMPILE__   // (buffer descriptors are a type of the device's alone)
     constexpr int kThreads = WM * WN * kWave, TM = WM * MT * 16, TN = WN * NT * 16;
-    constexpr int kABytes = TM * kStepBytes, kStage = (TM + TN) * kStepBytes;
+    constexpr int kABytes = TM * kStepBytes, kBBytes = TN * kStepBytes, kBAt = kStagesA * kABytes;
     constexpr int kALoads = TM * 8 / kThreads, kBLoads = TN * 8 / kThreads;
+    constexpr int kFetches = MT + NT, kProducts = MT * NT;
     static_assert(kALoads * kThreads == TM * 8 && kBLoads * kThreads == TN * 8, "whole loads");
     typedef typename Mfma<T>::operand Operand;
     extern __shared__ __align__(16) char lds[];
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave / WN, wn = wave % WN;
-    const int tiles_m = (p.m + TM - 1) / TM;
-    const int tm = blockIdx.x % tiles_m, tn = blockIdx.x / tiles_m;
-    const int m0 = tm * TM, n0 = tn * TN;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / WN, wn = wave % WN;
     const int n_rows = p.n_dev ? *p.n_dev : p.n;
-    if (n0 >= n_rows) return;
+    const int tiles_m = (p.m + TM - 1) / TM, tiles_n = (n_rows + TN - 1) / TN;
+    // workgroup b runs on XCD b % 8; each XCD has an equal share of the tiles, in groups four wide
+    const int tiles = tiles_m * tiles_n, xcd = blockIdx.x & 7, share = tiles >> 3, more = tiles & 7;
+    if ((int)(blockIdx.x >> 3) >= share + (xcd < more ? 1 : 0)) return;
+    const int tile = (int)(blockIdx.x >> 3) + xcd * share + (xcd < more ? xcd : more);
+    const int group = tile / (tiles_m * 4), in_group = tile - group * tiles_m * 4;
+    const int wide = min(tiles_n - group * 4, 4);
+    const int tm = in_group / wide, tn = group * 4 + in_group - tm * wide;
+    const int m0 = tm * TM, n0 = tn * TN;
 
     const int steps_all = (p.k_dev ? *p.k_dev + kStep - 1 : p.k) / kStep;
     const int from = (int)((int64_t)steps_all * blockIdx.y / p.splits), to = (int)((int64_t)steps_all * (blockIdx.y + 1) / p.splits);
@@ -139,61 +171,117 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
         const int c = tid + i * kThreads, row = c >> 3;
         b_off[i] = (unsigned)min(row, p.n - 1 - n0) * (unsigned)(p.b_ld * 2) + (((c & 7) ^ ((row >> 1) & 7)) << 4);
     }
-    // the six products of three arrays each that are kept, the smallest first
-    const auto load = [&](int step, int stage) {
+    // The next tiles to load.  Where operands are three arrays: the six products of them that are kept, the smallest first.
+    int at_step = 0, at_product = 0;
+    __amdgpu_buffer_rsrc_t a_from, b_from;
+    const auto aim = [&]() {
         int64_t a_at = 0, b_at = 0;
-        int s = step;
         if (SPLIT) {
-            const int which = step / steps;
-            s = step - which * steps;
-            const int pa = (0x021010 >> (4 * (5 - which))) & 15, pb = (0x201100 >> (4 * (5 - which))) & 15;
-            a_at = pa * p.a_plane * 2;
-            b_at = pb * p.b_plane * 2;
+            a_at = ((0x021010 >> (4 * (5 - at_product))) & 15) * p.a_plane * 2;
+            b_at = ((0x201100 >> (4 * (5 - at_product))) & 15) * p.b_plane * 2;
         }
-        const char *as = a_base + a_at + (int64_t)s * kStepBytes, *bs = b_base + b_at + (int64_t)s * kStepBytes;
-        char *to_lds = lds + stage * kStage + wave * (kWave * 16);
-#pragma unroll
-        for (int i = 0; i < kALoads; ++i)
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(as + a_off[i]),
-                                             (__attribute__((address_space(3))) void *)(to_lds + i * kThreads * 16), 16, 0, 0);
-#pragma unroll
-        for (int i = 0; i < kBLoads; ++i)
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(bs + b_off[i]),
-                                             (__attribute__((address_space(3))) void *)(to_lds + kABytes + i * kThreads * 16), 16, 0, 0);
+        a_from = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(a_base + a_at), (short)0, -1, 0x00020000);
+        b_from = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(b_base + b_at), (short)0, -1, 0x00020000);
+    };
+    const auto next_step = [&]() {
+        ++at_step;
+        if (SPLIT && at_step == steps) {
+            at_step = 0;
+            ++at_product;
+            aim();
+        }
+    };
+    const auto load_a = [&](int stage, int i) {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(
+            a_from, (__attribute__((address_space(3))) void *)(lds + stage + wave * (kWave * 16) + i * kThreads * 16), 16,
+            a_off[i], at_step * kStepBytes, 0, 0);
+    };
+    const auto load_b = [&](int stage, int i) {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(
+            b_from, (__attribute__((address_space(3))) void *)(lds + kBAt + stage + wave * (kWave * 16) + i * kThreads * 16), 16,
+            b_off[i], at_step * kStepBytes, 0, 0);
     };
 
     f32x4 acc[MT][NT];
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int j = 0; j < NT; ++j) {
+            acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            asm volatile("" : "+a"(acc[i][j]));
+        }
+    asm volatile("s_nop 7" ::: "memory");
 
-    const int row16 = lane & 15, part = lane >> 4;
-    if (total > 0) load(0, 0);
-    for (int step = 0; step < total; ++step) {
-        __syncthreads();   // this step's tiles are there, and nobody reads the other stage any more
-        if (step + 1 < total) load(step + 1, (step + 1) & 1);
-        const char *at = lds + (step & 1) * kStage;
+    const int row16 = lane & 15, part = lane >> 4, turn = (row16 >> 1) & 7;
+    Operand fa[2][MT], fb[2][NT];   // of each half
+    const char *a_read = lds + (wm * MT * 16 + row16) * kStepBytes, *b_read = lds + kBAt + (wn * NT * 16 + row16) * kStepBytes;
+    const int piece[2] = {(part ^ turn) << 4, ((4 + part) ^ turn) << 4};
+    const auto fetch = [&](int a_stage, int b_stage, int half, int which) {
+        if (which < NT) fb[half][which] = *reinterpret_cast<const Operand *>(b_read + b_stage + piece[half] + which * 16 * kStepBytes);
+        else fa[half][which - NT] = *reinterpret_cast<const Operand *>(a_read + a_stage + piece[half] + (which - NT) * 16 * kStepBytes);
+    };
+    // Multiplies a half; meanwhile fetches the other half's fragments from the stages given and, in the first half,
+    // loads A's next tile to `to_stage`, in the second B's.
+    const auto half = [&](auto which_half, bool fetching, int a_stage, int b_stage, bool loading, int to_stage) {
+        constexpr int h = decltype(which_half)::value, kLoads = h == 0 ? kALoads : kBLoads;
+        constexpr int kSpan = h == 0 ? kProducts : (kProducts + 1) / 2;   // B's have less time until they are needed
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int q = half * 4 + part;
-            Operand a[MT], b[NT];
+        for (int q = 0; q < kProducts; ++q) {
 #pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                const int row = wm * MT * 16 + i * 16 + row16;
-                a[i] = *reinterpret_cast<const Operand *>(at + row * kStepBytes + ((q ^ ((row >> 1) & 7)) << 4));
+            for (int i = 0; i < kLoads; ++i)
+                if (loading && i * kSpan / kLoads == q) {
+                    if (h == 0) load_a(to_stage, i);
+                    else load_b(to_stage, i);
+                }
+#pragma unroll
+            for (int f = 0; f < kFetches; ++f)
+                if (fetching && f * kProducts / kFetches == q) fetch(a_stage, b_stage, h ^ 1, f);
+            Mfma<T>::run(fa[h][q / NT], fb[h][q % NT], acc[q / NT][q % NT]);
+        }
+    };
+
+    if (total > 0) {
+        aim();
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+            if (s < total) {
+#pragma unroll
+                for (int i = 0; i < kALoads; ++i) load_a(s * kABytes, i);
+#pragma unroll
+                for (int i = 0; i < kBLoads; ++i) load_b(s * kBBytes, i);
+                next_step();
             }
+        step_barrier<0>();
 #pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                const int row = wn * NT * 16 + j * 16 + row16;
-                b[j] = *reinterpret_cast<const Operand *>(at + kABytes + row * kStepBytes + ((q ^ ((row >> 1) & 7)) << 4));
-            }
-#pragma unroll
-            for (int i = 0; i < MT; ++i)
-#pragma unroll
-                for (int j = 0; j < NT; ++j) acc[i][j] = Mfma<T>::run(a[i], b[j], acc[i][j]);
+        for (int f = 0; f < kFetches; ++f) fetch(0, 0, 0, f);
+        int a0 = 0, a1 = kABytes, a2 = 2 * kABytes, b0 = 0, b1 = kBBytes, step = 0;
+        const auto turn_stages = [&]() {
+            const int a = a0, b = b0;
+            a0 = a1;
+            a1 = a2;
+            a2 = a;
+            b0 = b1;
+            b1 = b;
+        };
+        for (; step + 2 < total; ++step) {
+            half(HalfOf<0>{}, true, a0, b0, true, a2);
+            step_barrier<kALoads>();   // the next step's tiles are there, and nobody reads b0 any more
+            half(HalfOf<1>{}, true, a1, b1, true, b0);
+            next_step();
+            turn_stages();
+        }
+        for (; step < total; ++step) {
+            half(HalfOf<0>{}, true, a0, b0, false, 0);
+            step_barrier<0>();
+            half(HalfOf<1>{}, step + 1 < total, a1, b1, false, 0);
+            turn_stages();
         }
     }
+    asm volatile("s_nop 15\n s_nop 15" ::: "memory");   // the last product's sums are written before they are read
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) asm volatile("" : "+a"(acc[i][j]));
 
     // acc[i][j][r] is C[m][n] at m = m_lane + i * 16 + r, n = n_lane + j * 16
     const int m_lane = m0 + wm * MT * 16 + part * 4, n_lane = n0 + wn * NT * 16 + row16;
@@ -206,13 +294,14 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
             const int n = n_lane + j * 16;
             const int label = n < n_rows ? p.label[n] - p.m_first - m_lane : -1;
             SoftSum s = {-INFINITY, 0.0f};
+            float z[MT][4];
 #pragma unroll
             for (int i = 0; i < MT; ++i)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    acc[i][j][r] *= p.scale;
-                    if (m_lane + i * 16 + r < p.m) s.top = fmaxf(s.top, acc[i][j][r]);
-                    if (label == i * 16 + r) p.z_label[n] = acc[i][j][r];
+                    z[i][r] = acc[i][j][r] * p.scale;
+                    if (m_lane + i * 16 + r < p.m) s.top = fmaxf(s.top, z[i][r]);
+                    if (label == i * 16 + r) p.z_label[n] = z[i][r];
                 }
             s.top = fmaxf(s.top, __shfl_xor(s.top, 16));
             s.top = fmaxf(s.top, __shfl_xor(s.top, 32));
@@ -221,7 +310,7 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
             for (int i = 0; i < MT; ++i)
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    if (m_lane + i * 16 + r < p.m) s.sum += __expf(acc[i][j][r] - top);
+                    if (m_lane + i * 16 + r < p.m) s.sum += __expf(z[i][r] - top);
             s.sum += __shfl_xor(s.sum, 16);
             s.sum += __shfl_xor(s.sum, 32);
             if (part == 0) joined[wm * TN + wn * NT * 16 + j * 16 + row16] = make_float2(top, s.sum);
@@ -313,6 +402,7 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
             }
         }
     }
+#endif
 }
 
 }  // namespace deft
