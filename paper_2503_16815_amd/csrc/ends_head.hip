@@ -19,6 +19,7 @@ constexpr int kTile = 256;
 constexpr int64_t kPieceBytes = (int64_t)1 << 29;    // of d and d^T together
 constexpr int64_t kWeightBytes = (int64_t)1 << 28;   // of a piece's rows, packed or transposed
 constexpr int kMaxSplits = 16;
+constexpr int kFew = 64;                             // positions that a tile of 64 holds
 
 int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
@@ -190,6 +191,41 @@ __global__ void __launch_bounds__(256) join_loss_kernel(JoinArgs a)
     }
 }
 
+// Up to 64 positions are not packed together: those without a label are left out here.
+struct FewArgs {
+    int n, vocab, tiles;
+    const int32_t *labels;
+    const float2 *parts;
+    const float *z_label;
+    float *loss, *lse;
+    int32_t *status;
+};
+
+__global__ void __launch_bounds__(256) join_few_kernel(FewArgs a)
+{
+    __shared__ SoftSum of_wave[4];
+    const int row = blockIdx.x, tid = threadIdx.x;
+    const int label = a.labels[row];
+    SoftSum s = {-INFINITY, 0.0f};
+    for (int t = tid; t < a.tiles; t += 256) {
+        const float2 x = a.parts[(int64_t)row * a.tiles + t];
+        s = soft_join(s, SoftSum{x.x, x.y});
+    }
+    const float top = wave_max(s.top);
+    s.sum = wave_sum(s.sum == 0.0f ? 0.0f : s.sum * __expf(s.top - top));
+    if ((tid & 63) == 0) of_wave[tid >> 6] = SoftSum{top, s.sum};
+    __syncthreads();
+    if (tid != 0) return;
+    s = of_wave[0];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) s = soft_join(s, of_wave[w]);
+    const bool in = label >= 0 && label < a.vocab;
+    const float lse = s.top + __logf(s.sum);
+    a.lse[row] = in ? lse : 0.0f;
+    a.loss[row] = in ? lse - a.z_label[row] : 0.0f;
+    if (a.status) a.status[row] = in || label == -1 ? DEFT_OK : DEFT_ERR_INVALID_ARG;
+}
+
 struct HiddenArgs {
     int n, hidden, splits;
     const int *at_of;
@@ -215,13 +251,55 @@ __global__ void __launch_bounds__(256) join_hidden_kernel(HiddenArgs a)
                 x += *reinterpret_cast<const f32x4 *>(a.sums + s * a.sums_split + (int64_t)at * a.sums_ld + c);
             x *= alpha;
         }
+        if (c + 4 <= a.hidden) {
+            typedef O O4 __attribute__((ext_vector_type(4), aligned(sizeof(O))));
+            *reinterpret_cast<O4 *>(out + c) = O4{(O)x[0], (O)x[1], (O)x[2], (O)x[3]};
+        } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (c + i < a.hidden) out[c + i] = (O)x[i];
+            for (int i = 0; i < 4; ++i)
+                if (c + i < a.hidden) out[c + i] = (O)x[i];
+        }
     }
 }
 
 // ---- launches -------------------------------------------------------------------------------
+
+// The shape of a product's tiles.  Up to 64 rows of b: 256 x 64, bound by reading a.  Otherwise 256 x 256, one workgroup to
+// a compute unit, or 128 x 128, two to a compute unit (80 KB of LDS each), where that leaves fewer of them idle.
+enum Shape { kLarge, kSmall, kNarrow };
+
+// Rounds of the 256 x 256 shape that the tiles take.  A pair of small tiles on a compute unit takes 0.59 of a large one's
+// time, one alone 0.36.
+double rounds_of(Shape shape, int64_t m, int64_t n, int64_t splits, int64_t compute_units)
+{
+    if (shape == kNarrow) return (double)up(up(m, 256) / 256 * splits, compute_units) / (double)compute_units;
+    if (shape == kLarge) return (double)up(up(m, 256) / 256 * (up(n, 256) / 256) * splits, compute_units) / (double)compute_units;
+    const int64_t tiles = up(m, 128) / 128 * (up(n, 128) / 128) * splits, rest = tiles % (2 * compute_units);
+    return 0.59 * (double)(tiles / (2 * compute_units)) + (rest == 0 ? 0.0 : rest <= compute_units ? 0.36 : 0.59);
+}
+
+Shape shape_of(int64_t m, int64_t n, int64_t splits, int64_t compute_units)
+{
+    if (n <= kFew) return kNarrow;
+    return rounds_of(kSmall, m, n, splits, compute_units) < rounds_of(kLarge, m, n, splits, compute_units) ? kSmall : kLarge;
+}
+
+// Parts that a sum over k is cut into, where its tiles leave compute units idle: each part's sums go to memory and are
+// joined later, so there are no more of them than shorten the whole by a twentieth.
+int splits_of(int64_t m, int64_t n, int64_t k, int64_t compute_units)
+{
+    const int64_t tiles = up(m, 256) / 256 * (n <= kFew ? 1 : up(n, 256) / 256);
+    int best = 1;
+    double least = 1e30;
+    for (int s = 1; s <= kMaxSplits && (s == 1 || (tiles * s <= 2 * compute_units && k / kStep >= s * 8)); s *= 2) {
+        const double t = rounds_of(shape_of(m, n, s, compute_units), m, n, s, compute_units) / s;
+        if (t < 0.95 * least) {
+            least = t;
+            best = s;
+        }
+    }
+    return best;
+}
 
 template <typename T, typename O, int E, int WM, int WN, int MT, int NT, bool SPLIT>
 hipError_t product_shape(const ProductArgs &p, hipStream_t st)
@@ -233,20 +311,22 @@ hipError_t product_shape(const ProductArgs &p, hipStream_t st)
 }
 
 template <typename T, typename O, int E, bool SPLIT>
-hipError_t product(const ProductArgs &p, hipStream_t st)
+hipError_t product(const ProductArgs &p, Shape shape, hipStream_t st)
 {
-    if (p.n > 64) return product_shape<T, O, E, 2, 4, 8, 4, SPLIT>(p, st);
-    return product_shape<T, O, E, 4, 2, 4, 2, SPLIT>(p, st);
+    if (shape == kNarrow) return product_shape<T, O, E, 4, 2, 4, 2, SPLIT>(p, st);
+    if (shape == kSmall) return product_shape<T, O, E, 2, 2, 4, 4, SPLIT>(p, st);
+    return product_shape<T, O, E, 2, 4, 8, 4, SPLIT>(p, st);
 }
 
 template <typename T, typename O, int E, bool SPLIT>
 hipError_t allow_lds()
 {
-    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&product_kernel<T, O, E, 2, 4, 8, 4, SPLIT>),
-                                       hipFuncAttributeMaxDynamicSharedMemorySize, product_lds(256, 256));
-    if (e == hipSuccess)
-        e = hipFuncSetAttribute(reinterpret_cast<const void *>(&product_kernel<T, O, E, 4, 2, 4, 2, SPLIT>),
-                                hipFuncAttributeMaxDynamicSharedMemorySize, product_lds(256, 64));
+    const auto allow = [](const void *kernel, int tm, int tn) {
+        return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, product_lds(tm, tn));
+    };
+    hipError_t e = allow(reinterpret_cast<const void *>(&product_kernel<T, O, E, 2, 4, 8, 4, SPLIT>), 256, 256);
+    if (e == hipSuccess) e = allow(reinterpret_cast<const void *>(&product_kernel<T, O, E, 4, 2, 4, 2, SPLIT>), 256, 64);
+    if (e == hipSuccess) e = allow(reinterpret_cast<const void *>(&product_kernel<T, O, E, 2, 2, 4, 4, SPLIT>), 128, 128);
     return e;
 }
 
@@ -309,9 +389,9 @@ struct Head {
         return hipGetLastError();
     }
 
-    // the positions that count, packed: hidden states (and, for the gradient, their transpose)
-    static hipError_t positions(const Scratch &s, const void *hidden_states, int64_t stride, int n, int hidden, bool transposed,
-                                hipStream_t st)
+    // hidden states (and, for the gradient, their transpose): of the positions that count, packed together, or of all
+    static hipError_t positions(const Scratch &s, const void *hidden_states, int64_t stride, int n, int hidden, bool counted,
+                                bool transposed, hipStream_t st)
     {
         const int64_t n_up = up(n, kTile), k = up(hidden, kStep);
         PackArgs h{};
@@ -319,8 +399,10 @@ struct Head {
         h.src_stride = stride;
         h.rows = n;
         h.cols = hidden;
-        h.row_of = s.row_of;
-        h.rows_dev = s.count;
+        if (counted) {
+            h.row_of = s.row_of;
+            h.rows_dev = s.count;
+        }
         h.out = s.hidden;
         h.out_ld = k;
         h.out_plane = n_up * k;
@@ -376,35 +458,64 @@ struct Head {
         return hipSuccess;
     }
 
-    static hipError_t loss(const HeadPlan &plan, const deft_head_loss_t &a, const Scratch &s, hipStream_t st)
+    static hipError_t loss(const HeadPlan &plan, const deft_head_loss_t &a, const Scratch &s, int compute_units, hipStream_t st)
     {
-        RowsArgs r{};
-        r.n = a.n_rows;
-        r.vocab = a.vocab;
-        r.labels = a.labels;
-        r.status = a.status;
-        r.loss = a.loss;
-        r.lse_out = a.lse;
-        r.count = s.count;
-        r.row_of = s.row_of;
-        r.at_of = s.at_of;
-        r.label = s.label;
-        r.t_scale = s.t_scale;
-        rows_kernel<<<1, 1024, 0, st>>>(r);
-        hipError_t e = positions(s, a.hidden_states, a.hidden_stride, a.n_rows, a.hidden, false, st);
-        const int tiles = (a.vocab + kTile - 1) / kTile;
+        const int n = a.n_rows;
+        const bool few = n <= kFew;
+        const bool from_caller = few && !kSplit && in_place(a.hidden_states, a.hidden_stride, a.hidden);
+        hipError_t e = hipSuccess;
+        if (!few) {
+            RowsArgs r{};
+            r.n = n;
+            r.vocab = a.vocab;
+            r.labels = a.labels;
+            r.status = a.status;
+            r.loss = a.loss;
+            r.lse_out = a.lse;
+            r.count = s.count;
+            r.row_of = s.row_of;
+            r.at_of = s.at_of;
+            r.label = s.label;
+            r.t_scale = s.t_scale;
+            rows_kernel<<<1, 1024, 0, st>>>(r);
+        }
+        if (!from_caller) e = positions(s, a.hidden_states, a.hidden_stride, n, a.hidden, !few, false, st);
         const bool whole = !kSplit && in_place(a.weight, a.weight_stride, a.hidden);   // nothing to pack: no pieces
-        const int piece = whole ? a.vocab : plan.piece;
+        const int piece = whole || a.vocab < plan.piece ? a.vocab : plan.piece;
+        const Shape shape = shape_of(piece, n, 1, compute_units);
+        const int tiles = (int)(up(a.vocab, shape == kSmall ? 128 : 256) / (shape == kSmall ? 128 : 256));
         for (int first = 0; first < a.vocab && e == hipSuccess; first += piece) {
             const int rows = a.vocab - first < piece ? a.vocab - first : piece;
             ProductArgs p;
-            e = logits(plan, s, a.weight, a.weight_stride, first, rows, a.n_rows, a.hidden, a.logit_scale, false, &p, st);
+            e = logits(plan, s, a.weight, a.weight_stride, first, rows, n, a.hidden, a.logit_scale, false, &p, st);
             p.parts = s.parts;
             p.parts_ld = tiles;
             p.z_label = s.z_label;
-            if (e == hipSuccess) e = product<T, S, kSoftmax, kSplit>(p, st);
+            if (few) {
+                p.n_dev = nullptr;
+                p.label = a.labels;
+            }
+            if (from_caller) {
+                p.b = a.hidden_states;
+                p.b_ld = a.hidden_stride;
+            }
+            if (e == hipSuccess) e = product<T, S, kSoftmax, kSplit>(p, shape, st);
         }
         if (e != hipSuccess) return e;
+        if (few) {
+            FewArgs f{};
+            f.n = n;
+            f.vocab = a.vocab;
+            f.tiles = tiles;
+            f.labels = a.labels;
+            f.parts = s.parts;
+            f.z_label = s.z_label;
+            f.loss = a.loss;
+            f.lse = a.lse;
+            f.status = a.status;
+            join_few_kernel<<<n, 256, 0, st>>>(f);
+            return hipGetLastError();
+        }
         JoinArgs j{};
         j.tiles = tiles;
         j.parts_ld = tiles;
@@ -414,7 +525,7 @@ struct Head {
         j.z_label = s.z_label;
         j.loss = a.loss;
         j.lse = a.lse;
-        join_loss_kernel<<<(a.n_rows + 3) / 4, 256, 0, st>>>(j);
+        join_loss_kernel<<<(n + 3) / 4, 256, 0, st>>>(j);
         return hipGetLastError();
     }
 
@@ -439,14 +550,9 @@ struct Head {
         r.t_top = kHalf ? 32768.0f : 0.0f;
         rows_kernel<<<1, 1024, 0, st>>>(r);
         hipError_t e = hipGetLastError();
-        if (e == hipSuccess && n > 0) e = positions(s, a.hidden_states, a.hidden_stride, n, a.hidden, a.grad_weight != nullptr, st);
+        if (e == hipSuccess && n > 0) e = positions(s, a.hidden_states, a.hidden_stride, n, a.hidden, true, a.grad_weight != nullptr, st);
 
-        int splits = 1;   // of a piece's part of grad_hidden, where its tiles leave compute units idle
-        if (n > 0) {
-            const int64_t tiles = up(a.hidden, kTile) / kTile * (n > 64 ? n_up / kTile : 1);
-            const int piece = plan.piece < a.vocab ? plan.piece : a.vocab;
-            while (splits < kMaxSplits && tiles * splits * 2 <= compute_units && piece / kStep >= splits * 8) splits *= 2;
-        }
+        const int splits = splits_of(a.hidden, n, plan.piece < a.vocab ? plan.piece : a.vocab, compute_units);
         int piece_number = 0;
         for (int first = 0; first < a.vocab && e == hipSuccess; first += plan.piece, ++piece_number) {
             const int rows = a.vocab - first < plan.piece ? a.vocab - first : plan.piece;
@@ -463,7 +569,7 @@ struct Head {
                 p.d_t = s.d_t;
                 p.d_t_ld = n_up;
                 p.d_t_plane = n_up * plan.piece;
-                if (e == hipSuccess) e = product<T, S, kDerivative, kSplit>(p, st);
+                if (e == hipSuccess) e = product<T, S, kDerivative, kSplit>(p, shape_of(rows, n, 1, compute_units), st);
             }
             if (e == hipSuccess && a.grad_weight) {
                 ProductArgs q{};
@@ -482,7 +588,7 @@ struct Head {
                 q.add = a.accumulate;
                 q.out = static_cast<S *>(a.grad_weight) + (int64_t)first * a.grad_weight_stride;
                 q.out_ld = a.grad_weight_stride;
-                e = product<T, S, kGradient, kSplit>(q, st);
+                e = product<T, S, kGradient, kSplit>(q, shape_of(a.hidden, rows, 1, compute_units), st);
             }
             if (e == hipSuccess && piece_number < a.n_piece_events)
                 e = hipEventRecord(static_cast<hipEvent_t>(a.piece_events[piece_number]), st);
@@ -503,7 +609,7 @@ struct Head {
                 q.sums_ld = sums_ld;
                 q.sums_split = n_up * sums_ld;
                 q.add = first > 0;
-                e = product<T, S, kSums, kSplit>(q, st);
+                e = product<T, S, kSums, kSplit>(q, shape_of(a.hidden, n, splits, compute_units), st);
             }
         }
         if (e != hipSuccess || !a.grad_hidden || n == 0) return e;
@@ -554,14 +660,14 @@ void head_plan(int dtype, int max_rows, int max_vocab, int max_hidden, bool grad
     plan->floats = take((64 + 3 * n) * 4);
     plan->hidden = take(plan->planes * n * k * 2);
     plan->weight = take(plan->planes * piece * k * 2);
-    plan->parts = take(n * ((max_vocab + kTile - 1) / kTile) * 8);
+    plan->parts = take(n * ((max_vocab + 127) / 128) * 8);
     if (grad) {
         plan->hidden_t = take(plan->planes * n * k * 2);
         plan->weight_t = take(plan->planes * piece * k * 2);
         plan->d = take(plan->planes * n * piece * 2);
         plan->d_t = take(plan->planes * n * piece * 2);
-        // one array of sums, or several where splits * tiles stays within the compute units
-        const int64_t one = n * up(max_hidden, 4), split = (int64_t)compute_units * kTile * kTile;
+        // one array of sums, or several where splits * tiles stays within twice the compute units
+        const int64_t one = n * up(max_hidden, 4), split = 2 * (int64_t)compute_units * kTile * kTile;
         plan->sums = take((one > split ? one : split) * 4);
     }
     plan->scratch_bytes = at;
@@ -575,12 +681,13 @@ hipError_t head_prepare()
     return e;
 }
 
-hipError_t head_loss_launch(const HeadPlan &plan, int dtype, const deft_head_loss_t &a, void *scratch, int, hipStream_t st)
+hipError_t head_loss_launch(const HeadPlan &plan, int dtype, const deft_head_loss_t &a, void *scratch, int compute_units,
+                            hipStream_t st)
 {
     const Scratch s(plan, scratch);
-    if (dtype == DEFT_F32) return Head<float, bf16, 3>::loss(plan, a, s, st);
-    if (dtype == DEFT_F16) return Head<f16, f16, 1>::loss(plan, a, s, st);
-    return Head<bf16, bf16, 1>::loss(plan, a, s, st);
+    if (dtype == DEFT_F32) return Head<float, bf16, 3>::loss(plan, a, s, compute_units, st);
+    if (dtype == DEFT_F16) return Head<f16, f16, 1>::loss(plan, a, s, compute_units, st);
+    return Head<bf16, bf16, 1>::loss(plan, a, s, compute_units, st);
 }
 
 hipError_t head_grad_launch(const HeadPlan &plan, int dtype, const deft_head_grad_t &a, void *scratch, int compute_units,

@@ -7,8 +7,8 @@ elements of a row apart) are refused with ValueError; nothing is copied or conve
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
+import functools
 from typing import Iterable, Optional, Sequence
 
 import torch
@@ -87,6 +87,21 @@ def load_library() -> ctypes.CDLL:
     return lib
 
 
+def _on_stream(method):
+    """Adds the `stream` argument: what the call allocates belongs to that stream, and its tensors are recorded there."""
+    @functools.wraps(method)
+    def call(self, *args, stream: Optional[torch.cuda.Stream] = None, **kwargs):
+        if stream is None:
+            return method(self, *args, **kwargs)
+        with torch.cuda.stream(stream):
+            out = method(self, *args, **kwargs)
+        for t in (*args, *kwargs.values()):
+            if isinstance(t, torch.Tensor):
+                t.record_stream(stream)
+        return out
+    return call
+
+
 class DeftEnds:
     """Owner of one deft_ends_t handle.
 
@@ -107,8 +122,7 @@ class DeftEnds:
             if name not in OPERATORS:
                 raise ValueError(f"operators are {list(OPERATORS)}: got {name!r}")
             mask |= OPERATORS[name]
-        self.dtype, self.device = dtype, torch.device("cuda", device)
-        self._bytes = torch.empty(0, dtype=dtype).element_size()
+        self.dtype, self.device, self._index = dtype, torch.device("cuda", device), device
         cfg = deft_ends_config_t(device, DTYPES[dtype], mask, max_rows, max_vocab, max_hidden, max_top_k)
         rc = self._lib.deft_ends_create(ctypes.byref(cfg), ctypes.byref(self._h))
         if rc != DEFT_OK:
@@ -135,59 +149,58 @@ class DeftEnds:
 
     # ---- the operators ----------------------------------------------------------------------
 
+    @_on_stream
     def embed(self, tokens: torch.Tensor, table: torch.Tensor, scale: float = 1.0, out: Optional[torch.Tensor] = None,
-              status: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+              status: Optional[torch.Tensor] = None) -> torch.Tensor:
         """out[n] = scale * table[tokens[n]]."""
         vocab, hidden = self._rows("table", table, None, None)
         n = self._words("tokens", tokens, torch.int32, (None,))[0]
-        with self._on(stream, tokens, table, out, status) as st:
-            if out is None:
-                out = torch.empty((n, hidden), dtype=self.dtype, device=self.device)
-            self._rows("out", out, n, hidden)
-            if status is not None:
-                self._words("status", status, torch.int32, (n,))
-            self._call("deft_embed", ctypes.byref(deft_embed_t(
-                n, vocab, hidden, scale, _p(tokens), _p(table), _ld(table), _p(out), _ld(out), _p(status), st)))
+        if out is None:
+            out = torch.empty((n, hidden), dtype=self.dtype, device=self.device)
+        self._rows("out", out, n, hidden)
+        if status is not None:
+            self._words("status", status, torch.int32, (n,))
+        self._call("deft_embed", ctypes.byref(deft_embed_t(
+            n, vocab, hidden, scale, _p(tokens), _p(table), _ld(table), _p(out), _ld(out), _p(status), self._stream())))
         return out
 
+    @_on_stream
     def embed_grad(self, tokens: torch.Tensor, grad_out: torch.Tensor, vocab: Optional[int] = None, scale: float = 1.0,
-                   grad_table: Optional[torch.Tensor] = None, accumulate: bool = False,
-                   stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+                   grad_table: Optional[torch.Tensor] = None, accumulate: bool = False) -> torch.Tensor:
         """grad_table[v] (+)= scale * the sum of grad_out over the rows whose token is v.  Either
         `grad_table` or `vocab` says how many rows the table has."""
         n = self._words("tokens", tokens, torch.int32, (None,))[0]
         _, hidden = self._rows("grad_out", grad_out, n, None)
         if grad_table is None and (vocab is None or accumulate):
             raise ValueError("embed_grad needs grad_table, or vocab and nothing to add to")
-        with self._on(stream, tokens, grad_out, grad_table) as st:
-            if grad_table is None:
-                grad_table = torch.empty((vocab, hidden), dtype=self.dtype, device=self.device)
-            vocab, _ = self._rows("grad_table", grad_table, vocab, hidden)
-            self._call("deft_embed_grad", ctypes.byref(deft_embed_grad_t(
-                n, vocab, hidden, scale, int(accumulate), _p(tokens), _p(grad_out), _ld(grad_out), _p(grad_table),
-                _ld(grad_table), st)))
+        if grad_table is None:
+            grad_table = torch.empty((vocab, hidden), dtype=self.dtype, device=self.device)
+        vocab, _ = self._rows("grad_table", grad_table, vocab, hidden)
+        self._call("deft_embed_grad", ctypes.byref(deft_embed_grad_t(
+            n, vocab, hidden, scale, int(accumulate), _p(tokens), _p(grad_out), _ld(grad_out), _p(grad_table),
+            _ld(grad_table), self._stream())))
         return grad_table
 
+    @_on_stream
     def head_loss(self, hidden: torch.Tensor, weight: torch.Tensor, labels: torch.Tensor, logit_scale: float = 1.0,
-                  status: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+                  status: Optional[torch.Tensor] = None):
         """(loss, lse) of every position, float32."""
         n, width = self._rows("hidden", hidden, None, None)
         vocab, _ = self._rows("weight", weight, None, width)
         self._words("labels", labels, torch.int32, (n,))
-        with self._on(stream, hidden, weight, labels, status) as st:
-            both = torch.empty((2, n), dtype=torch.float32, device=self.device)
-            if status is not None:
-                self._words("status", status, torch.int32, (n,))
-            self._call("deft_head_loss", ctypes.byref(deft_head_loss_t(
-                n, vocab, width, logit_scale, _p(hidden), _ld(hidden), _p(weight), _ld(weight), _p(labels), _p(both[0]),
-                _p(both[1]), _p(status), st)))
+        both = torch.empty((2, n), dtype=torch.float32, device=self.device)
+        if status is not None:
+            self._words("status", status, torch.int32, (n,))
+        self._call("deft_head_loss", ctypes.byref(deft_head_loss_t(
+            n, vocab, width, logit_scale, _p(hidden), _ld(hidden), _p(weight), _ld(weight), _p(labels), _p(both[0]),
+            _p(both[1]), _p(status), self._stream())))
         return both[0], both[1]
 
+    @_on_stream
     def head_grad(self, hidden: torch.Tensor, weight: torch.Tensor, labels: torch.Tensor, lse: torch.Tensor,
                   row_grad: torch.Tensor, logit_scale: float = 1.0, grad_hidden: Optional[torch.Tensor] = None,
                   grad_weight: Optional[torch.Tensor] = None, accumulate: bool = False, need_hidden: bool = True,
-                  need_weight: bool = True, piece_events: Optional[Sequence[torch.cuda.Event]] = None,
-                  stream: Optional[torch.cuda.Stream] = None):
+                  need_weight: bool = True, piece_events: Optional[Sequence[torch.cuda.Event]] = None):
         """(grad_hidden, grad_weight) of sum(row_grad * loss); accumulate adds into grad_weight.  Event i of
         piece_events is recorded once the rows of grad_weight below (i + 1) * info().vocab_piece are final."""
         n, width = self._rows("hidden", hidden, None, None)
@@ -197,56 +210,55 @@ class DeftEnds:
         self._words("row_grad", row_grad, torch.float32, (n,))
         if accumulate and (grad_weight is None or not need_weight):
             raise ValueError("accumulate needs grad_weight")
-        with self._on(stream, hidden, weight, labels, lse, row_grad, grad_hidden, grad_weight) as st:
-            if need_hidden and grad_hidden is None:
-                grad_hidden = torch.empty((n, width), dtype=self.dtype, device=self.device)
-            if need_weight and grad_weight is None:
-                grad_weight = torch.empty((vocab, width), dtype=self.dtype, device=self.device)
-            grad_hidden, grad_weight = grad_hidden if need_hidden else None, grad_weight if need_weight else None
-            if need_hidden:
-                self._rows("grad_hidden", grad_hidden, n, width)
-            if need_weight:
-                self._rows("grad_weight", grad_weight, vocab, width)
-            events = None
-            if piece_events:
-                on = torch.cuda.ExternalStream(st.value or 0, device=self.device)
-                for e in piece_events:   # (torch makes an event when it is first recorded)
-                    e.record(on)
-                events = (_vp * len(piece_events))(*[e.cuda_event for e in piece_events])
-            self._call("deft_head_grad", ctypes.byref(deft_head_grad_t(
-                n, vocab, width, logit_scale, int(accumulate), len(piece_events or ()), _p(hidden), _ld(hidden),
-                _p(weight), _ld(weight), _p(labels), _p(lse), _p(row_grad), _p(grad_hidden), _ld(grad_hidden),
-                _p(grad_weight), _ld(grad_weight), ctypes.cast(events, _vp) if events else None, st)))
+        if need_hidden and grad_hidden is None:
+            grad_hidden = torch.empty((n, width), dtype=self.dtype, device=self.device)
+        if need_weight and grad_weight is None:
+            grad_weight = torch.empty((vocab, width), dtype=self.dtype, device=self.device)
+        grad_hidden, grad_weight = grad_hidden if need_hidden else None, grad_weight if need_weight else None
+        if need_hidden:
+            self._rows("grad_hidden", grad_hidden, n, width)
+        if need_weight:
+            self._rows("grad_weight", grad_weight, vocab, width)
+        events = None
+        if piece_events:
+            on = torch.cuda.current_stream(self.device)
+            for e in piece_events:   # (torch makes an event when it is first recorded)
+                e.record(on)
+            events = (_vp * len(piece_events))(*[e.cuda_event for e in piece_events])
+        self._call("deft_head_grad", ctypes.byref(deft_head_grad_t(
+            n, vocab, width, logit_scale, int(accumulate), len(piece_events or ()), _p(hidden), _ld(hidden),
+            _p(weight), _ld(weight), _p(labels), _p(lse), _p(row_grad), _p(grad_hidden), _ld(grad_hidden),
+            _p(grad_weight), _ld(grad_weight), ctypes.cast(events, _vp) if events else None, self._stream())))
         return grad_hidden, grad_weight
 
+    @_on_stream
     def distill(self, logits: torch.Tensor, teacher_index: torch.Tensor, teacher_logit: torch.Tensor,
-                temperature: float = 1.0, status: Optional[torch.Tensor] = None,
-                stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+                temperature: float = 1.0, status: Optional[torch.Tensor] = None) -> torch.Tensor:
         """loss of every row, float32."""
-        return self._distill(logits, teacher_index, teacher_logit, None, temperature, None, status, stream)[0]
+        return self._distill(logits, teacher_index, teacher_logit, None, temperature, None, status)[0]
 
+    @_on_stream
     def distill_grad(self, logits: torch.Tensor, teacher_index: torch.Tensor, teacher_logit: torch.Tensor,
                      row_grad: torch.Tensor, temperature: float = 1.0, grad_logits: Optional[torch.Tensor] = None,
-                     status: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+                     status: Optional[torch.Tensor] = None):
         """(loss, grad_logits) in one pass over the logits; grad_logits may be the logits themselves."""
         self._words("row_grad", row_grad, torch.float32, (logits.shape[0],))
-        return self._distill(logits, teacher_index, teacher_logit, row_grad, temperature, grad_logits, status, stream)
+        return self._distill(logits, teacher_index, teacher_logit, row_grad, temperature, grad_logits, status)
 
-    def _distill(self, logits, teacher_index, teacher_logit, row_grad, temperature, grad_logits, status, stream):
+    def _distill(self, logits, teacher_index, teacher_logit, row_grad, temperature, grad_logits, status):
         n, vocab = self._rows("logits", logits, None, None)
         top_k = self._words("teacher_index", teacher_index, torch.int32, (n, None))[1]
         self._words("teacher_logit", teacher_logit, torch.float32, (n, top_k))
-        with self._on(stream, logits, teacher_index, teacher_logit, row_grad, grad_logits, status) as st:
-            loss = torch.empty(n, dtype=torch.float32, device=self.device)
-            if row_grad is not None:
-                if grad_logits is None:
-                    grad_logits = torch.empty((n, vocab), dtype=self.dtype, device=self.device)
-                self._rows("grad_logits", grad_logits, n, vocab)
-            if status is not None:
-                self._words("status", status, torch.int32, (n,))
-            self._call("deft_distill", ctypes.byref(deft_distill_t(
-                n, vocab, top_k, temperature, _p(logits), _ld(logits), _p(teacher_index), _p(teacher_logit),
-                _p(row_grad), _p(loss), _p(grad_logits), _ld(grad_logits), _p(status), st)))
+        loss = torch.empty(n, dtype=torch.float32, device=self.device)
+        if row_grad is not None:
+            if grad_logits is None:
+                grad_logits = torch.empty((n, vocab), dtype=self.dtype, device=self.device)
+            self._rows("grad_logits", grad_logits, n, vocab)
+        if status is not None:
+            self._words("status", status, torch.int32, (n,))
+        self._call("deft_distill", ctypes.byref(deft_distill_t(
+            n, vocab, top_k, temperature, _p(logits), _ld(logits), _p(teacher_index), _p(teacher_logit),
+            _p(row_grad), _p(loss), _p(grad_logits), _ld(grad_logits), _p(status), self._stream())))
         return loss, grad_logits
 
     # ---- marshalling ------------------------------------------------------------------------
@@ -260,36 +272,29 @@ class DeftEnds:
 
     def _rows(self, name, t, rows, width):
         """Checks a matrix of the handle's type whose rows lie apart as they like; gives its shape."""
-        if not isinstance(t, torch.Tensor) or t.dim() != 2 or t.dtype != self.dtype or t.device != self.device:
+        if not isinstance(t, torch.Tensor) or t.dim() != 2 or t.dtype != self.dtype or t.get_device() != self._index:
             raise ValueError(f"{name}: a matrix of {self.dtype} on {self.device} is wanted")
-        if (rows is not None and t.shape[0] != rows) or (width is not None and t.shape[1] != width):
-            raise ValueError(f"{name}: shape {tuple(t.shape)} does not fit ({rows}, {width})")
-        if (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+        n, w = t.shape
+        if (rows is not None and n != rows) or (width is not None and w != width):
+            raise ValueError(f"{name}: shape {(n, w)} does not fit {(rows, width)}")
+        if not t.is_contiguous() and ((w > 1 and t.stride(1) != 1) or (n > 1 and t.stride(0) < w)):
             raise ValueError(f"{name}: a row's elements have to be next to each other, rows apart")
-        return t.shape
+        return n, w
 
     def _words(self, name, t, dtype, shape):
-        if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != self.device or not t.is_contiguous():
+        if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.get_device() != self._index or not t.is_contiguous():
             raise ValueError(f"{name}: a contiguous tensor of {dtype} on {self.device} is wanted")
-        if t.dim() != len(shape) or any(s is not None and s != g for s, g in zip(shape, t.shape)):
-            raise ValueError(f"{name}: shape {tuple(t.shape)} does not fit {shape}")
-        return t.shape
+        got = t.shape
+        if len(got) != len(shape) or any(s is not None and s != g for s, g in zip(shape, got)):
+            raise ValueError(f"{name}: shape {tuple(got)} does not fit {shape}")
+        return got
 
-    @contextlib.contextmanager
-    def _on(self, stream, *tensors):
-        current = torch.cuda.current_stream(self.device)
-        if stream is None or stream == current:
-            yield _vp(current.cuda_stream)
-            return
-        with torch.cuda.stream(stream):   # what is allocated in here belongs to that stream
-            yield _vp(stream.cuda_stream)
-        for t in tensors:
-            if t is not None:
-                t.record_stream(stream)
+    def _stream(self) -> int:
+        return torch._C._cuda_getCurrentRawStream(self._index)
 
 
 def _p(t):
-    return None if t is None else _vp(t.data_ptr())
+    return None if t is None else t.data_ptr()
 
 
 def _ld(t):
