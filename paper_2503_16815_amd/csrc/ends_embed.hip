@@ -53,14 +53,23 @@ __global__ void __launch_bounds__(256) embed_kernel(deft_embed_t e)
     if (lane == 0 && e.status) e.status[row] = in || token == -1 ? DEFT_OK : DEFT_ERR_INVALID_ARG;
     T *out = static_cast<T *>(e.out) + (int64_t)row * e.out_stride;
     const T *from = static_cast<const T *>(e.table) + (int64_t)(in ? token : 0) * e.table_stride;
-    for (int at = lane * n; at < e.hidden; at += kWave * n) {
-        float x[n] = {};
-        if (in) {
-            const typename Vec<T>::type v = load_part<T>(from, at, e.hidden);
+    constexpr int kAhead = 4;   // vectors of a lane that are on their way together
+    for (int first = lane * n; first < e.hidden; first += kWave * n * kAhead) {
+        typename Vec<T>::type v[kAhead];
 #pragma unroll
-            for (int i = 0; i < n; ++i) x[i] = e.scale * (float)v[i];
+        for (int j = 0; j < kAhead; ++j) {
+            const int at = first + j * kWave * n;
+            v[j] = typename Vec<T>::type{};
+            if (in && at < e.hidden) v[j] = load_part<T>(from, at, e.hidden);
         }
-        store_part<T>(out, at, e.hidden, x);
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            const int at = first + j * kWave * n;
+            float x[n];
+#pragma unroll
+            for (int i = 0; i < n; ++i) x[i] = in ? e.scale * (float)v[j][i] : 0.0f;
+            if (at < e.hidden) store_part<T>(out, at, e.hidden, x);
+        }
     }
 }
 
@@ -171,133 +180,114 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(SortArgs a)
     }
 }
 
-// ---- up to 16384 rows: sorted by one workgroup -----------------------------------------------
+// ---- up to 16384 rows: two launches ---------------------------------------------------------
 
-// A token number and its row fit one word (18 and 14 bits), sixteen words a lane.  Everything happens in
-// registers and LDS in one launch, which has the other compute units to itself: they clear the rows of the
-// table that no token points to.  (Measured on 16384 tokens of a vocabulary of 50257: the six launches of the
-// sort in memory 50 us and the clearing 21 us before it.)
-constexpr int kSmallThreads = 1024, kSmallWaves = 16, kSmallItems = 16, kSmall = kSmallThreads * kSmallItems;
-constexpr int kRowBits = 14, kSmallVocab = 1 << (32 - kRowBits);
+// A token number and its row fit one word (18 and 14 bits); no two words are the same, so any sort of them is the stable
+// one.  The first launch sorts lists of 1024 words, a workgroup each.  The second finds each word's place: its
+// place in its own list plus, by bisection, the words of every other list below it.  The other workgroups of
+// both launches clear half of the table each; the rows that have tokens are written again by the sums, which costs
+// less than finding out which these are.  (Measured on 16384 tokens of a vocabulary of 50257: radix sort in memory,
+// six launches, 50 us; radix sort by one workgroup in registers and LDS 32 us, bound by the instructions of a
+// single compute unit; this 18 us.)
+constexpr int kListBits = 10, kList = 1 << kListBits, kSmallThreads = 1024, kSmallWaves = kSmallThreads / kWave;
+constexpr int kRowBits = 14, kSmall = 1 << kRowBits, kSmallVocab = 1 << (32 - kRowBits);
+constexpr int kRanked = 256, kShare = kSmallThreads / kRanked;   // words that a workgroup places, lanes to a word
 
 struct SmallArgs {
-    int n, vocab, hidden, digit_bits, passes;
+    int n, vocab, hidden, lists;
+    int workers;               // workgroups that sort; the others clear
+    int clear_from, clear_to;  // rows of the table
     const int32_t *tokens;
+    unsigned *words;
     int32_t *keys, *rows;
     void *table;
     int64_t stride;
 };
 
-// What lanes of a wavefront wrote to LDS before is what they read behind it (its accesses are in order).
-__device__ __forceinline__ void in_wave()
+// this workgroup's share of the rows
+template <typename T>
+__device__ __forceinline__ void clear_rows(const SmallArgs &a)
 {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
+    const int share = blockIdx.x - a.workers, shares = gridDim.x - a.workers, rows = a.clear_to - a.clear_from;
+    const int from = a.clear_from + (int)((int64_t)rows * share / shares);
+    const int to = a.clear_from + (int)((int64_t)rows * (share + 1) / shares);
+    constexpr int n = Vec<T>::n;
+    const float zero[n] = {};
+    for (int row = from + (int)(threadIdx.x >> 6); row < to; row += kSmallWaves) {
+        T *to_row = static_cast<T *>(a.table) + (int64_t)row * a.stride;
+        for (int at = (threadIdx.x & 63) * n; at < a.hidden; at += kWave * n) store_part<T>(to_row, at, a.hidden, zero);
+    }
 }
 
-__device__ __forceinline__ void sort_small(const SmallArgs &a, unsigned *words, int (*count)[kDigits], int *wave_total)
+__device__ __forceinline__ void write_place(const SmallArgs &a, int at, unsigned word)
 {
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int rounds = (a.n + kSmallThreads - 1) / kSmallThreads, first = wave * rounds * kWave + lane;
-    unsigned item[kSmallItems];
-    int rank[kSmallItems];
-#pragma unroll
-    for (int r = 0; r < kSmallItems; ++r) {
-        const int i = first + r * kWave;
-        if (r < rounds && i < a.n) {
-            const int t = a.tokens[i];
-            item[r] = (unsigned)(t >= 0 && t < a.vocab ? t : a.vocab) << kRowBits | (unsigned)i;
-        }
-    }
-    for (int pass = 0; pass < a.passes; ++pass) {
-        const int shift = kRowBits + pass * a.digit_bits, digits = 1 << a.digit_bits;
-        for (int d = lane; d < digits; d += kWave) count[wave][d] = 0;
-        in_wave();
-#pragma unroll
-        for (int r = 0; r < kSmallItems; ++r) {
-            if (r < rounds) {
-                const bool valid = first + r * kWave < a.n;
-                const int digit = (item[r] >> shift) & (digits - 1);
-                const uint64_t same = same_digit(digit, valid);
-                const int before = __popcll(same & ((1ull << lane) - 1));
-                const int base = valid ? count[wave][digit] : 0;
-                in_wave();   // every lane has read what the first of each digit now writes
-                rank[r] = base + before;
-                if (valid && before == 0) count[wave][digit] = base + __popcll(same);
-                in_wave();
-            }
-        }
-        __syncthreads();
-        // counts become the places of each wavefront's first item of a digit
-        int own = 0, x = 0;
-        if (tid < digits)
-            for (int w = 0; w < kSmallWaves; ++w) own += count[w][tid];
-        x = own;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int y = __shfl_up(x, d);
-            if (lane >= d) x += y;
-        }
-        if (lane == 63) wave_total[wave] = x;
-        __syncthreads();
-        if (tid < digits) {
-            int at = x - own;
-            for (int w = 0; w < wave; ++w) at += wave_total[w];
-            for (int w = 0; w < kSmallWaves; ++w) {
-                const int c = count[w][tid];
-                count[w][tid] = at;
-                at += c;
-            }
-        }
-        __syncthreads();
-#pragma unroll
-        for (int r = 0; r < kSmallItems; ++r)
-            if (r < rounds && first + r * kWave < a.n) words[count[wave][(item[r] >> shift) & (digits - 1)] + rank[r]] = item[r];
-        __syncthreads();
-        if (pass + 1 < a.passes) {
-#pragma unroll
-            for (int r = 0; r < kSmallItems; ++r)
-                if (r < rounds && first + r * kWave < a.n) item[r] = words[first + r * kWave];
-        }
-    }
-    for (int i = tid; i < a.n; i += kSmallThreads) {
-        a.keys[i] = (int32_t)(words[i] >> kRowBits);
-        a.rows[i] = (int32_t)(words[i] & ((1u << kRowBits) - 1));
-    }
+    a.keys[at] = (int32_t)(word >> kRowBits);
+    a.rows[at] = (int32_t)(word & (kSmall - 1));
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kSmallThreads) sort_small_kernel(SmallArgs a)
+__global__ void __launch_bounds__(kSmallThreads) sort_lists_kernel(SmallArgs a)
 {
-    __shared__ unsigned words[kSmall];
-    __shared__ int count[kSmallWaves][kDigits];
-    __shared__ int wave_total[kSmallWaves];
-    if (blockIdx.x == 0) {
-        sort_small(a, words, count, wave_total);
+    __shared__ unsigned other[kList];
+    if ((int)blockIdx.x >= a.workers) {
+        clear_rows<T>(a);
         return;
     }
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int share = blockIdx.x - 1, shares = gridDim.x - 1;
-    const int from = (int)((int64_t)a.vocab * share / shares), to = (int)((int64_t)a.vocab * (share + 1) / shares);
-    for (int i = tid; i < (to - from + 31) / 32; i += kSmallThreads) words[i] = 0;   // (fewer rows than kSmall bits)
-    __syncthreads();
-    for (int i = tid; i < a.n; i += kSmallThreads) {
+    const int tid = threadIdx.x, i = blockIdx.x * kList + tid;
+    unsigned word = ~0u;   // beyond the list: after all others
+    if (i < a.n) {
         const int t = a.tokens[i];
-        if (t >= from && t < to) atomicOr(&words[(t - from) >> 5], 1u << ((t - from) & 31));
+        word = (unsigned)(t >= 0 && t < a.vocab ? t : a.vocab) << kRowBits | (unsigned)i;   // tokens that add nothing come last
     }
+    for (int size = 2; size <= kList; size <<= 1)          // bitonic: runs of `size` become sorted
+        for (int d = size >> 1; d > 0; d >>= 1) {
+            unsigned with;
+            if (d >= kWave) {
+                __syncthreads();
+                other[tid] = word;
+                __syncthreads();
+                with = other[tid ^ d];
+            } else {
+                with = __shfl_xor(word, d);
+            }
+            const bool up = (tid & size) == 0, first = (tid & d) == 0;
+            word = up == first ? min(word, with) : max(word, with);
+        }
+    if (i >= a.n) return;                                  // (as many words as tokens come before the fill)
+    if (a.lists == 1) write_place(a, i, word);
+    else a.words[i] = word;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kSmallThreads) place_words_kernel(SmallArgs a)
+{
+    __shared__ unsigned words[kSmall];
+    if ((int)blockIdx.x >= a.workers) {
+        clear_rows<T>(a);
+        return;
+    }
+    const int tid = threadIdx.x;
+    for (int i = tid; i < a.lists * kList; i += kSmallThreads) words[i] = i < a.n ? a.words[i] : ~0u;
     __syncthreads();
-    constexpr int n = Vec<T>::n;
-    const float zero[n] = {};
-    for (int row = from + wave; row < to; row += kSmallWaves) {
-        if (words[(row - from) >> 5] >> ((row - from) & 31) & 1) continue;
-        T *to_row = static_cast<T *>(a.table) + (int64_t)row * a.stride;
-        for (int at = lane * n; at < a.hidden; at += kWave * n) store_part<T>(to_row, at, a.hidden, zero);
+    const int i = blockIdx.x * kRanked + tid / kShare, own = i >> kListBits;
+    const unsigned word = i < a.n ? words[i] : 0;
+    int below = 0;
+    for (int list = tid % kShare; list < a.lists; list += kShare) {
+        const unsigned *w = words + list * kList;
+        int at = 0;
+#pragma unroll
+        for (int d = kList / 2; d > 0; d >>= 1) at += w[at + d - 1] < word ? d : 0;
+        at += w[at] < word ? 1 : 0;
+        below += list == own ? i & (kList - 1) : at;
     }
+    below += __shfl_xor(below, 1);
+    below += __shfl_xor(below, 2);
+    if (i < a.n && tid % kShare == 0) write_place(a, below, word);
 }
 
 // ---- sums over the sorted rows --------------------------------------------------------------
 
-constexpr int kBatch = 8, kJoin = 8;
+constexpr int kBatch = 8, kJoin = 16;
 
 struct SumArgs {
     int n, vocab, hidden, accumulate, chunk, chunks;
@@ -494,15 +484,26 @@ hipError_t grad_launch(const EmbedPlan &plan, const deft_embed_grad_t &e, char *
         s.n = e.n_rows;
         s.vocab = e.vocab;
         s.hidden = e.hidden;
-        s.passes = (bits + 7) / 8;
-        s.digit_bits = (bits + s.passes - 1) / s.passes;
+        s.lists = (e.n_rows + kList - 1) / kList;
         s.tokens = e.tokens;
+        s.words = reinterpret_cast<unsigned *>(scratch + l.keys_b);
         s.keys = keys[0];
         s.rows = rows[0];
         s.table = table;
         s.stride = e.grad_table_stride;
-        const int shares = e.accumulate ? 0 : e.vocab < compute_units - 1 ? e.vocab : compute_units - 1;
-        sort_small_kernel<T><<<1 + shares, kSmallThreads, 0, st>>>(s);
+        const auto clearers = [&](int rows_to_clear, int workers) {
+            const int most = 2 * compute_units > workers ? 2 * compute_units - workers : 1;
+            return e.accumulate ? 0 : rows_to_clear < most ? rows_to_clear : most;
+        };
+        s.workers = s.lists;
+        s.clear_to = s.lists == 1 ? e.vocab : e.vocab / 2;
+        sort_lists_kernel<T><<<s.workers + clearers(s.clear_to, s.workers), kSmallThreads, 0, st>>>(s);
+        if (s.lists > 1) {
+            s.workers = (e.n_rows + kRanked - 1) / kRanked;
+            s.clear_from = s.clear_to;
+            s.clear_to = e.vocab;
+            place_words_kernel<T><<<s.workers + clearers(s.clear_to - s.clear_from, s.workers), kSmallThreads, 0, st>>>(s);
+        }
     } else {
         if (!e.accumulate) {
             const int blocks = (e.vocab + 3) / 4;
@@ -549,7 +550,11 @@ hipError_t grad_launch(const EmbedPlan &plan, const deft_embed_grad_t &e, char *
     const int per_block = 256 / a.lanes;
     const dim3 grid((a.chunks + per_block - 1) / per_block, (parts + a.lanes - 1) / a.lanes);
     embed_sum_kernel<T><<<grid, 256, 0, st>>>(a);
-    if (a.chunks > 1) embed_join_kernel<T><<<grid, 256, 0, st>>>(a);
+    if (a.chunks > 1) {   // a long run's sums are spread over several compute units by their columns
+        a.lanes = a.lanes < 32 ? a.lanes : 32;
+        const int joined = 256 / a.lanes;
+        embed_join_kernel<T><<<dim3((a.chunks + joined - 1) / joined, (parts + a.lanes - 1) / a.lanes), 256, 0, st>>>(a);
+    }
     return hipGetLastError();
 }
 
