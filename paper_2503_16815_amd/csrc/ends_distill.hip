@@ -164,8 +164,31 @@ __device__ __forceinline__ SoftSum wave_join2(SoftSum s, int from)
     return s;
 }
 
-// Each lane holds NV vectors of the row, kRowThreads vectors apart, and one of its last `vocab % n` elements; the
-// k-th lane the teacher's k-th entry.  Logits are scaled by log2(e) / T as they are used.
+// 16 bytes of logits as floats
+__device__ __forceinline__ void widen(i32x4 v, float (&x)[4], float)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = __int_as_float(v[i]);
+}
+__device__ __forceinline__ void widen(i32x4 v, float (&x)[8], bf16)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __int_as_float(v[i] << 16);
+        x[2 * i + 1] = __int_as_float(v[i] & (int)0xffff0000);
+    }
+}
+__device__ __forceinline__ void widen(i32x4 v, float (&x)[8], f16)
+{
+    typedef f16 f16x8 __attribute__((ext_vector_type(8)));
+    const f16x8 h = __builtin_bit_cast(f16x8, v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = (float)h[i];
+}
+
+// Each lane holds NV vectors of the row, kRowThreads vectors apart, from the row's first 16-byte boundary on (a wave's
+// vectors that straddle such boundaries cost a tenth of the time), and one of the elements before and behind them;
+// the k-th lane the teacher's k-th entry.  Logits are scaled by log2(e) / T as they are used.
 template <typename T, int kRowThreads, int NV, bool GRAD>
 __global__ void __launch_bounds__(kRowThreads, 4) distill_row_kernel(deft_distill_t a)
 {
@@ -180,16 +203,25 @@ __global__ void __launch_bounds__(kRowThreads, 4) distill_row_kernel(deft_distil
     __shared__ float same_prob[kRowThreads];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const float c = kLog2e / a.temperature;
-    const int whole = a.vocab / n * n, rest = a.vocab - whole;
     const T *const logits = static_cast<const T *>(a.logits);
     for (int i = tid; i < kMarkBits / 32; i += kRowThreads) mark[i] = 0;
     if (tid < 2) twice[tid] = 0;
 
-    V x[NV];
+    // where a row's vectors begin, how many elements they have, and this lane's single element (or -1)
+    const auto before = [&](int64_t row) {
+        const int at = (int)((uintptr_t)(logits + row * a.logits_stride) & 15);
+        return min(at ? (16 - at) / (int)sizeof(T) : 0, a.vocab);
+    };
+    const auto inside = [&](int head) { return (a.vocab - head) / n * n; };
+    const auto single = [&](int head, int whole) {
+        const int at = tid < head ? tid : tid + whole;
+        return at < a.vocab && tid < 2 * n ? at : -1;
+    };
+    i32x4 x[NV];
     T last = (T)0.0f;
-    const auto load = [&](int64_t row, int j) {
+    const auto load = [&](int64_t row, int head, int whole, int j) {
         const int at = (j * kRowThreads + tid) * n;
-        if (at < whole) x[j] = *reinterpret_cast<const V *>(logits + row * a.logits_stride + at);
+        if (at < whole) x[j] = __builtin_bit_cast(i32x4, *reinterpret_cast<const V *>(logits + row * a.logits_stride + head + at));
     };
     const auto entry = [&](int64_t row, int &index, float &u) {
         index = -1;
@@ -203,15 +235,17 @@ __global__ void __launch_bounds__(kRowThreads, 4) distill_row_kernel(deft_distil
     float u, next_u;
     entry(blockIdx.x, index, u);
     bool kept = __syncthreads_or(index != -1);
+    int head = before(blockIdx.x), whole = inside(head);
     if (kept) {
 #pragma unroll
-        for (int j = 0; j < NV; ++j) load(blockIdx.x, j);
-        if (tid < rest) last = logits[(int64_t)blockIdx.x * a.logits_stride + whole + tid];
+        for (int j = 0; j < NV; ++j) load(blockIdx.x, head, whole, j);
+        if (single(head, whole) >= 0) last = logits[(int64_t)blockIdx.x * a.logits_stride + single(head, whole)];
     }
 
     int odd = 0;
     for (int64_t row = blockIdx.x; row < a.n_rows; row += gridDim.x, odd ^= 1) {
         const int64_t next = row + gridDim.x;
+        const int at_last = single(head, whole);
         const bool in = index >= 0 && index < a.vocab;
         float z_at = 0.0f;   // the logit at this lane's entry
         if (in) z_at = (float)logits[row * a.logits_stride + index] * c;
@@ -223,23 +257,30 @@ __global__ void __launch_bounds__(kRowThreads, 4) distill_row_kernel(deft_distil
         SoftSum s = {-INFINITY, 0.0f}, t = {in ? u * c : -INFINITY, 0.0f};
         if (kept) {
             // -3e38 in the place of -infinity: exp2(-infinity - that) is 0, and a NaN stays one
-            float top = tid < rest ? (float)last * c : -3.0e38f;
-            top = fmaxf(top, -3.0e38f);
+            float top = at_last >= 0 ? (float)last : -3.0e38f;
 #pragma unroll
-            for (int j = 0; j < NV; ++j)
+            for (int j = 0; j < NV; ++j) {
                 if ((j * kRowThreads + tid) * n < whole) {
+                    float w[n];
+                    widen(x[j], w, T());
 #pragma unroll
-                    for (int i = 0; i < n; ++i) top = fmaxf(top, (float)x[j][i] * c);
+                    for (int i = 0; i < n; i += 2) top = fmaxf(top, fmaxf(w[i], w[i + 1]));
                 }
-            s.top = top;
-            if (tid < rest) s.sum = exp2_of(__builtin_fmaf((float)last, c, -top));
+                asm volatile("" : "+v"(x[j]));   // (widened again for the sum: kept as floats the row would not fit)
+            }
+            top = fmaxf(top * c, -3.0e38f);
+            float sum[2] = {at_last >= 0 ? exp2_of(__builtin_fmaf((float)last, c, -top)) : 0.0f, 0.0f};
 #pragma unroll
-            for (int j = 0; j < NV; ++j)
+            for (int j = 0; j < NV; ++j) {
                 if ((j * kRowThreads + tid) * n < whole) {
+                    float w[n];
+                    widen(x[j], w, T());
 #pragma unroll
-                    for (int i = 0; i < n; ++i) s.sum += exp2_of(__builtin_fmaf((float)x[j][i], c, -top));
+                    for (int i = 0; i < n; ++i) sum[i & 1] += exp2_of(__builtin_fmaf(w[i], c, -top));
                 }
-            s = wave_join2(s, 32);
+                asm volatile("" : "+v"(x[j]));
+            }
+            s = wave_join2(SoftSum{top, sum[0] + sum[1]}, 32);
             if (in) t.sum = t.top == -INFINITY ? 0.0f : exp2_of(t.top - t.top);   // (1, or the NaN that the entry is)
             t = wave_join2(t, 32);
         }
@@ -280,20 +321,23 @@ __global__ void __launch_bounds__(kRowThreads, 4) distill_row_kernel(deft_distil
         if (tid == 0) twice[odd ^ 1] = 0;
 
         T *grad = GRAD ? static_cast<T *>(a.grad_logits) + row * a.grad_stride : nullptr;
-        if (GRAD && tid < rest) grad[whole + tid] = ok ? (T)(g * exp2_of(__builtin_fmaf((float)last, c, -lse))) : (T)0.0f;
-        if (next_kept && tid < rest) last = logits[next * a.logits_stride + whole + tid];
+        if (GRAD && at_last >= 0) grad[at_last] = ok ? (T)(g * exp2_of(__builtin_fmaf((float)last, c, -lse))) : (T)0.0f;
+        const int next_head = before(next), next_whole = inside(next_head);
+        if (next_kept && single(next_head, next_whole) >= 0) last = logits[next * a.logits_stride + single(next_head, next_whole)];
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int at = (j * kRowThreads + tid) * n;
             if (GRAD && at < whole) {
                 V y = {};
                 if (ok) {
+                    float w[n];
+                    widen(x[j], w, T());
 #pragma unroll
-                    for (int i = 0; i < n; ++i) y[i] = (T)(g * exp2_of(__builtin_fmaf((float)x[j][i], c, -lse)));
+                    for (int i = 0; i < n; ++i) y[i] = (T)(g * exp2_of(__builtin_fmaf(w[i], c, -lse)));
                 }
-                *reinterpret_cast<V *>(grad + at) = y;
+                *reinterpret_cast<V *>(grad + head + at) = y;
             }
-            if (next_kept) load(next, j);
+            if (next_kept) load(next, next_head, next_whole, j);
         }
         if (GRAD) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the stores above come before those below
         __syncthreads();
@@ -308,28 +352,34 @@ __global__ void __launch_bounds__(kRowThreads, 4) distill_row_kernel(deft_distil
         index = next_index;
         u = next_u;
         kept = next_kept;
+        head = next_head;
+        whole = next_whole;
     }
 }
 
-template <typename T, int THREADS, int NV>
+// PER_UNIT: workgroups that a compute unit holds at once, by their registers.
+template <typename T, int THREADS, int NV, int PER_UNIT>
 hipError_t row_launch(const deft_distill_t &a, int compute_units, hipStream_t st)
 {
-    const int most = compute_units * (1024 / THREADS), blocks = a.n_rows < most ? a.n_rows : most;
+    const int most = compute_units * PER_UNIT, blocks = a.n_rows < most ? a.n_rows : most;
     if (a.grad_logits) distill_row_kernel<T, THREADS, NV, true><<<blocks, THREADS, 0, st>>>(a);
     else distill_row_kernel<T, THREADS, NV, false><<<blocks, THREADS, 0, st>>>(a);
     return hipGetLastError();
 }
 
-// By the row's bytes alone (and by top_k, an entry a lane).  Up to 128 KB two workgroups of 512 lanes share a
-// compute unit, so that one's reductions fall into the other's reads and writes.
+// By the row's bytes alone (and by top_k, an entry a lane): as few lanes as hold it, so that more workgroups
+// share a compute unit and one's reductions fall into the others' reads and writes.  Few rows (no more than
+// compute units) have one each to themselves: twice the lanes read them sooner.
 template <typename T>
 hipError_t any_launch(const deft_distill_t &a, int compute_units, hipStream_t st)
 {
     const int vectors = a.vocab / Vec<T>::n;
-    if (a.top_k <= 512 && vectors <= 512 * 4) return row_launch<T, 512, 4>(a, compute_units, st);
-    if (a.top_k <= 512 && vectors <= 512 * 8) return row_launch<T, 512, 8>(a, compute_units, st);
-    if (a.top_k <= 512 && vectors <= 512 * 16) return row_launch<T, 512, 16>(a, compute_units, st);
-    if (vectors <= 1024 * 16) return row_launch<T, 1024, 16>(a, compute_units, st);
+    const bool few = a.n_rows <= compute_units;
+    if (!few && a.top_k <= 256 && vectors <= 256 * 4) return row_launch<T, 256, 4, 7>(a, compute_units, st);
+    if (!few && a.top_k <= 512 && vectors <= 512 * 4) return row_launch<T, 512, 4, 3>(a, compute_units, st);
+    if (!few && a.top_k <= 512 && vectors <= 512 * 8) return row_launch<T, 512, 8, 2>(a, compute_units, st);
+    if (!few && a.top_k <= 512 && vectors <= 512 * 16) return row_launch<T, 512, 16, 2>(a, compute_units, st);
+    if (vectors <= 1024 * 16) return row_launch<T, 1024, 16, 1>(a, compute_units, st);
     distill_kernel<T><<<a.n_rows, kThreads, (size_t)a.top_k * 8, st>>>(a);
     return hipGetLastError();
 }
