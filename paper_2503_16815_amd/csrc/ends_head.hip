@@ -1,636 +1,15 @@
-// The head of a language model with its softmax cross entropy, the logits never kept.
-//
-//   z = s h w^T;  lse = log sum_v exp z_v;  loss = lse - z_label
-//   d = g (exp(z - lse) - [v == label]);  dh = s d w;  dw = s d^T h
-//
-// Positions without a label are left out first: the others are packed together, so that they cost nothing.
-// The loss is one product whose tiles leave each position's softmax sum (largest logit, sum of
-// exponentials) behind, joined afterwards.  The gradient takes the vocabulary in pieces: the product
-// again, its tiles turned into d as they come out of the matrix units (and d^T, so that each of the
-// three products reads both operands along k), then dw of the piece, final at once, and the piece's part
-// of dh, summed in 32 bits over the pieces.  Four products of 2 n V D operations: bound by the matrix
-// units where positions are many.
-#include "ends_product.h"
+// The head's scratch memory, and its calls by type (each type's kernels are a file of their own).
+#include "ends_shapes.h"
 
 namespace deft {
-namespace {
 
-constexpr int kTile = 256;
-constexpr int64_t kPieceBytes = (int64_t)1 << 29;    // of d and d^T together
-constexpr int64_t kWeightBytes = (int64_t)1 << 28;   // of a piece's rows, packed or transposed
-constexpr int kMaxSplits = 16;
-constexpr int kFew = 64;                             // positions that a tile of 64 holds
-
-int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
-
-// ---- positions that count -------------------------------------------------------------------
-
-struct RowsArgs {
-    int n, vocab;
-    const int32_t *labels;
-    int32_t *status;
-    float *loss, *lse_out;          // the loss call: zeros for the others
-    const float *lse, *row_grad;    // the gradient call: packed too
-    int32_t *count, *row_of, *at_of, *label;   // [1], [n] each
-    float *lse_packed, *grad_packed, *t_scale;
-    float t_top;                    // largest power of two that d^T may be scaled to, or 0 where it is not
-};
-
-__global__ void __launch_bounds__(1024) rows_kernel(RowsArgs a)
-{
-    __shared__ int wave_count[16];
-    __shared__ float wave_top[16];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    int base = 0;
-    float top = 0.0f;
-    for (int first = 0; first < a.n; first += 1024) {
-        const int i = first + tid;
-        const int label = i < a.n ? a.labels[i] : -1;
-        const bool in = label >= 0 && label < a.vocab;
-        const uint64_t mask = __ballot(in);
-        if (lane == 0) wave_count[wave] = __popcll(mask);
-        __syncthreads();
-        int at = base, all = 0;
-#pragma unroll
-        for (int w = 0; w < 16; ++w) {
-            if (w < wave) at += wave_count[w];
-            all += wave_count[w];
-        }
-        at += __popcll(mask & ((1ull << lane) - 1));
-        if (i < a.n) {
-            if (a.status) a.status[i] = in || label == -1 ? DEFT_OK : DEFT_ERR_INVALID_ARG;
-            a.at_of[i] = in ? at : -1;
-            if (in) {
-                a.row_of[at] = i;
-                a.label[at] = label;
-                if (a.row_grad) {
-                    a.lse_packed[at] = a.lse[i];
-                    a.grad_packed[at] = a.row_grad[i];
-                    top = fmaxf(top, fabsf(a.row_grad[i]));
-                }
-            } else if (a.loss) {
-                a.loss[i] = 0.0f;
-                a.lse_out[i] = 0.0f;
-            }
-        }
-        base += all;
-        __syncthreads();
-    }
-    top = wave_max(top);
-    if (lane == 0) wave_top[wave] = top;
-    __syncthreads();
-    if (tid == 0) {
-        *a.count = base;
-        for (int w = 0; w < 16; ++w) top = fmaxf(top, wave_top[w]);
-        // (between 2^e-1 and 2^e, so that the largest entry stays within t_top)
-        *a.t_scale = a.t_top > 0.0f && top > 0.0f && top < INFINITY ? ldexpf(a.t_top, -min(max(ilogbf(top) + 1, -100), 100)) : 1.0f;
-    }
-}
-
-// ---- operands as the products read them ------------------------------------------------------
-
-struct PackArgs {
-    const void *src;
-    int64_t src_stride;
-    int rows, cols;
-    const int *row_of, *rows_dev;   // packed positions, or NULL
-    void *out;                      // [rows up to a tile][out_ld], zeros beyond the source; or NULL
-    int64_t out_ld, out_plane;
-    void *out_t;                    // [cols][t_ld]; or NULL
-    int64_t t_ld, t_plane;
-};
-
-template <typename S, typename T, int P>
-__global__ void __launch_bounds__(256) pack_kernel(PackArgs a)
-{
-    typedef S S8 __attribute__((ext_vector_type(8), aligned(sizeof(S))));
-    typedef T T8 __attribute__((ext_vector_type(8)));
-    constexpr int kPitch = 66;
-    __shared__ T tile[P][64][kPitch];
-    const int col0 = blockIdx.x * 64, row0 = blockIdx.y * 64, tid = threadIdx.x;
-    const int rows = a.rows_dev ? *a.rows_dev : a.rows;
-    if (row0 >= (rows + kTile - 1) / kTile * kTile) return;
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        const int r = half * 32 + (tid >> 3), c = (tid & 7) * 8, row = row0 + r, col = col0 + c;
-        S x[8] = {};
-        if (row < rows) {
-            const S *from = static_cast<const S *>(a.src) + (int64_t)(a.row_of ? a.row_of[row] : row) * a.src_stride;
-            if (col + 8 <= a.cols) {
-                const S8 v = *reinterpret_cast<const S8 *>(from + col);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = v[i];
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (col + i < a.cols) x[i] = from[col + i];
-            }
-        }
-        T8 y[P];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if constexpr (P == 3) {
-                bf16 s[3];
-                split3(x[i], s);
-#pragma unroll
-                for (int p = 0; p < 3; ++p) y[p][i] = s[p];
-            } else {
-                y[0][i] = x[i];
-            }
-        }
-#pragma unroll
-        for (int p = 0; p < P; ++p) {
-            if (a.out) *reinterpret_cast<T8 *>(static_cast<T *>(a.out) + p * a.out_plane + (int64_t)row * a.out_ld + col) = y[p];
-            if (a.out_t) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) tile[p][r][c + i] = y[p][i];
-            }
-        }
-    }
-    if (!a.out_t) return;
-    __syncthreads();
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        const int c = half * 32 + (tid >> 3), r = (tid & 7) * 8;
-        if (col0 + c >= a.cols) continue;
-#pragma unroll
-        for (int p = 0; p < P; ++p) {
-            T8 y;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = tile[p][r + i][c];
-            *reinterpret_cast<T8 *>(static_cast<T *>(a.out_t) + p * a.t_plane + (int64_t)(col0 + c) * a.t_ld + row0 + r) = y;
-        }
-    }
-}
-
-// ---- joins ----------------------------------------------------------------------------------
-
-struct JoinArgs {
-    int tiles, parts_ld;
-    const int *count, *row_of;
-    const float2 *parts;
-    const float *z_label;
-    float *loss, *lse;
-};
-
-__global__ void __launch_bounds__(256) join_loss_kernel(JoinArgs a)
-{
-    const int at = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (at >= *a.count) return;
-    SoftSum s = {-INFINITY, 0.0f};
-    for (int t = lane; t < a.tiles; t += kWave) {
-        const float2 x = a.parts[(int64_t)at * a.parts_ld + t];
-        s = soft_join(s, SoftSum{x.x, x.y});
-    }
-    const float top = wave_max(s.top);
-    const float sum = wave_sum(s.sum == 0.0f ? 0.0f : s.sum * __expf(s.top - top));
-    if (lane == 0) {
-        const float lse = top + __logf(sum);
-        a.lse[a.row_of[at]] = lse;
-        a.loss[a.row_of[at]] = lse - a.z_label[at];
-    }
-}
-
-// Up to 64 positions are not packed together: those without a label are left out here.
-struct FewArgs {
-    int n, vocab, tiles;
-    const int32_t *labels;
-    const float2 *parts;
-    const float *z_label;
-    float *loss, *lse;
-    int32_t *status;
-};
-
-__global__ void __launch_bounds__(256) join_few_kernel(FewArgs a)
-{
-    __shared__ SoftSum of_wave[4];
-    const int row = blockIdx.x, tid = threadIdx.x;
-    const int label = a.labels[row];
-    SoftSum s = {-INFINITY, 0.0f};
-    for (int t = tid; t < a.tiles; t += 256) {
-        const float2 x = a.parts[(int64_t)row * a.tiles + t];
-        s = soft_join(s, SoftSum{x.x, x.y});
-    }
-    const float top = wave_max(s.top);
-    s.sum = wave_sum(s.sum == 0.0f ? 0.0f : s.sum * __expf(s.top - top));
-    if ((tid & 63) == 0) of_wave[tid >> 6] = SoftSum{top, s.sum};
-    __syncthreads();
-    if (tid != 0) return;
-    s = of_wave[0];
-#pragma unroll
-    for (int w = 1; w < 4; ++w) s = soft_join(s, of_wave[w]);
-    const bool in = label >= 0 && label < a.vocab;
-    const float lse = s.top + __logf(s.sum);
-    a.lse[row] = in ? lse : 0.0f;
-    a.loss[row] = in ? lse - a.z_label[row] : 0.0f;
-    if (a.status) a.status[row] = in || label == -1 ? DEFT_OK : DEFT_ERR_INVALID_ARG;
-}
-
-struct HiddenArgs {
-    int n, hidden, splits;
-    const int *at_of;
-    const float *sums, *grad;
-    int64_t sums_ld, sums_split;
-    float scale;
-    void *out;
-    int64_t out_stride;
-};
-
-template <typename O>
-__global__ void __launch_bounds__(256) join_hidden_kernel(HiddenArgs a)
-{
-    const int row = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (row >= a.n) return;
-    const int at = a.at_of[row];
-    O *out = static_cast<O *>(a.out) + (int64_t)row * a.out_stride;
-    const float alpha = at >= 0 ? a.grad[at] * a.scale : 0.0f;
-    for (int c = lane * 4; c < a.hidden; c += kWave * 4) {
-        f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (at >= 0) {
-            for (int s = 0; s < a.splits; ++s)
-                x += *reinterpret_cast<const f32x4 *>(a.sums + s * a.sums_split + (int64_t)at * a.sums_ld + c);
-            x *= alpha;
-        }
-        if (c + 4 <= a.hidden) {
-            typedef O O4 __attribute__((ext_vector_type(4), aligned(sizeof(O))));
-            *reinterpret_cast<O4 *>(out + c) = O4{(O)x[0], (O)x[1], (O)x[2], (O)x[3]};
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (c + i < a.hidden) out[c + i] = (O)x[i];
-        }
-    }
-}
-
-// ---- launches -------------------------------------------------------------------------------
-
-// The shape of a product's tiles.  Up to 64 rows of b: 256 x 64, bound by reading a.  Otherwise 256 x 256, one workgroup to
-// a compute unit, or 128 x 128, two to a compute unit (80 KB of LDS each), where that leaves fewer of them idle.
-enum Shape { kLarge, kSmall, kNarrow };
-
-// Rounds of the 256 x 256 shape that the tiles take.  A pair of small tiles on a compute unit takes 0.59 of a large one's
-// time, one alone 0.36.
-double rounds_of(Shape shape, int64_t m, int64_t n, int64_t splits, int64_t compute_units)
-{
-    if (shape == kNarrow) return (double)up(up(m, 256) / 256 * splits, compute_units) / (double)compute_units;
-    if (shape == kLarge) return (double)up(up(m, 256) / 256 * (up(n, 256) / 256) * splits, compute_units) / (double)compute_units;
-    const int64_t tiles = up(m, 128) / 128 * (up(n, 128) / 128) * splits, rest = tiles % (2 * compute_units);
-    return 0.59 * (double)(tiles / (2 * compute_units)) + (rest == 0 ? 0.0 : rest <= compute_units ? 0.36 : 0.59);
-}
-
-Shape shape_of(int64_t m, int64_t n, int64_t splits, int64_t compute_units)
-{
-    if (n <= kFew) return kNarrow;
-    return rounds_of(kSmall, m, n, splits, compute_units) < rounds_of(kLarge, m, n, splits, compute_units) ? kSmall : kLarge;
-}
-
-// Parts that a sum over k is cut into, where its tiles leave compute units idle: each part's sums go to memory and are
-// joined later, so there are no more of them than shorten the whole by a twentieth.
-int splits_of(int64_t m, int64_t n, int64_t k, int64_t compute_units)
-{
-    const int64_t tiles = up(m, 256) / 256 * (n <= kFew ? 1 : up(n, 256) / 256);
-    int best = 1;
-    double least = 1e30;
-    for (int s = 1; s <= kMaxSplits && (s == 1 || (tiles * s <= 2 * compute_units && k / kStep >= s * 8)); s *= 2) {
-        const double t = rounds_of(shape_of(m, n, s, compute_units), m, n, s, compute_units) / s;
-        if (t < 0.95 * least) {
-            least = t;
-            best = s;
-        }
-    }
-    return best;
-}
-
-template <typename T, typename O, int E, int WM, int WN, int MT, int NT, bool SPLIT>
-hipError_t product_shape(const ProductArgs &p, hipStream_t st)
-{
-    constexpr int TM = WM * MT * 16, TN = WN * NT * 16, kLds = product_lds(TM, TN);
-    const dim3 grid(((p.m + TM - 1) / TM) * ((p.n + TN - 1) / TN), p.splits);
-    product_kernel<T, O, E, WM, WN, MT, NT, SPLIT><<<grid, WM * WN * kWave, kLds, st>>>(p);
-    return hipGetLastError();
-}
-
-template <typename T, typename O, int E, bool SPLIT>
-hipError_t product(const ProductArgs &p, Shape shape, hipStream_t st)
-{
-    if (shape == kNarrow) return product_shape<T, O, E, 4, 2, 4, 2, SPLIT>(p, st);
-    if (shape == kSmall) return product_shape<T, O, E, 2, 2, 4, 4, SPLIT>(p, st);
-    return product_shape<T, O, E, 2, 4, 8, 4, SPLIT>(p, st);
-}
-
-template <typename T, typename O, int E, bool SPLIT>
-hipError_t allow_lds()
-{
-    const auto allow = [](const void *kernel, int tm, int tn) {
-        return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, product_lds(tm, tn));
-    };
-    hipError_t e = allow(reinterpret_cast<const void *>(&product_kernel<T, O, E, 2, 4, 8, 4, SPLIT>), 256, 256);
-    if (e == hipSuccess) e = allow(reinterpret_cast<const void *>(&product_kernel<T, O, E, 4, 2, 4, 2, SPLIT>), 256, 64);
-    if (e == hipSuccess) e = allow(reinterpret_cast<const void *>(&product_kernel<T, O, E, 2, 2, 4, 4, SPLIT>), 128, 128);
-    return e;
-}
-
-template <typename T, typename O, bool SPLIT>
-hipError_t allow_all()
-{
-    hipError_t e = allow_lds<T, O, kSoftmax, SPLIT>();
-    if (e == hipSuccess) e = allow_lds<T, O, kDerivative, SPLIT>();
-    if (e == hipSuccess) e = allow_lds<T, O, kSums, SPLIT>();
-    if (e == hipSuccess) e = allow_lds<T, O, kGradient, SPLIT>();
-    return e;
-}
-
-// One call's view of the scratch memory.
-struct Scratch {
-    int32_t *count, *row_of, *at_of, *label;
-    float *lse, *grad, *z_label, *t_scale;
-    float2 *parts;
-    char *hidden, *weight, *hidden_t, *weight_t, *d, *d_t;
-    float *sums;
-    Scratch(const HeadPlan &plan, void *scratch)
-    {
-        char *s = static_cast<char *>(scratch);
-        const int64_t n = up(plan.max_rows, kTile);
-        count = reinterpret_cast<int32_t *>(s + plan.ints);
-        row_of = count + 64;
-        at_of = row_of + n;
-        label = at_of + n;
-        t_scale = reinterpret_cast<float *>(s + plan.floats);
-        lse = t_scale + 64;
-        grad = lse + n;
-        z_label = grad + n;
-        parts = reinterpret_cast<float2 *>(s + plan.parts);
-        hidden = s + plan.hidden;
-        weight = s + plan.weight;
-        hidden_t = s + plan.hidden_t;
-        weight_t = s + plan.weight_t;
-        d = s + plan.d;
-        d_t = s + plan.d_t;
-        sums = reinterpret_cast<float *>(s + plan.sums);
-    }
-};
-
-// Whether a product can read rows of the weights where they are: whole steps of k (the next row's
-// elements, or what lies between rows, must not come in), 16-byte pieces, offsets within 32 bits.
-bool in_place(const void *p, int64_t stride, int hidden)
-{
-    return hidden % kStep == 0 && stride % 8 == 0 && ((uintptr_t)p & 15) == 0 && stride <= (1 << 22);
-}
-
-template <typename S, typename T, int P>
-struct Head {
-    static constexpr bool kSplit = P == 3;
-    static constexpr bool kHalf = __is_same(T, f16);
-
-    static hipError_t pack(const PackArgs &a, int rows_to, hipStream_t st)
-    {
-        const dim3 grid((unsigned)(up(a.cols, kStep) / 64), (unsigned)(rows_to / 64));
-        pack_kernel<S, T, P><<<grid, 256, 0, st>>>(a);
-        return hipGetLastError();
-    }
-
-    // hidden states (and, for the gradient, their transpose): of the positions that count, packed together, or of all
-    static hipError_t positions(const Scratch &s, const void *hidden_states, int64_t stride, int n, int hidden, bool counted,
-                                bool transposed, hipStream_t st)
-    {
-        const int64_t n_up = up(n, kTile), k = up(hidden, kStep);
-        PackArgs h{};
-        h.src = hidden_states;
-        h.src_stride = stride;
-        h.rows = n;
-        h.cols = hidden;
-        if (counted) {
-            h.row_of = s.row_of;
-            h.rows_dev = s.count;
-        }
-        h.out = s.hidden;
-        h.out_ld = k;
-        h.out_plane = n_up * k;
-        if (transposed) {
-            h.out_t = s.hidden_t;
-            h.t_ld = n_up;
-            h.t_plane = n_up * k;
-        }
-        return pack(h, (int)n_up, st);
-    }
-
-    // the operands of the logits of the vocabulary's rows `first` .. `first` + `rows` - 1
-    static hipError_t logits(const HeadPlan &plan, const Scratch &s, const void *weight, int64_t stride, int first, int rows, int n,
-                             int hidden, float scale, bool transposed, ProductArgs *p, hipStream_t st)
-    {
-        const int64_t k = up(hidden, kStep);
-        const S *from = static_cast<const S *>(weight) + (int64_t)first * stride;
-        const bool direct = !kSplit && in_place(weight, stride, hidden);
-        if (!direct || transposed) {
-            PackArgs w{};
-            w.src = from;
-            w.src_stride = stride;
-            w.rows = rows;
-            w.cols = hidden;
-            if (!direct) {
-                w.out = s.weight;
-                w.out_ld = k;
-                w.out_plane = (int64_t)plan.piece * k;
-            }
-            if (transposed) {
-                w.out_t = s.weight_t;
-                w.t_ld = plan.piece;
-                w.t_plane = (int64_t)plan.piece * k;
-            }
-            const hipError_t e = pack(w, (int)up(rows, kTile), st);
-            if (e != hipSuccess) return e;
-        }
-        *p = ProductArgs{};
-        p->a = direct ? static_cast<const void *>(from) : s.weight;
-        p->a_ld = direct ? stride : k;
-        p->a_plane = (int64_t)plan.piece * k;
-        p->b = s.hidden;
-        p->b_ld = k;
-        p->b_plane = up(n, kTile) * k;
-        p->m = rows;
-        p->n = n;
-        p->n_dev = s.count;
-        p->k = (int)k;
-        p->splits = 1;
-        p->scale = scale;
-        p->m_first = first;
-        p->label = s.label;
-        return hipSuccess;
-    }
-
-    static hipError_t loss(const HeadPlan &plan, const deft_head_loss_t &a, const Scratch &s, int compute_units, hipStream_t st)
-    {
-        const int n = a.n_rows;
-        const bool few = n <= kFew;
-        const bool from_caller = few && !kSplit && in_place(a.hidden_states, a.hidden_stride, a.hidden);
-        hipError_t e = hipSuccess;
-        if (!few) {
-            RowsArgs r{};
-            r.n = n;
-            r.vocab = a.vocab;
-            r.labels = a.labels;
-            r.status = a.status;
-            r.loss = a.loss;
-            r.lse_out = a.lse;
-            r.count = s.count;
-            r.row_of = s.row_of;
-            r.at_of = s.at_of;
-            r.label = s.label;
-            r.t_scale = s.t_scale;
-            rows_kernel<<<1, 1024, 0, st>>>(r);
-        }
-        if (!from_caller) e = positions(s, a.hidden_states, a.hidden_stride, n, a.hidden, !few, false, st);
-        const bool whole = !kSplit && in_place(a.weight, a.weight_stride, a.hidden);   // nothing to pack: no pieces
-        const int piece = whole || a.vocab < plan.piece ? a.vocab : plan.piece;
-        const Shape shape = shape_of(piece, n, 1, compute_units);
-        const int tiles = (int)(up(a.vocab, shape == kSmall ? 128 : 256) / (shape == kSmall ? 128 : 256));
-        for (int first = 0; first < a.vocab && e == hipSuccess; first += piece) {
-            const int rows = a.vocab - first < piece ? a.vocab - first : piece;
-            ProductArgs p;
-            e = logits(plan, s, a.weight, a.weight_stride, first, rows, n, a.hidden, a.logit_scale, false, &p, st);
-            p.parts = s.parts;
-            p.parts_ld = tiles;
-            p.z_label = s.z_label;
-            if (few) {
-                p.n_dev = nullptr;
-                p.label = a.labels;
-            }
-            if (from_caller) {
-                p.b = a.hidden_states;
-                p.b_ld = a.hidden_stride;
-            }
-            if (e == hipSuccess) e = product<T, S, kSoftmax, kSplit>(p, shape, st);
-        }
-        if (e != hipSuccess) return e;
-        if (few) {
-            FewArgs f{};
-            f.n = n;
-            f.vocab = a.vocab;
-            f.tiles = tiles;
-            f.labels = a.labels;
-            f.parts = s.parts;
-            f.z_label = s.z_label;
-            f.loss = a.loss;
-            f.lse = a.lse;
-            f.status = a.status;
-            join_few_kernel<<<n, 256, 0, st>>>(f);
-            return hipGetLastError();
-        }
-        JoinArgs j{};
-        j.tiles = tiles;
-        j.parts_ld = tiles;
-        j.count = s.count;
-        j.row_of = s.row_of;
-        j.parts = s.parts;
-        j.z_label = s.z_label;
-        j.loss = a.loss;
-        j.lse = a.lse;
-        join_loss_kernel<<<(n + 3) / 4, 256, 0, st>>>(j);
-        return hipGetLastError();
-    }
-
-    static hipError_t gradient(const HeadPlan &plan, const deft_head_grad_t &a, const Scratch &s, int compute_units, hipStream_t st)
-    {
-        const int n = a.n_rows;
-        const int64_t n_up = up(n, kTile), k = up(a.hidden, kStep), sums_ld = up(a.hidden, 4);
-        const float d_scale = kHalf ? 32768.0f : 1.0f;   // |softmax - one| <= 1 fills the range of a 16-bit float
-        RowsArgs r{};
-        r.n = n;
-        r.vocab = a.vocab;
-        r.labels = a.labels;
-        r.lse = a.lse;
-        r.row_grad = a.row_grad;
-        r.count = s.count;
-        r.row_of = s.row_of;
-        r.at_of = s.at_of;
-        r.label = s.label;
-        r.lse_packed = s.lse;
-        r.grad_packed = s.grad;
-        r.t_scale = s.t_scale;
-        r.t_top = kHalf ? 32768.0f : 0.0f;
-        rows_kernel<<<1, 1024, 0, st>>>(r);
-        hipError_t e = hipGetLastError();
-        if (e == hipSuccess && n > 0) e = positions(s, a.hidden_states, a.hidden_stride, n, a.hidden, true, a.grad_weight != nullptr, st);
-
-        const int splits = splits_of(a.hidden, n, plan.piece < a.vocab ? plan.piece : a.vocab, compute_units);
-        int piece_number = 0;
-        for (int first = 0; first < a.vocab && e == hipSuccess; first += plan.piece, ++piece_number) {
-            const int rows = a.vocab - first < plan.piece ? a.vocab - first : plan.piece;
-            ProductArgs p{};
-            if (n > 0) {
-                e = logits(plan, s, a.weight, a.weight_stride, first, rows, n, a.hidden, a.logit_scale, a.grad_hidden != nullptr, &p, st);
-                p.lse = s.lse;
-                p.row_grad = s.grad;
-                p.t_scale = s.t_scale;
-                p.d_scale = d_scale;
-                p.d = s.d;
-                p.d_ld = plan.piece;
-                p.d_plane = n_up * plan.piece;
-                p.d_t = s.d_t;
-                p.d_t_ld = n_up;
-                p.d_t_plane = n_up * plan.piece;
-                if (e == hipSuccess) e = product<T, S, kDerivative, kSplit>(p, shape_of(rows, n, 1, compute_units), st);
-            }
-            if (e == hipSuccess && a.grad_weight) {
-                ProductArgs q{};
-                q.a = s.hidden_t;
-                q.a_ld = n_up;
-                q.a_plane = n_up * k;
-                q.b = s.d_t;
-                q.b_ld = n_up;
-                q.b_plane = n_up * plan.piece;
-                q.m = a.hidden;
-                q.n = rows;
-                q.k_dev = s.count;
-                q.splits = 1;
-                q.scale = a.logit_scale;
-                q.t_scale = s.t_scale;
-                q.add = a.accumulate;
-                q.out = static_cast<S *>(a.grad_weight) + (int64_t)first * a.grad_weight_stride;
-                q.out_ld = a.grad_weight_stride;
-                e = product<T, S, kGradient, kSplit>(q, shape_of(a.hidden, rows, 1, compute_units), st);
-            }
-            if (e == hipSuccess && piece_number < a.n_piece_events)
-                e = hipEventRecord(static_cast<hipEvent_t>(a.piece_events[piece_number]), st);
-            if (e == hipSuccess && a.grad_hidden && n > 0) {
-                ProductArgs q{};
-                q.a = s.weight_t;
-                q.a_ld = plan.piece;
-                q.a_plane = (int64_t)plan.piece * k;
-                q.b = s.d;
-                q.b_ld = plan.piece;
-                q.b_plane = n_up * plan.piece;
-                q.m = a.hidden;
-                q.n = n;
-                q.n_dev = s.count;
-                q.k = (int)up(rows, kStep);
-                q.splits = splits;
-                q.sums = s.sums;
-                q.sums_ld = sums_ld;
-                q.sums_split = n_up * sums_ld;
-                q.add = first > 0;
-                e = product<T, S, kSums, kSplit>(q, shape_of(a.hidden, n, splits, compute_units), st);
-            }
-        }
-        if (e != hipSuccess || !a.grad_hidden || n == 0) return e;
-        HiddenArgs j{};
-        j.n = n;
-        j.hidden = a.hidden;
-        j.splits = splits;
-        j.at_of = s.at_of;
-        j.sums = s.sums;
-        j.grad = s.grad;
-        j.sums_ld = sums_ld;
-        j.sums_split = n_up * sums_ld;
-        j.scale = a.logit_scale / d_scale;
-        j.out = a.grad_hidden;
-        j.out_stride = a.grad_hidden_stride;
-        join_hidden_kernel<S><<<(n + 3) / 4, 256, 0, st>>>(j);
-        return hipGetLastError();
-    }
-};
-
-}  // namespace
+#define DEFT_HEAD_TYPE(NAME)                                                                                                   \
+    hipError_t head_prepare_##NAME();                                                                                          \
+    hipError_t head_loss_##NAME(const HeadPlan &, const deft_head_loss_t &, void *, int, hipStream_t);                         \
+    hipError_t head_grad_##NAME(const HeadPlan &, const deft_head_grad_t &, void *, int, hipStream_t);
+DEFT_HEAD_TYPE(bf16)
+DEFT_HEAD_TYPE(f16)
+DEFT_HEAD_TYPE(f32)
 
 void head_plan(int dtype, int max_rows, int max_vocab, int max_hidden, bool grad, int compute_units, HeadPlan *plan)
 {
@@ -647,8 +26,27 @@ void head_plan(int dtype, int max_rows, int max_vocab, int max_hidden, bool grad
     }
     piece = piece / kTile * kTile;
     if (piece < 4 * kTile) piece = 4 * kTile;
-    const int64_t pieces = (max_vocab + piece - 1) / piece;   // of nearly the same size
-    piece = up((max_vocab + pieces - 1) / pieces, kTile);
+    if (piece > up(max_vocab, kTile)) piece = up(max_vocab, kTile);
+    if (grad) {   // of the sizes that fit, the one whose products leave the fewest compute units idle over all pieces
+        const int64_t products = plan->planes == 3 ? 6 : 1, most = piece;
+        double least = 1e300;
+        for (int64_t p = most; p >= kTile && p * 8 >= most; p -= kTile) {
+            double t = 0.0;
+            const int64_t whole = max_vocab / p, rest = max_vocab % p;
+            for (int last = 0; last < 2; ++last) {
+                const int64_t rows = last ? rest : p, times = last ? 1 : whole;
+                if (rows == 0 || times == 0) continue;
+                const int64_t steps = up(rows, kStep) / kStep * products;
+                t += (double)times * (12.0 + least_cost(rows, max_rows, k / kStep * products, 1, compute_units) +
+                                      least_cost(max_hidden, rows, up(max_rows, kStep) / kStep * products, 1, compute_units) +
+                                      least_cost(max_hidden, max_rows, steps, splits_of(max_hidden, max_rows, steps, compute_units), compute_units));
+            }
+            if (t < least) {
+                least = t;
+                piece = p;
+            }
+        }
+    }
     plan->piece = (int)piece;
     int64_t at = 0;
     const auto take = [&](int64_t bytes) {
@@ -675,28 +73,26 @@ void head_plan(int dtype, int max_rows, int max_vocab, int max_hidden, bool grad
 
 hipError_t head_prepare()
 {
-    hipError_t e = allow_all<bf16, bf16, false>();
-    if (e == hipSuccess) e = allow_all<f16, f16, false>();
-    if (e == hipSuccess) e = allow_all<bf16, float, true>();
+    hipError_t e = head_prepare_bf16();
+    if (e == hipSuccess) e = head_prepare_f16();
+    if (e == hipSuccess) e = head_prepare_f32();
     return e;
 }
 
 hipError_t head_loss_launch(const HeadPlan &plan, int dtype, const deft_head_loss_t &a, void *scratch, int compute_units,
                             hipStream_t st)
 {
-    const Scratch s(plan, scratch);
-    if (dtype == DEFT_F32) return Head<float, bf16, 3>::loss(plan, a, s, compute_units, st);
-    if (dtype == DEFT_F16) return Head<f16, f16, 1>::loss(plan, a, s, compute_units, st);
-    return Head<bf16, bf16, 1>::loss(plan, a, s, compute_units, st);
+    if (dtype == DEFT_F32) return head_loss_f32(plan, a, scratch, compute_units, st);
+    if (dtype == DEFT_F16) return head_loss_f16(plan, a, scratch, compute_units, st);
+    return head_loss_bf16(plan, a, scratch, compute_units, st);
 }
 
 hipError_t head_grad_launch(const HeadPlan &plan, int dtype, const deft_head_grad_t &a, void *scratch, int compute_units,
                             hipStream_t st)
 {
-    const Scratch s(plan, scratch);
-    if (dtype == DEFT_F32) return Head<float, bf16, 3>::gradient(plan, a, s, compute_units, st);
-    if (dtype == DEFT_F16) return Head<f16, f16, 1>::gradient(plan, a, s, compute_units, st);
-    return Head<bf16, bf16, 1>::gradient(plan, a, s, compute_units, st);
+    if (dtype == DEFT_F32) return head_grad_f32(plan, a, scratch, compute_units, st);
+    if (dtype == DEFT_F16) return head_grad_f16(plan, a, scratch, compute_units, st);
+    return head_grad_bf16(plan, a, scratch, compute_units, st);
 }
 
 }  // namespace deft

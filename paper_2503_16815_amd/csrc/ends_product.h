@@ -20,11 +20,10 @@
 // 32-bit operands come as three 16-bit arrays whose sum they are (8 bits of the significand in
 // each); the six products of those arrays that matter at 24 bits are summed one after the other.
 #pragma once
-#include "ends.h"
+#include "ends_shapes.h"
 
 namespace deft {
 
-constexpr int kStep = 64;            // elements of k per step
 constexpr int kStepBytes = kStep * 2;
 
 enum Epilogue { kSoftmax = 0, kDerivative = 1, kSums = 2, kGradient = 3 };
@@ -43,7 +42,7 @@ struct ProductArgs {
     int m_first;
     const int *label;                // [n]
     float2 *parts;                   // [n][parts_ld]: each tile's softmax sum of the position
-    int parts_ld;
+    int parts_ld, parts_first;       // the number of the first tile's part
     float *z_label;                  // [n]
     const float *lse;                // [n]
     const float *row_grad;           // [n]
@@ -112,7 +111,12 @@ __device__ __forceinline__ unsigned pack2(bf16 a, bf16 b)
 }
 
 constexpr int kStagesA = 3, kStagesB = 2;
-constexpr int product_lds(int tm, int tn) { return (kStagesA * tm + kStagesB * tn) * kStepBytes; }
+// The rows that a tile's loads bring: every thread loads 16 bytes, an eighth of a row, at a time.
+constexpr int product_rows(int rows, int threads) { return (rows * 8 + threads - 1) / threads * threads / 8; }
+constexpr int product_lds(int tm, int tn, int threads)
+{
+    return (kStagesA * product_rows(tm, threads) + kStagesB * product_rows(tn, threads)) * kStepBytes;
+}
 
 // All of this wavefront's LDS reads are done, and all but `N` of its loads; then the others' are too.
 template <int N>
@@ -134,10 +138,10 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
 {
 #ifdef __HIP_DEVICE_COMPILE__   // (buffer descriptors are a type of the device's alone)
     constexpr int kThreads = WM * WN * kWave, TM = WM * MT * 16, TN = WN * NT * 16;
-    constexpr int kABytes = TM * kStepBytes, kBBytes = TN * kStepBytes, kBAt = kStagesA * kABytes;
-    constexpr int kALoads = TM * 8 / kThreads, kBLoads = TN * 8 / kThreads;
+    constexpr int kARows = product_rows(TM, kThreads), kBRows = product_rows(TN, kThreads);   // that whole loads bring
+    constexpr int kABytes = kARows * kStepBytes, kBBytes = kBRows * kStepBytes, kBAt = kStagesA * kABytes;
+    constexpr int kALoads = kARows * 8 / kThreads, kBLoads = kBRows * 8 / kThreads;
     constexpr int kFetches = MT + NT, kProducts = MT * NT;
-    static_assert(kALoads * kThreads == TM * 8 && kBLoads * kThreads == TN * 8, "whole loads");
     typedef typename Mfma<T>::operand Operand;
     extern __shared__ __align__(16) char lds[];
 
@@ -320,7 +324,7 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
             SoftSum s = {joined[i].x, joined[i].y};
 #pragma unroll
             for (int w = 1; w < WM; ++w) s = soft_join(s, SoftSum{joined[w * TN + i].x, joined[w * TN + i].y});
-            p.parts[(int64_t)(n0 + i) * p.parts_ld + p.m_first / TM + tm] = make_float2(s.top, s.sum);
+            p.parts[(int64_t)(n0 + i) * p.parts_ld + p.parts_first + tm] = make_float2(s.top, s.sum);
         }
     } else if constexpr (E == kDerivative) {
         const float t_scale = *p.t_scale;
@@ -402,6 +406,8 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
             }
         }
     }
+#else
+    (void)p;
 #endif
 }
 
