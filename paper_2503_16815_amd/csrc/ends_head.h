@@ -3,12 +3,15 @@
 //   z = s h w^T;  lse = log sum_v exp z_v;  loss = lse - z_label
 //   d = g (exp(z - lse) - [v == label]);  dh = s d w;  dw = s d^T h
 //
+// Each row's g is taken apart, g = f 2^e with 1 <= f < 2.  d is rounded to the type with f alone (in 16-bit floats times
+// 2^14, so that softmax values down to 1e-9 keep their bits); the powers of two come back exactly, in
+// dh by the row, in dw with the transposed hidden states relative to the largest.
+//
 // Positions without a label are left out first: the others are packed together, so that they cost nothing.
 // The loss is one product whose tiles leave each position's softmax sum (largest logit, sum of
 // exponentials) behind, joined afterwards.  The gradient takes the vocabulary in pieces: the product
-// again, its tiles turned into d as they come out of the matrix units (and d^T, so that each of the
-// three products reads both operands along k), then dw of the piece, final at once, and the piece's part
-// of dh, summed in 32 bits over the pieces.  Four products of 2 n V D operations: bound by the matrix
+// again, its tiles turned into d as they come out of the matrix units, then dw of the piece, final at
+// once, and the piece's part of dh, summed in 32 bits over the pieces.  Four products of 2 n V D operations: bound by the matrix
 // units where positions are many.
 #pragma once
 #include "ends_product.h"
@@ -26,8 +29,8 @@ struct RowsArgs {
     float *loss, *lse_out;          // the loss call: zeros for the others
     const float *lse, *row_grad;    // the gradient call: packed too
     int32_t *count, *row_of, *at_of, *label;   // [1], [n] each
-    float *lse_packed, *grad_packed, *t_scale;
-    float t_top;                    // largest power of two that d^T may be scaled to, or 0 where it is not
+    float *lse_packed, *grad_packed, *power, *most;   // [n]: f times d_scale and 2^e; [1]: the largest power
+    float d_scale;
 };
 
 __global__ void __launch_bounds__(1024) rows_kernel(RowsArgs a)
@@ -58,9 +61,14 @@ __global__ void __launch_bounds__(1024) rows_kernel(RowsArgs a)
                 a.row_of[at] = i;
                 a.label[at] = label;
                 if (a.row_grad) {
+                    const float g = a.row_grad[i], size = fabsf(g);
+                    // (zero, infinity and NaN stay as they are; the smallest numbers have f < 1)
+                    const int e = size > 0.0f && size < INFINITY ? max(ilogbf(size), -100) : -100;
+                    const bool taken = e > -100 || (size > 0.0f && size < INFINITY);
                     a.lse_packed[at] = a.lse[i];
-                    a.grad_packed[at] = a.row_grad[i];
-                    top = fmaxf(top, fabsf(a.row_grad[i]));
+                    a.grad_packed[at] = (taken ? ldexpf(g, -e) : g) * a.d_scale;
+                    a.power[at] = taken ? ldexpf(1.0f, e) : 1.0f;
+                    if (taken) top = fmaxf(top, ldexpf(1.0f, e));
                 }
             } else if (a.loss) {
                 a.loss[i] = 0.0f;
@@ -76,8 +84,7 @@ __global__ void __launch_bounds__(1024) rows_kernel(RowsArgs a)
     if (tid == 0) {
         *a.count = base;
         for (int w = 0; w < 16; ++w) top = fmaxf(top, wave_top[w]);
-        // (between 2^e-1 and 2^e, so that the largest entry stays within t_top)
-        *a.t_scale = a.t_top > 0.0f && top > 0.0f && top < INFINITY ? ldexpf(a.t_top, -min(max(ilogbf(top) + 1, -100), 100)) : 1.0f;
+        if (a.most) *a.most = top > 0.0f ? top : 1.0f;
     }
 }
 
@@ -92,6 +99,7 @@ struct PackArgs {
     int64_t out_ld, out_plane;
     void *out_t;                    // [cols][t_ld]; or NULL
     int64_t t_ld, t_plane;
+    const float *power, *most;      // out_t's columns are scaled by power[row] / most; or NULL
 };
 
 template <typename S, typename T, int P>
@@ -135,9 +143,19 @@ __global__ void __launch_bounds__(256) pack_kernel(PackArgs a)
 #pragma unroll
         for (int p = 0; p < P; ++p) {
             if (a.out) *reinterpret_cast<T8 *>(static_cast<T *>(a.out) + p * a.out_plane + (int64_t)row * a.out_ld + col) = y[p];
-            if (a.out_t) {
+        }
+        if (a.out_t) {
+            const float scale = a.power && row < rows ? a.power[row] / *a.most : 1.0f;   // (a power of two up to 1, or 0)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) tile[p][r][c + i] = y[p][i];
+            for (int i = 0; i < 8; ++i) {
+                if constexpr (P == 3) {
+                    bf16 s[3];
+                    split3(x[i] * scale, s);
+#pragma unroll
+                    for (int p = 0; p < 3; ++p) tile[p][r][c + i] = s[p];
+                } else {
+                    tile[0][r][c + i] = (T)((float)x[i] * scale);
+                }
             }
         }
     }
@@ -223,7 +241,7 @@ __global__ void __launch_bounds__(256) join_few_kernel(FewArgs a)
 struct HiddenArgs {
     int n, hidden, splits;
     const int *at_of;
-    const float *sums, *grad;
+    const float *sums, *power;
     int64_t sums_ld, sums_split;
     float scale;
     void *out;
@@ -237,7 +255,7 @@ __global__ void __launch_bounds__(256) join_hidden_kernel(HiddenArgs a)
     if (row >= a.n) return;
     const int at = a.at_of[row];
     O *out = static_cast<O *>(a.out) + (int64_t)row * a.out_stride;
-    const float alpha = at >= 0 ? a.grad[at] * a.scale : 0.0f;
+    const float alpha = at >= 0 ? a.power[at] * a.scale : 0.0f;
     for (int c = lane * 4; c < a.hidden; c += kWave * 4) {
         f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
         if (at >= 0) {
@@ -312,9 +330,9 @@ hipError_t allow_all()
 // One call's view of the scratch memory.
 struct Scratch {
     int32_t *count, *row_of, *at_of, *label;
-    float *lse, *grad, *z_label, *t_scale;
+    float *lse, *grad, *z_label, *power, *most;
     float2 *parts;
-    char *hidden, *weight, *hidden_t, *weight_t, *d, *d_t;
+    char *hidden, *weight, *hidden_t, *weight_t, *d;
     float *sums;
     Scratch(const HeadPlan &plan, void *scratch)
     {
@@ -324,17 +342,17 @@ struct Scratch {
         row_of = count + 64;
         at_of = row_of + n;
         label = at_of + n;
-        t_scale = reinterpret_cast<float *>(s + plan.floats);
-        lse = t_scale + 64;
+        most = reinterpret_cast<float *>(s + plan.floats);
+        lse = most + 64;
         grad = lse + n;
         z_label = grad + n;
+        power = z_label + n;
         parts = reinterpret_cast<float2 *>(s + plan.parts);
         hidden = s + plan.hidden;
         weight = s + plan.weight;
         hidden_t = s + plan.hidden_t;
         weight_t = s + plan.weight_t;
         d = s + plan.d;
-        d_t = s + plan.d_t;
         sums = reinterpret_cast<float *>(s + plan.sums);
     }
 };
@@ -379,6 +397,8 @@ struct Head {
             h.out_t = s.hidden_t;
             h.t_ld = n_up;
             h.t_plane = n_up * k;
+            h.power = s.power;
+            h.most = s.most;
         }
         return pack(h, (int)n_up, st);
     }
@@ -445,7 +465,6 @@ struct Head {
             r.row_of = s.row_of;
             r.at_of = s.at_of;
             r.label = s.label;
-            r.t_scale = s.t_scale;
             rows_kernel<<<1, 1024, 0, st>>>(r);
         }
         if (!from_caller) e = positions(s, a.hidden_states, a.hidden_stride, n, a.hidden, !few, false, st);
@@ -508,7 +527,7 @@ struct Head {
     {
         const int n = a.n_rows;
         const int64_t n_up = up(n, kTile), k = up(a.hidden, kStep), sums_ld = up(a.hidden, 4);
-        const float d_scale = kHalf ? 32768.0f : 1.0f;   // |softmax - one| <= 1 fills the range of a 16-bit float
+        const float d_scale = kHalf ? 16384.0f : 1.0f;   // |softmax - one| f < 2 fills the range of a 16-bit float
         RowsArgs r{};
         r.n = n;
         r.vocab = a.vocab;
@@ -521,8 +540,9 @@ struct Head {
         r.label = s.label;
         r.lse_packed = s.lse;
         r.grad_packed = s.grad;
-        r.t_scale = s.t_scale;
-        r.t_top = kHalf ? 32768.0f : 0.0f;
+        r.power = s.power;
+        r.most = s.most;
+        r.d_scale = d_scale;
         rows_kernel<<<1, 1024, 0, st>>>(r);
         hipError_t e = hipGetLastError();
         if (e == hipSuccess && n > 0) e = positions(s, a.hidden_states, a.hidden_stride, n, a.hidden, true, a.grad_weight != nullptr, st);
@@ -538,14 +558,10 @@ struct Head {
                 e = logits(plan, s, a.weight, a.weight_stride, first, rows, n, a.hidden, a.logit_scale, a.grad_hidden != nullptr, &p, st);
                 p.lse = s.lse;
                 p.row_grad = s.grad;
-                p.t_scale = s.t_scale;
-                p.d_scale = d_scale;
                 p.d = s.d;
-                p.d_ld = plan.piece;
+                p.d_cols = plan.piece;
+                p.d_panel = n_up * 256;
                 p.d_plane = n_up * plan.piece;
-                p.d_t = s.d_t;
-                p.d_t_ld = n_up;
-                p.d_t_plane = n_up * plan.piece;
                 if (e == hipSuccess) e = product<T, S, kDerivative, kSplit>(p, shape_of(rows, n, logit_steps, 1, compute_units), st);
             }
             if (e == hipSuccess && a.grad_weight) {
@@ -553,15 +569,16 @@ struct Head {
                 q.a = s.hidden_t;
                 q.a_ld = n_up;
                 q.a_plane = n_up * k;
-                q.b = s.d_t;
-                q.b_ld = n_up;
+                q.b = s.d;
+                q.b_ld = 256;
                 q.b_plane = n_up * plan.piece;
+                q.d_panel = n_up * 256;
                 q.m = a.hidden;
                 q.n = rows;
                 q.k_dev = s.count;
                 q.splits = 1;
-                q.scale = a.logit_scale;
-                q.t_scale = s.t_scale;
+                q.scale = a.logit_scale / d_scale;
+                q.out_scale = s.most;
                 q.add = a.accumulate;
                 q.out = static_cast<S *>(a.grad_weight) + (int64_t)first * a.grad_weight_stride;
                 q.out_ld = a.grad_weight_stride;
@@ -575,8 +592,9 @@ struct Head {
                 q.a_ld = plan.piece;
                 q.a_plane = (int64_t)plan.piece * k;
                 q.b = s.d;
-                q.b_ld = plan.piece;
+                q.b_ld = 256;
                 q.b_plane = n_up * plan.piece;
+                q.d_panel = n_up * 256;
                 q.m = a.hidden;
                 q.n = n;
                 q.n_dev = s.count;
@@ -596,7 +614,7 @@ struct Head {
         j.splits = splits;
         j.at_of = s.at_of;
         j.sums = s.sums;
-        j.grad = s.grad;
+        j.power = s.power;
         j.sums_ld = sums_ld;
         j.sums_split = n_up * sums_ld;
         j.scale = a.logit_scale / d_scale;

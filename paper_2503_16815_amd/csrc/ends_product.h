@@ -1,7 +1,8 @@
-// The matrix product that the head's operators are made of:  C[m][n] = sum_k A[m][k] B[n][k], both
-// operands with their k elements next to each other, 16-bit elements, 32-bit sums.  What happens
-// to C is the epilogue's business (it is never stored as it is): softmax statistics, the loss's
-// derivative, or a sum into a gradient.
+// The matrix product that the head's operators are made of:  C[m][n] = sum_k A[m][k] B[n][k], 16-bit
+// elements, 32-bit sums.  Both operands have their k elements next to each other, or B its n
+// elements (kGradient, which so reads the derivative as it was written).  What happens to C is the
+// epilogue's business (it is never stored as it is): softmax statistics, the loss's derivative,
+// or a sum into a gradient.
 //
 // A workgroup of eight wavefronts owns a tile of C.  Both operands' tiles go from memory to LDS without
 // passing registers, 64 elements of k at a time.  LDS holds three of A's and two of B's (160 KB at 256 x 256):
@@ -9,10 +10,16 @@
 // over the half's matrix instructions, so that neither waits for the other (measured at 8192^3 in bf16: all of it at
 // the step's beginning 1130 TFLOP/s, spread 1230; addresses in 64-bit registers instead of a buffer's 1180).  The fragments
 // of a half are read from LDS during the half before.  The matrix instructions are written out, so that
-// sums stay in accumulation registers and everything else comes between them in this order.
+// sums stay in accumulation registers and everything else comes between them in this order, and so are the loads to
+// LDS, which have no register to wait for: the compiler would let every transposing LDS read wait for all of them.
 //
 // The 16-byte pieces of a row are permuted by the row's number, so that the sixteen rows that a wavefront
-// reads together lie in different banks (no bank conflicts counted).
+// reads together lie in different banks (no bank conflicts counted).  A B with its n elements next to each other
+// lies in LDS as it came, a row of TN elements to each k; the transposing LDS read gives every lane four k of its
+// column, from four rows whose 32-byte pieces are permuted by the row's number too.
+//
+// The derivative lies in panels of 256 columns, so that a step of either product that reads it finds it in one
+// stretch of memory.
 //
 // Tiles are dealt out so that the workgroups of an XCD work on neighbouring ones, four wide: 12 rows of tiles
 // come into its L2 for 32 workgroups instead of 33 (131072 x 8192 x 4096: 890 to 1110 TFLOP/s by itself).
@@ -29,7 +36,7 @@ constexpr int kStepBytes = kStep * 2;
 enum Epilogue { kSoftmax = 0, kDerivative = 1, kSums = 2, kGradient = 3 };
 
 struct ProductArgs {
-    const void *a, *b;
+    const void *a, *b;               // kSums, kGradient: b is the derivative, as below
     int64_t a_ld, b_ld;              // elements between rows
     int64_t a_plane, b_plane;        // elements between the three arrays of a 32-bit operand
     int m, n;                        // rows of a and of b
@@ -45,15 +52,15 @@ struct ProductArgs {
     int parts_ld, parts_first;       // the number of the first tile's part
     float *z_label;                  // [n]
     const float *lse;                // [n]
-    const float *row_grad;           // [n]
-    const float *t_scale;            // the power of two that d_t is scaled with
-    float d_scale;                   // the one that d is scaled with
-    void *d, *d_t;                   // [n][d_ld], [m][d_t_ld]
-    int64_t d_ld, d_t_ld, d_plane, d_t_plane;
+    const float *row_grad;           // [n], scaled into d's range
+    void *d;                         // panels of 256 columns: [d_cols / 256][rows][256]
+    int64_t d_panel, d_plane;        // elements between panels, between the three arrays
+    int d_cols;
     // kSums: sums[split][n][m]; kGradient: out[n][m]
     float *sums;
     int64_t sums_ld, sums_split;
     int add;
+    const float *out_scale;          // beside `scale`
     void *out;
     int64_t out_ld;
 };
@@ -88,19 +95,6 @@ __device__ __forceinline__ void split3(float x, bf16 (&p)[3])
     p[2] = (bf16)(rest - second);
 }
 
-// Four rows' values of four neighbouring lanes, two to a word: lane q of the four gets row q's.
-__device__ __forceinline__ uint2 transpose4(unsigned x01, unsigned x23)
-{
-    const int q = threadIdx.x & 3;
-    const unsigned far = __builtin_amdgcn_update_dpp(0u, q < 2 ? x23 : x01, 0x4E, 0xf, 0xf, true);   // from lane ^ 2
-    const unsigned a = q < 2 ? x01 : far, b = q < 2 ? far : x23;
-    const bool odd = q & 1;
-    const unsigned lo = __builtin_amdgcn_perm(b, a, 0x05040100u), hi = __builtin_amdgcn_perm(b, a, 0x07060302u);
-    const unsigned got = __builtin_amdgcn_update_dpp(0u, odd ? lo : hi, 0xB1, 0xf, 0xf, true);       // from lane ^ 1
-    const unsigned left = odd ? got : lo, right = odd ? hi : got;
-    return make_uint2(__builtin_amdgcn_perm(right, left, 0x05040100u), __builtin_amdgcn_perm(right, left, 0x07060302u));
-}
-
 __device__ __forceinline__ unsigned pack2(f16 a, f16 b)
 {
     return (unsigned)__builtin_bit_cast(unsigned short, a) | (unsigned)__builtin_bit_cast(unsigned short, b) << 16;
@@ -127,6 +121,17 @@ __device__ __forceinline__ void step_barrier()
     asm volatile("" ::: "memory");
 }
 
+// 16 bytes a lane from `from` + offset + at to LDS, a wavefront's lanes one after the other from to_lds on.
+__device__ __forceinline__ void load_to_lds(i32x4 from, unsigned offset, int at, unsigned to_lds)
+{
+    asm volatile("s_mov_b32 m0, %3\n"
+                 "s_nop 0\n"
+                 "buffer_load_dwordx4 %1, %0, %2 offen lds"
+                 :
+                 : "s"(from), "v"(offset), "s"(at), "s"(to_lds)
+                 : "memory", "m0");
+}
+
 template <int H> struct HalfOf {
     static constexpr int value = H;
 };
@@ -136,12 +141,17 @@ template <int H> struct HalfOf {
 template <typename T, typename O, int E, int WM, int WN, int MT, int NT, bool SPLIT>
 __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p)
 {
-#ifdef __HIP_DEVICE_COMPILE__   // (buffer descriptors are a type of the device's alone)
+#ifdef __HIP_DEVICE_COMPILE__   // (the host has no such registers)
     constexpr int kThreads = WM * WN * kWave, TM = WM * MT * 16, TN = WN * NT * 16;
     constexpr int kARows = product_rows(TM, kThreads), kBRows = product_rows(TN, kThreads);   // that whole loads bring
     constexpr int kABytes = kARows * kStepBytes, kBBytes = kBRows * kStepBytes, kBAt = kStagesA * kABytes;
     constexpr int kALoads = kARows * 8 / kThreads, kBLoads = kBRows * 8 / kThreads;
     constexpr int kFetches = MT + NT, kProducts = MT * NT;
+    constexpr bool kTurned = E == kGradient;   // B's n elements are next to each other
+    constexpr bool kPanels = E == kSums || E == kGradient;
+    constexpr int kPanelSteps = 256 / kStep;
+    constexpr int kPieces = TN / 8, kTurns = TN / 16 < 16 ? TN / 16 : 16;   // 16-byte pieces of a row of TN; permutations
+    static_assert(!kTurned || kBRows == TN, "whole rows of k");
     typedef typename Mfma<T>::operand Operand;
     extern __shared__ __align__(16) char lds[];
 
@@ -163,7 +173,10 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
 
     // where this thread's 16-byte pieces come from (rows past the operand's last one read that one)
     const char *a_base = static_cast<const char *>(p.a) + ((int64_t)m0 * p.a_ld + (int64_t)from * kStep) * 2;
-    const char *b_base = static_cast<const char *>(p.b) + ((int64_t)n0 * p.b_ld + (int64_t)from * kStep) * 2;
+    const char *b_base = static_cast<const char *>(p.b);
+    if (kTurned) b_base += ((n0 >> 8) * p.d_panel + (n0 & 255)) * 2;
+    else if (kPanels) b_base += (int64_t)n0 * p.b_ld * 2;
+    else b_base += ((int64_t)n0 * p.b_ld + (int64_t)from * kStep) * 2;
     unsigned a_off[kALoads], b_off[kBLoads];
 #pragma unroll
     for (int i = 0; i < kALoads; ++i) {
@@ -172,20 +185,32 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
     }
 #pragma unroll
     for (int i = 0; i < kBLoads; ++i) {
-        const int c = tid + i * kThreads, row = c >> 3;
-        b_off[i] = (unsigned)min(row, p.n - 1 - n0) * (unsigned)(p.b_ld * 2) + (((c & 7) ^ ((row >> 1) & 7)) << 4);
+        const int c = tid + i * kThreads;
+        if constexpr (kTurned) {   // (a panel has whole tiles of 64 rows)
+            const int row = c / kPieces, piece = c % kPieces, turn = ((row & 3) + ((row >> 3) & 3) * 4) & (kTurns - 1);
+            b_off[i] = (unsigned)row * (unsigned)(p.b_ld * 2) + (((piece >> 1 ^ turn) * 2 + (piece & 1)) << 4);
+        } else {
+            const int row = c >> 3;
+            b_off[i] = (unsigned)min(row, p.n - 1 - n0) * (unsigned)(p.b_ld * 2) + (((c & 7) ^ ((row >> 1) & 7)) << 4);
+        }
     }
     // The next tiles to load.  Where operands are three arrays: the six products of them that are kept, the smallest first.
     int at_step = 0, at_product = 0;
-    __amdgpu_buffer_rsrc_t a_from, b_from;
+    i32x4 a_from, b_from;   // buffer descriptors
+    const auto descriptor = [](const char *base) {
+        const uint64_t at = (uint64_t)base;
+        return i32x4{(int)(uint32_t)at, (int)(uint32_t)(at >> 32) & 0xffff, -1, 0x00020000};
+    };
     const auto aim = [&]() {
         int64_t a_at = 0, b_at = 0;
+        if (kTurned) b_at = (int64_t)(from + at_step) * kStep * 512;
+        else if (kPanels) b_at = ((from + at_step) / kPanelSteps * p.d_panel + (from + at_step) % kPanelSteps * kStep) * 2;
         if (SPLIT) {
             a_at = ((0x021010 >> (4 * (5 - at_product))) & 15) * p.a_plane * 2;
-            b_at = ((0x201100 >> (4 * (5 - at_product))) & 15) * p.b_plane * 2;
+            b_at += ((0x201100 >> (4 * (5 - at_product))) & 15) * p.b_plane * 2;
         }
-        a_from = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(a_base + a_at), (short)0, -1, 0x00020000);
-        b_from = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(b_base + b_at), (short)0, -1, 0x00020000);
+        a_from = descriptor(a_base + a_at);
+        b_from = descriptor(b_base + b_at);
     };
     const auto next_step = [&]() {
         ++at_step;
@@ -193,17 +218,16 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
             at_step = 0;
             ++at_product;
             aim();
+        } else if (kPanels) {   // (beyond an offset's 32 bits)
+            aim();
         }
     };
+    const unsigned lds_at = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)lds + wave * (kWave * 16);
     const auto load_a = [&](int stage, int i) {
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(
-            a_from, (__attribute__((address_space(3))) void *)(lds + stage + wave * (kWave * 16) + i * kThreads * 16), 16,
-            a_off[i], at_step * kStepBytes, 0, 0);
+        load_to_lds(a_from, a_off[i], at_step * kStepBytes, lds_at + stage + i * kThreads * 16);
     };
     const auto load_b = [&](int stage, int i) {
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(
-            b_from, (__attribute__((address_space(3))) void *)(lds + kBAt + stage + wave * (kWave * 16) + i * kThreads * 16), 16,
-            b_off[i], at_step * kStepBytes, 0, 0);
+        load_to_lds(b_from, b_off[i], kPanels ? 0 : at_step * kStepBytes, lds_at + kBAt + stage + i * kThreads * 16);
     };
 
     f32x4 acc[MT][NT];
@@ -220,8 +244,22 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
     Operand fa[2][MT], fb[2][NT];   // of each half
     const char *a_read = lds + (wm * MT * 16 + row16) * kStepBytes, *b_read = lds + kBAt + (wn * NT * 16 + row16) * kStepBytes;
     const int piece[2] = {(part ^ turn) << 4, ((4 + part) ^ turn) << 4};
+    // turned: rows part * 8 + 0 .. 7 of the half; lane i of sixteen asks for 4 columns of row i / 4 and gets column i of 4 rows
+    const char *t_read = lds + kBAt + (part * 8 + (row16 >> 2)) * (TN * 2) + (row16 & 3) * 8;
+    const int t_turn = ((row16 >> 2) + part * 4) & (kTurns - 1);
     const auto fetch = [&](int a_stage, int b_stage, int half, int which) {
-        if (which < NT) fb[half][which] = *reinterpret_cast<const Operand *>(b_read + b_stage + piece[half] + which * 16 * kStepBytes);
+        if (which < NT) {
+            if constexpr (kTurned) {
+                typedef short s16x4 __attribute__((ext_vector_type(4)));
+                typedef __attribute__((address_space(3))) s16x4 lds16x4;
+                const char *at = t_read + b_stage + half * 32 * (TN * 2) + ((wn * NT + which) ^ t_turn) * 32;
+                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds16x4 *)at);
+                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds16x4 *)(at + 4 * (TN * 2)));
+                fb[half][which] = __builtin_bit_cast(Operand, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+            } else {
+                fb[half][which] = *reinterpret_cast<const Operand *>(b_read + b_stage + piece[half] + which * 16 * kStepBytes);
+            }
+        }
         else fa[half][which - NT] = *reinterpret_cast<const Operand *>(a_read + a_stage + piece[half] + (which - NT) * 16 * kStepBytes);
     };
     // Multiplies a half; meanwhile fetches the other half's fragments from the stages given and, in the first half,
@@ -327,44 +365,44 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
             p.parts[(int64_t)(n0 + i) * p.parts_ld + p.parts_first + tm] = make_float2(s.top, s.sum);
         }
     } else if constexpr (E == kDerivative) {
-        const float t_scale = *p.t_scale;
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
             const int n = n_lane + j * 16;
             const bool in = n < n_rows;
             const int label = in ? p.label[n] - p.m_first - m_lane : -1;
-            const float lse = in ? p.lse[n] : 0.0f, g = in ? p.row_grad[n] * t_scale : 0.0f;
+            const float lse = in ? p.lse[n] : 0.0f, g = in ? p.row_grad[n] : 0.0f;
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
+                const int m = m_lane + i * 16;
+                if (m >= p.d_cols) continue;   // (tiles of 192 and 160 rows may pass the last panel)
                 float d[4];
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const float q = __expf(acc[i][j][r] * p.scale - lse) - (label == i * 16 + r ? 1.0f : 0.0f);
-                    d[r] = in && m_lane + i * 16 + r < p.m ? q : 0.0f;
+                    d[r] = in && m + r < p.m ? q * g : 0.0f;
                 }
-                const int m = m_lane + i * 16, first = m - part * 4;   // `first` of the tile's sixteen rows
-                T *to_d = static_cast<T *>(p.d) + (int64_t)n * p.d_ld + m;
-                T *to_t = static_cast<T *>(p.d_t) + (int64_t)(first + part * 4 + (lane & 3)) * p.d_t_ld + (n & ~3);
+                T *to_d = static_cast<T *>(p.d) + (m >> 8) * p.d_panel + (int64_t)n * 256 + (m & 255);
                 if constexpr (SPLIT) {
-                    bf16 x[4][3], y[4][3];
+                    bf16 x[4][3];
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        split3(d[r] * p.d_scale, x[r]);
-                        split3(d[r] * g, y[r]);
-                    }
+                    for (int r = 0; r < 4; ++r) split3(d[r], x[r]);
 #pragma unroll
-                    for (int s = 0; s < 3; ++s) {
+                    for (int s = 0; s < 3; ++s)
                         *reinterpret_cast<uint2 *>(to_d + s * p.d_plane) =
                             make_uint2(pack2(x[0][s], x[1][s]), pack2(x[2][s], x[3][s]));
-                        *reinterpret_cast<uint2 *>(to_t + s * p.d_t_plane) =
-                            transpose4(pack2(y[0][s], y[1][s]), pack2(y[2][s], y[3][s]));
-                    }
                 } else {
-                    *reinterpret_cast<uint2 *>(to_d) = make_uint2(pack2((T)(d[0] * p.d_scale), (T)(d[1] * p.d_scale)),
-                                                                  pack2((T)(d[2] * p.d_scale), (T)(d[3] * p.d_scale)));
-                    *reinterpret_cast<uint2 *>(to_t) =
-                        transpose4(pack2((T)(d[0] * g), (T)(d[1] * g)), pack2((T)(d[2] * g), (T)(d[3] * g)));
+                    *reinterpret_cast<uint2 *>(to_d) = make_uint2(pack2((T)d[0], (T)d[1]), pack2((T)d[2], (T)d[3]));
                 }
+            }
+        }
+        // the next product reads whole steps of 64: what tiles of 160 rows leave of the last one is zero
+        if (TM % kStep != 0 && tm == tiles_m - 1) {
+            const int first = tiles_m * TM, end = (p.m + kStep - 1) / kStep * kStep;
+            for (int i = tid; i < TN * kStep; i += kThreads) {
+                const int m = first + i % kStep;
+                if (m < end)
+                    for (int s = 0; s < (SPLIT ? 3 : 1); ++s)
+                        static_cast<T *>(p.d)[s * p.d_plane + (m >> 8) * p.d_panel + (int64_t)(n0 + i / kStep) * 256 + (m & 255)] = (T)0.0f;
             }
         }
     } else if constexpr (E == kSums) {
@@ -382,7 +420,7 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
             }
         }
     } else {
-        const float alpha = p.scale / *p.t_scale;
+        const float alpha = p.scale * *p.out_scale;
         typedef O O4 __attribute__((ext_vector_type(4), aligned(sizeof(O))));
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
