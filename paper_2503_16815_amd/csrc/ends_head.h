@@ -5,7 +5,9 @@
 //
 // Each row's g is taken apart, g = f 2^e with 1 <= f < 2.  d is rounded to the type with f alone (in 16-bit floats times
 // 2^14, so that softmax values down to 1e-9 keep their bits); the powers of two come back exactly, in
-// dh by the row, in dw with the transposed hidden states relative to the largest.
+// dh by the row, in dw with the transposed hidden states relative to the largest.  What the rounding takes from the
+// label's entry, mostly the largest of its row, is added to dh afterwards in 32 bits.  Up to 64 positions, where dw is
+// bound by writing it, what the rounding takes from every entry is kept in a second array and multiplied too.
 //
 // Positions without a label are left out first: the others are packed together, so that they cost nothing.
 // The loss is one product whose tiles leave each position's softmax sum (largest logit, sum of
@@ -242,6 +244,10 @@ struct HiddenArgs {
     int n, hidden, splits;
     const int *at_of;
     const float *sums, *power;
+    const float *residual;          // times the label's row of the weights
+    const int *label;
+    const void *weight;
+    int64_t weight_stride;
     int64_t sums_ld, sums_split;
     float scale;
     void *out;
@@ -261,6 +267,20 @@ __global__ void __launch_bounds__(256) join_hidden_kernel(HiddenArgs a)
         if (at >= 0) {
             for (int s = 0; s < a.splits; ++s)
                 x += *reinterpret_cast<const f32x4 *>(a.sums + s * a.sums_split + (int64_t)at * a.sums_ld + c);
+            if (a.residual) {
+                const O *w = static_cast<const O *>(a.weight) + (int64_t)a.label[at] * a.weight_stride + c;
+                const float residual = a.residual[at];
+                typedef O O4 __attribute__((ext_vector_type(4), aligned(sizeof(O))));
+                if (c + 4 <= a.hidden) {
+                    const O4 v = *reinterpret_cast<const O4 *>(w);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[i] += residual * (float)v[i];
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (c + i < a.hidden) x[i] += residual * (float)w[i];
+                }
+            }
             x *= alpha;
         }
         if (c + 4 <= a.hidden) {
@@ -330,7 +350,7 @@ hipError_t allow_all()
 // One call's view of the scratch memory.
 struct Scratch {
     int32_t *count, *row_of, *at_of, *label;
-    float *lse, *grad, *z_label, *power, *most;
+    float *lse, *grad, *z_label, *power, *most, *residual;
     float2 *parts;
     char *hidden, *weight, *hidden_t, *weight_t, *d;
     float *sums;
@@ -347,6 +367,7 @@ struct Scratch {
         grad = lse + n;
         z_label = grad + n;
         power = z_label + n;
+        residual = power + n;
         parts = reinterpret_cast<float2 *>(s + plan.parts);
         hidden = s + plan.hidden;
         weight = s + plan.weight;
@@ -550,6 +571,7 @@ struct Head {
         const int products = kSplit ? 6 : 1;   // of the arrays that an operand is held in
         const int64_t logit_steps = k / kStep * products, weight_steps = up(n, kStep) / kStep * products;
         const int splits = splits_of(a.hidden, n, up(plan.piece < a.vocab ? plan.piece : a.vocab, kStep) / kStep * products, compute_units);
+        const int arrays = n <= kFew && !kSplit ? 2 : 1;
         int piece_number = 0;
         for (int first = 0; first < a.vocab && e == hipSuccess; first += plan.piece, ++piece_number) {
             const int rows = a.vocab - first < plan.piece ? a.vocab - first : plan.piece;
@@ -559,9 +581,11 @@ struct Head {
                 p.lse = s.lse;
                 p.row_grad = s.grad;
                 p.d = s.d;
+                p.residual = a.grad_hidden && !kSplit ? s.residual : nullptr;
                 p.d_cols = plan.piece;
                 p.d_panel = n_up * 256;
                 p.d_plane = n_up * plan.piece;
+                p.d_arrays = arrays;
                 if (e == hipSuccess) e = product<T, S, kDerivative, kSplit>(p, shape_of(rows, n, logit_steps, 1, compute_units), st);
             }
             if (e == hipSuccess && a.grad_weight) {
@@ -579,6 +603,8 @@ struct Head {
                 q.splits = 1;
                 q.scale = a.logit_scale / d_scale;
                 q.out_scale = s.most;
+                q.d_plane = n_up * plan.piece;
+                q.d_arrays = arrays;
                 q.add = a.accumulate;
                 q.out = static_cast<S *>(a.grad_weight) + (int64_t)first * a.grad_weight_stride;
                 q.out_ld = a.grad_weight_stride;
@@ -615,6 +641,12 @@ struct Head {
         j.at_of = s.at_of;
         j.sums = s.sums;
         j.power = s.power;
+        if (!kSplit) {
+            j.residual = s.residual;
+            j.label = s.label;
+            j.weight = a.weight;
+            j.weight_stride = a.weight_stride;
+        }
         j.sums_ld = sums_ld;
         j.sums_split = n_up * sums_ld;
         j.scale = a.logit_scale / d_scale;

@@ -53,8 +53,10 @@ struct ProductArgs {
     float *z_label;                  // [n]
     const float *lse;                // [n]
     const float *row_grad;           // [n], scaled into d's range
+    float *residual;                 // [n]: what rounding took from the label's derivative; or NULL
     void *d;                         // panels of 256 columns: [d_cols / 256][rows][256]
-    int64_t d_panel, d_plane;        // elements between panels, between the three arrays
+    int64_t d_panel, d_plane;        // elements between panels, between arrays
+    int d_arrays;                    // 16-bit types: 1, or 2 where a second array holds what rounding took (kGradient reads both)
     int d_cols;
     // kSums: sums[split][n][m]; kGradient: out[n][m]
     float *sums;
@@ -169,7 +171,7 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
 
     const int steps_all = (p.k_dev ? *p.k_dev + kStep - 1 : p.k) / kStep;
     const int from = (int)((int64_t)steps_all * blockIdx.y / p.splits), to = (int)((int64_t)steps_all * (blockIdx.y + 1) / p.splits);
-    const int steps = to - from, total = SPLIT ? steps * 6 : steps;
+    const int steps = to - from, total = SPLIT ? steps * 6 : kTurned ? steps * p.d_arrays : steps;
 
     // where this thread's 16-byte pieces come from (rows past the operand's last one read that one)
     const char *a_base = static_cast<const char *>(p.a) + ((int64_t)m0 * p.a_ld + (int64_t)from * kStep) * 2;
@@ -208,13 +210,15 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
         if (SPLIT) {
             a_at = ((0x021010 >> (4 * (5 - at_product))) & 15) * p.a_plane * 2;
             b_at += ((0x201100 >> (4 * (5 - at_product))) & 15) * p.b_plane * 2;
+        } else if (kTurned) {
+            b_at += at_product * p.d_plane * 2;
         }
         a_from = descriptor(a_base + a_at);
         b_from = descriptor(b_base + b_at);
     };
     const auto next_step = [&]() {
         ++at_step;
-        if (SPLIT && at_step == steps) {
+        if ((SPLIT || kTurned) && at_step == steps) {
             at_step = 0;
             ++at_product;
             aim();
@@ -371,6 +375,7 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
             const bool in = n < n_rows;
             const int label = in ? p.label[n] - p.m_first - m_lane : -1;
             const float lse = in ? p.lse[n] : 0.0f, g = in ? p.row_grad[n] : 0.0f;
+            float of_label = 0.0f;
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
                 const int m = m_lane + i * 16;
@@ -380,6 +385,7 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
                 for (int r = 0; r < 4; ++r) {
                     const float q = __expf(acc[i][j][r] * p.scale - lse) - (label == i * 16 + r ? 1.0f : 0.0f);
                     d[r] = in && m + r < p.m ? q * g : 0.0f;
+                    if (!SPLIT) of_label = label == i * 16 + r ? d[r] : of_label;
                 }
                 T *to_d = static_cast<T *>(p.d) + (m >> 8) * p.d_panel + (int64_t)n * 256 + (m & 255);
                 if constexpr (SPLIT) {
@@ -391,9 +397,19 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
                         *reinterpret_cast<uint2 *>(to_d + s * p.d_plane) =
                             make_uint2(pack2(x[0][s], x[1][s]), pack2(x[2][s], x[3][s]));
                 } else {
-                    *reinterpret_cast<uint2 *>(to_d) = make_uint2(pack2((T)d[0], (T)d[1]), pack2((T)d[2], (T)d[3]));
+                    T x[4];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) x[r] = (T)d[r];
+                    *reinterpret_cast<uint2 *>(to_d) = make_uint2(pack2(x[0], x[1]), pack2(x[2], x[3]));
+                    if (TN == 64 && p.d_arrays == 2) {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) x[r] = (T)(d[r] - (float)x[r]);
+                        *reinterpret_cast<uint2 *>(to_d + p.d_plane) = make_uint2(pack2(x[0], x[1]), pack2(x[2], x[3]));
+                    }
                 }
             }
+            if (!SPLIT && p.residual && label >= 0 && label < MT * 16 && (label & 15) < 4 && m_lane + label < p.m)
+                p.residual[n] = of_label - (float)(T)of_label;
         }
         // the next product reads whole steps of 64: what tiles of 160 rows leave of the last one is zero
         if (TM % kStep != 0 && tm == tiles_m - 1) {
@@ -401,7 +417,7 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
             for (int i = tid; i < TN * kStep; i += kThreads) {
                 const int m = first + i % kStep;
                 if (m < end)
-                    for (int s = 0; s < (SPLIT ? 3 : 1); ++s)
+                    for (int s = 0; s < (SPLIT ? 3 : p.d_arrays); ++s)
                         static_cast<T *>(p.d)[s * p.d_plane + (m >> 8) * p.d_panel + (int64_t)(n0 + i / kStep) * 256 + (m & 255)] = (T)0.0f;
             }
         }
