@@ -1,0 +1,78 @@
+"""The head on sizes that run each shape of its products' tiles (256 x 256, 192 x 256, 160 x 256, 256 x 128,
+128 x 128; 256 x 64 is what up to 64 positions run) in each of the four products, last tiles that pass the
+operands' ends among them.  Definitions and bounds as in test_gpu_ends.py."""
+import pytest
+
+from tests.test_gpu_ends import handle, head_definition, head_inputs, torch, within  # noqa: F401  (torch is a fixture)
+
+pytestmark = pytest.mark.gpu
+
+SIZES = [  # rows, vocab, hidden: what the 16-bit types run there
+    (777, 12297, 40),     # logits 256 x 256
+    (520, 13625, 40),     # logits 192 x 256
+    (520, 13069, 40),     # logits 160 x 256
+    (777, 10369, 40),     # logits 192 x 256, the last tile passes the last panel of 256 columns
+    (520, 13300, 40),     # logits 160 x 256, likewise
+    (70, 2033, 40),       # logits 256 x 128
+    (520, 10901, 320),    # weights' gradient 256 x 128
+    (70, 13110, 777),     # weights' gradient 256 x 256
+    (70, 9223, 1000),     # weights' gradient 192 x 256
+    (70, 9352, 777),      # weights' gradient 160 x 256
+    (1100, 8153, 130),    # hidden states' gradient 256 x 128, in 16 parts
+    (520, 4044, 1601),    # hidden states' gradient 192 x 256, in 8 parts
+    (520, 8150, 777),     # hidden states' gradient 160 x 256, in 16 parts
+    (4096, 600, 1024),    # hidden states' gradient without parts
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("rows,vocab,hidden", SIZES)
+def test_head_by_shape(torch, dtype, rows, vocab, hidden):  # noqa: F811
+    h, w, labels, row_grad = head_inputs(torch, rows + hidden, rows, vocab, hidden, 0, 0, 0.05, dtype)
+    valid, loss, lse, gh, gw = head_definition(torch, h, w, labels, 1.0, row_grad, dtype)
+    with handle(torch, ("head_loss", "head_grad"), dtype, rows, vocab, hidden) as e:
+        got_loss, got_lse = e.head_loss(h, w, labels)
+        within(got_loss, *loss, "loss")
+        within(got_lse, *lse, "lse")
+        got_gh, got_gw = e.head_grad(h, w, labels, got_lse, row_grad)
+        within(got_gh, *gh, "grad_hidden")
+        within(got_gw, *gw, "grad_weight")
+        again = e.head_grad(h, w, labels, got_lse, row_grad)
+        assert torch.equal(again[0], got_gh) and torch.equal(again[1], got_gw)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("rows,vocab,hidden", [(15, 8339, 173), (64, 3000, 256), (300, 5000, 320)])
+def test_roundings_of_the_derivative(torch, dtype, rows, vocab, hidden):  # noqa: F811
+    """The hidden states' gradient is as close as its own type allows, a half more at most, and so is the weights'
+    of up to 64 positions: rounding the derivative costs next to nothing there.  (The norm of a rounding of relative
+    size up to u, evenly spread, is u / sqrt(3) at most.)"""
+    h, w, labels, row_grad = head_inputs(torch, 9, rows, vocab, hidden, 0, 0, 0.0, dtype)
+    _, _, _, gh, gw = head_definition(torch, h, w, labels, 1.0, row_grad, dtype)
+    half = {"bf16": 2.0 ** -9, "f16": 2.0 ** -12}[dtype] * 2 / 3 ** 0.5
+    with handle(torch, ("head_loss", "head_grad"), dtype, rows, vocab, hidden) as e:
+        got = e.head_grad(h, w, labels, e.head_loss(h, w, labels)[1], row_grad)
+    off = [float((g.double() - x[0]).norm() / x[0].norm()) for g, x in zip(got, (gh, gw))]
+    assert off[0] <= 1.5 * half
+    if rows <= 64:
+        assert off[1] <= 1.5 * half
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_row_gradients_of_any_size(torch, dtype):  # noqa: F811
+    """Each row's factor is taken apart exactly: rows of very small and very large factors, zeros among them, have
+    gradients as exact as the others."""
+    rows, vocab, hidden = 200, 700, 96
+    h, w, labels, row_grad = head_inputs(torch, 77, rows, vocab, hidden, 0, 0, 0.0, dtype)
+    top = 6 if dtype == "f16" else 30
+    row_grad = row_grad * torch.pow(2.0, torch.randint(-top, top, (rows,), device="cuda").float())
+    row_grad[::17] = 0.0
+    row_grad[1::17] *= -1.0
+    _, _, _, gh, gw = head_definition(torch, h, w, labels, 1.0, row_grad, dtype)
+    with handle(torch, ("head_loss", "head_grad"), dtype, rows, vocab, hidden) as e:
+        got_gh, got_gw = e.head_grad(h, w, labels, e.head_loss(h, w, labels)[1], row_grad)
+        within(got_gh, *gh, "grad_hidden")
+        assert bool((got_gh[::17] == 0).all())
+        # (columns of the hidden states scaled below the largest factor's range add less than its rounding)
+        floor = float(row_grad.abs().max()) * (2.0 ** -38 if dtype == "f16" else 0.0) * rows * float(h.abs().max())
+        within(got_gw, gw[0], gw[1] + floor, "grad_weight")
