@@ -80,7 +80,7 @@ struct HeadPlan {
     int piece = 0;       // rows of the vocabulary at a time
     bool grad = false;
     // offsets into the scratch memory
-    int64_t ints, floats, hidden, weight, parts, hidden_t, weight_t, d, sums;
+    int64_t ints, floats, hidden, weight, parts, hidden_t, d, sums;
 };
 void head_plan(int dtype, int max_rows, int max_vocab, int max_hidden, bool grad, int compute_units, HeadPlan *plan);
 hipError_t head_prepare();   // kernel attributes, on the current device

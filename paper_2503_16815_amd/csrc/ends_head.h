@@ -352,7 +352,7 @@ struct Scratch {
     int32_t *count, *row_of, *at_of, *label;
     float *lse, *grad, *z_label, *power, *most, *residual;
     float2 *parts;
-    char *hidden, *weight, *hidden_t, *weight_t, *d;
+    char *hidden, *weight, *hidden_t, *d;
     float *sums;
     Scratch(const HeadPlan &plan, void *scratch)
     {
@@ -372,7 +372,6 @@ struct Scratch {
         hidden = s + plan.hidden;
         weight = s + plan.weight;
         hidden_t = s + plan.hidden_t;
-        weight_t = s + plan.weight_t;
         d = s + plan.d;
         sums = reinterpret_cast<float *>(s + plan.sums);
     }
@@ -426,27 +425,20 @@ struct Head {
 
     // the operands of the logits of the vocabulary's rows `first` .. `first` + `rows` - 1
     static hipError_t logits(const HeadPlan &plan, const Scratch &s, const void *weight, int64_t stride, int first, int rows, int n,
-                             int hidden, float scale, bool transposed, ProductArgs *p, hipStream_t st)
+                             int hidden, float scale, ProductArgs *p, hipStream_t st)
     {
         const int64_t k = up(hidden, kStep);
         const S *from = static_cast<const S *>(weight) + (int64_t)first * stride;
         const bool direct = !kSplit && in_place(weight, stride, hidden);
-        if (!direct || transposed) {
+        if (!direct) {
             PackArgs w{};
             w.src = from;
             w.src_stride = stride;
             w.rows = rows;
             w.cols = hidden;
-            if (!direct) {
-                w.out = s.weight;
-                w.out_ld = k;
-                w.out_plane = (int64_t)plan.piece * k;
-            }
-            if (transposed) {
-                w.out_t = s.weight_t;
-                w.t_ld = plan.piece;
-                w.t_plane = (int64_t)plan.piece * k;
-            }
+            w.out = s.weight;
+            w.out_ld = k;
+            w.out_plane = (int64_t)plan.piece * k;
             const hipError_t e = pack(w, (int)up(rows, kTile), st);
             if (e != hipSuccess) return e;
         }
@@ -500,7 +492,7 @@ struct Head {
         for (int first = 0; first < a.vocab && e == hipSuccess; first += piece) {
             const int rows = a.vocab - first < piece ? a.vocab - first : piece;
             ProductArgs p;
-            e = logits(plan, s, a.weight, a.weight_stride, first, rows, n, a.hidden, a.logit_scale, false, &p, st);
+            e = logits(plan, s, a.weight, a.weight_stride, first, rows, n, a.hidden, a.logit_scale, &p, st);
             p.parts = s.parts;
             p.parts_ld = tiles;
             p.parts_first = parts_first;
@@ -577,7 +569,7 @@ struct Head {
             const int rows = a.vocab - first < plan.piece ? a.vocab - first : plan.piece;
             ProductArgs p{};
             if (n > 0) {
-                e = logits(plan, s, a.weight, a.weight_stride, first, rows, n, a.hidden, a.logit_scale, a.grad_hidden != nullptr, &p, st);
+                e = logits(plan, s, a.weight, a.weight_stride, first, rows, n, a.hidden, a.logit_scale, &p, st);
                 p.lse = s.lse;
                 p.row_grad = s.grad;
                 p.d = s.d;
@@ -614,9 +606,10 @@ struct Head {
                 e = hipEventRecord(static_cast<hipEvent_t>(a.piece_events[piece_number]), st);
             if (e == hipSuccess && a.grad_hidden && n > 0) {
                 ProductArgs q{};
-                q.a = s.weight_t;
-                q.a_ld = plan.piece;
-                q.a_plane = (int64_t)plan.piece * k;
+                q.a = p.a;   // (as the logits' product read it)
+                q.a_ld = p.a_ld;
+                q.a_plane = p.a_plane;
+                q.a_rows = rows;
                 q.b = s.d;
                 q.b_ld = 256;
                 q.b_plane = n_up * plan.piece;

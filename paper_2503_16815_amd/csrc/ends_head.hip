@@ -61,7 +61,6 @@ void head_plan(int dtype, int max_rows, int max_vocab, int max_hidden, bool grad
     plan->parts = take(n * ((max_vocab + 127) / 128) * 8);
     if (grad) {
         plan->hidden_t = take(plan->planes * n * k * 2);
-        plan->weight_t = take(plan->planes * piece * k * 2);
         plan->d = take(plan->planes * (n < 2 * kTile ? 2 * kTile : n) * piece * 2);   // (room for a second array of few positions)
         // one array of sums, or several where splits * tiles stays within twice the compute units
         const int64_t one = n * up(max_hidden, 4), split = 2 * (int64_t)compute_units * kTile * kTile;

@@ -1,7 +1,7 @@
 // The matrix product that the head's operators are made of:  C[m][n] = sum_k A[m][k] B[n][k], 16-bit
 // elements, 32-bit sums.  Both operands have their k elements next to each other, or B its n
-// elements (kGradient, which so reads the derivative as it was written).  What happens to C is the
-// epilogue's business (it is never stored as it is): softmax statistics, the loss's derivative,
+// elements (kGradient, which so reads the derivative as it was written) or A its m elements (kSums, which so reads
+// the weights as they are).  What happens to C is the epilogue's business (it is never stored as it is): softmax statistics, the loss's derivative,
 // or a sum into a gradient.
 //
 // A workgroup of eight wavefronts owns a tile of C.  Both operands' tiles go from memory to LDS without
@@ -14,9 +14,9 @@
 // LDS, which have no register to wait for: the compiler would let every transposing LDS read wait for all of them.
 //
 // The 16-byte pieces of a row are permuted by the row's number, so that the sixteen rows that a wavefront
-// reads together lie in different banks (no bank conflicts counted).  A B with its n elements next to each other
-// lies in LDS as it came, a row of TN elements to each k; the transposing LDS read gives every lane four k of its
-// column, from four rows whose 32-byte pieces are permuted by the row's number too.
+// reads together lie in different banks (no bank conflicts counted).  An A or B with its m or n elements
+// next to each other lies in LDS as it came, a row of TM or TN elements to each k; the transposing LDS read gives every
+// lane four k of its column, from four rows whose 32-byte pieces are permuted by the row's number too.
 //
 // The derivative lies in panels of 256 columns, so that a step of either product that reads it finds it in one
 // stretch of memory.
@@ -42,6 +42,7 @@ struct ProductArgs {
     int m, n;                        // rows of a and of b
     const int *n_dev;                // rows of b that count, where the device knows it, or NULL
     int k;                           // a multiple of kStep
+    int a_rows;                      // kSums: the k that a has rows of
     const int *k_dev;                // or the rows of another operand, rounded up to kStep
     int splits;                      // of k, over blockIdx.y
     float scale;
@@ -134,6 +135,14 @@ __device__ __forceinline__ void load_to_lds(i32x4 from, unsigned offset, int at,
                  : "memory", "m0");
 }
 
+// What the 32-byte pieces of row k are permuted by (an exclusive or with their number) in a tile of `wide` elements
+// to a row: rows 0 .. 3 and 8 .. 11 of any sixteen, which a transposing read visits at a time, so fill all 64 banks.
+constexpr __host__ __device__ int turn_of(int wide, int k)
+{
+    const int low = k & 3, high = (k >> 3) & 3;
+    return wide == 160 ? high & 1 : wide == 192 ? low ^ (high & 1) : (low + high * 4) & ((wide / 16 < 16 ? wide / 16 : 16) - 1);
+}
+
 template <int H> struct HalfOf {
     static constexpr int value = H;
 };
@@ -150,9 +159,10 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
     constexpr int kALoads = kARows * 8 / kThreads, kBLoads = kBRows * 8 / kThreads;
     constexpr int kFetches = MT + NT, kProducts = MT * NT;
     constexpr bool kTurned = E == kGradient;   // B's n elements are next to each other
+    constexpr bool kTurnedA = E == kSums;      // A's m elements are
     constexpr bool kPanels = E == kSums || E == kGradient;
     constexpr int kPanelSteps = 256 / kStep;
-    constexpr int kPieces = TN / 8, kTurns = TN / 16 < 16 ? TN / 16 : 16;   // 16-byte pieces of a row of TN; permutations
+    constexpr int kPieces = TN / 8, kPiecesA = TM / 8;   // 16-byte pieces of a row of TN, of TM
     static_assert(!kTurned || kBRows == TN, "whole rows of k");
     typedef typename Mfma<T>::operand Operand;
     extern __shared__ __align__(16) char lds[];
@@ -174,22 +184,30 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
     const int steps = to - from, total = SPLIT ? steps * 6 : kTurned ? steps * p.d_arrays : steps;
 
     // where this thread's 16-byte pieces come from (rows past the operand's last one read that one)
-    const char *a_base = static_cast<const char *>(p.a) + ((int64_t)m0 * p.a_ld + (int64_t)from * kStep) * 2;
+    const char *a_base = static_cast<const char *>(p.a) + (kTurnedA ? (int64_t)m0 : (int64_t)m0 * p.a_ld + (int64_t)from * kStep) * 2;
     const char *b_base = static_cast<const char *>(p.b);
     if (kTurned) b_base += ((n0 >> 8) * p.d_panel + (n0 & 255)) * 2;
     else if (kPanels) b_base += (int64_t)n0 * p.b_ld * 2;
     else b_base += ((int64_t)n0 * p.b_ld + (int64_t)from * kStep) * 2;
     unsigned a_off[kALoads], b_off[kBLoads];
+    const auto turned_a = [&](int rows) {   // of a step that a has `rows` rows for; and columns past its last piece read that one
+#pragma unroll
+        for (int i = 0; i < kALoads; ++i) {
+            const int c = tid + i * kThreads, row = c / kPiecesA, piece = c % kPiecesA;
+            const int at = (piece >> 1 ^ turn_of(TM, row)) * 2 + (piece & 1);
+            a_off[i] = (unsigned)min(row, rows - 1) * (unsigned)(p.a_ld * 2) + (min(at, ((p.m + 7) >> 3) - 1 - (m0 >> 3)) << 4);
+        }
+    };
 #pragma unroll
     for (int i = 0; i < kALoads; ++i) {
         const int c = tid + i * kThreads, row = c >> 3;
-        a_off[i] = (unsigned)min(row, p.m - 1 - m0) * (unsigned)(p.a_ld * 2) + (((c & 7) ^ ((row >> 1) & 7)) << 4);
+        if (!kTurnedA) a_off[i] = (unsigned)min(row, p.m - 1 - m0) * (unsigned)(p.a_ld * 2) + (((c & 7) ^ ((row >> 1) & 7)) << 4);
     }
 #pragma unroll
     for (int i = 0; i < kBLoads; ++i) {
         const int c = tid + i * kThreads;
         if constexpr (kTurned) {   // (a panel has whole tiles of 64 rows)
-            const int row = c / kPieces, piece = c % kPieces, turn = ((row & 3) + ((row >> 3) & 3) * 4) & (kTurns - 1);
+            const int row = c / kPieces, piece = c % kPieces, turn = turn_of(TN, row);
             b_off[i] = (unsigned)row * (unsigned)(p.b_ld * 2) + (((piece >> 1 ^ turn) * 2 + (piece & 1)) << 4);
         } else {
             const int row = c >> 3;
@@ -201,14 +219,20 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
     i32x4 a_from, b_from;   // buffer descriptors
     const auto descriptor = [](const char *base) {
         const uint64_t at = (uint64_t)base;
-        return i32x4{(int)(uint32_t)at, (int)(uint32_t)(at >> 32) & 0xffff, -1, 0x00020000};
+        return i32x4{__builtin_amdgcn_readfirstlane((int)(uint32_t)at),
+                     __builtin_amdgcn_readfirstlane((int)(uint32_t)(at >> 32) & 0xffff), -1, 0x00020000};
     };
     const auto aim = [&]() {
         int64_t a_at = 0, b_at = 0;
         if (kTurned) b_at = (int64_t)(from + at_step) * kStep * 512;
         else if (kPanels) b_at = ((from + at_step) / kPanelSteps * p.d_panel + (from + at_step) % kPanelSteps * kStep) * 2;
+        if (kTurnedA) {
+            const int k = (from + at_step) * kStep;
+            a_at = (int64_t)k * p.a_ld * 2;
+            if (at_step == 0 || k + kStep > p.a_rows) turned_a(min(p.a_rows - k, kStep));
+        }
         if (SPLIT) {
-            a_at = ((0x021010 >> (4 * (5 - at_product))) & 15) * p.a_plane * 2;
+            a_at += ((0x021010 >> (4 * (5 - at_product))) & 15) * p.a_plane * 2;
             b_at += ((0x201100 >> (4 * (5 - at_product))) & 15) * p.b_plane * 2;
         } else if (kTurned) {
             b_at += at_product * p.d_plane * 2;
@@ -228,7 +252,7 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
     };
     const unsigned lds_at = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)lds + wave * (kWave * 16);
     const auto load_a = [&](int stage, int i) {
-        load_to_lds(a_from, a_off[i], at_step * kStepBytes, lds_at + stage + i * kThreads * 16);
+        load_to_lds(a_from, a_off[i], kTurnedA ? 0 : at_step * kStepBytes, lds_at + stage + i * kThreads * 16);
     };
     const auto load_b = [&](int stage, int i) {
         load_to_lds(b_from, b_off[i], kPanels ? 0 : at_step * kStepBytes, lds_at + kBAt + stage + i * kThreads * 16);
@@ -249,22 +273,28 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
     const char *a_read = lds + (wm * MT * 16 + row16) * kStepBytes, *b_read = lds + kBAt + (wn * NT * 16 + row16) * kStepBytes;
     const int piece[2] = {(part ^ turn) << 4, ((4 + part) ^ turn) << 4};
     // turned: rows part * 8 + 0 .. 7 of the half; lane i of sixteen asks for 4 columns of row i / 4 and gets column i of 4 rows
-    const char *t_read = lds + kBAt + (part * 8 + (row16 >> 2)) * (TN * 2) + (row16 & 3) * 8;
-    const int t_turn = ((row16 >> 2) + part * 4) & (kTurns - 1);
+    const int t_row = part * 8 + (row16 >> 2), t_turn = turn_of(TN, t_row), t_turn_a = turn_of(TM, t_row);
+    const char *t_read = lds + kBAt + t_row * (TN * 2) + (row16 & 3) * 8, *t_read_a = lds + t_row * (TM * 2) + (row16 & 3) * 8;
+    const auto turned = [](const char *at, int row_bytes) {
+        typedef short s16x4 __attribute__((ext_vector_type(4)));
+        typedef __attribute__((address_space(3))) s16x4 lds16x4;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds16x4 *)at);
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds16x4 *)(at + 4 * row_bytes));
+        return __builtin_bit_cast(Operand, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
     const auto fetch = [&](int a_stage, int b_stage, int half, int which) {
         if (which < NT) {
-            if constexpr (kTurned) {
-                typedef short s16x4 __attribute__((ext_vector_type(4)));
-                typedef __attribute__((address_space(3))) s16x4 lds16x4;
-                const char *at = t_read + b_stage + half * 32 * (TN * 2) + ((wn * NT + which) ^ t_turn) * 32;
-                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds16x4 *)at);
-                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds16x4 *)(at + 4 * (TN * 2)));
-                fb[half][which] = __builtin_bit_cast(Operand, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-            } else {
+            if constexpr (kTurned)
+                fb[half][which] = turned(t_read + b_stage + half * 32 * (TN * 2) + ((wn * NT + which) ^ t_turn) * 32, TN * 2);
+            else
                 fb[half][which] = *reinterpret_cast<const Operand *>(b_read + b_stage + piece[half] + which * 16 * kStepBytes);
-            }
+        } else {
+            const int i = which - NT;
+            if constexpr (kTurnedA)
+                fa[half][i] = turned(t_read_a + a_stage + half * 32 * (TM * 2) + ((wm * MT + i) ^ t_turn_a) * 32, TM * 2);
+            else
+                fa[half][i] = *reinterpret_cast<const Operand *>(a_read + a_stage + piece[half] + i * 16 * kStepBytes);
         }
-        else fa[half][which - NT] = *reinterpret_cast<const Operand *>(a_read + a_stage + piece[half] + (which - NT) * 16 * kStepBytes);
     };
     // Multiplies a half; meanwhile fetches the other half's fragments from the stages given and, in the first half,
     // loads A's next tile to `to_stage`, in the second B's.

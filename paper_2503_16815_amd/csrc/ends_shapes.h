@@ -7,7 +7,7 @@ namespace deft {
 constexpr int kStep = 64;            // elements of k per step of a product
 constexpr int kTile = 256;
 constexpr int64_t kPieceBytes = (int64_t)3 << 27;    // of d
-constexpr int64_t kWeightBytes = (int64_t)1 << 28;   // of a piece's rows, packed or transposed
+constexpr int64_t kWeightBytes = (int64_t)1 << 28;   // of a piece's rows, packed
 constexpr int kMaxSplits = 16;
 constexpr int kFew = 64;                             // positions that a tile of 64 holds
 

@@ -76,3 +76,24 @@ def test_row_gradients_of_any_size(torch, dtype):  # noqa: F811
         # (columns of the hidden states scaled below the largest factor's range add less than its rounding)
         floor = float(row_grad.abs().max()) * (2.0 ** -38 if dtype == "f16" else 0.0) * rows * float(h.abs().max())
         within(got_gw, gw[0], gw[1] + floor, "grad_weight")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("rows,vocab,hidden,pad", [(300, 1001, 128, 0), (300, 1001, 128, 64), (520, 8150, 832, 0), (520, 4044, 1600, 64),
+                                                   (70, 2033, 64, 64), (64, 517, 192, 0), (300, 1001, 100, 28)])
+def test_what_lies_behind_the_table(torch, dtype, rows, vocab, hidden, pad):  # noqa: F811
+    """Rows behind the table's last one and what lies between its rows are read by no product, whatever they hold."""
+    h, w, labels, row_grad = head_inputs(torch, rows + vocab, rows, vocab, hidden, 0, 0, 0.05, dtype)
+    _, _, _, gh, gw = head_definition(torch, h, w, labels, 1.0, row_grad, dtype)
+    around = torch.full((vocab + 300, hidden + pad), float("nan"), dtype=w.dtype, device=w.device)
+    around[:vocab, :hidden] = w
+    inside = around[:vocab, :hidden]
+    with handle(torch, ("head_loss", "head_grad"), dtype, rows, vocab, hidden) as e:
+        loss, lse = e.head_loss(h, w, labels)
+        plain = e.head_grad(h, w, labels, lse, row_grad)
+        got_loss, got_lse = e.head_loss(h, inside, labels)
+        got = e.head_grad(h, inside, labels, got_lse, row_grad)
+        within(plain[0], *gh, "grad_hidden")
+        within(plain[1], *gw, "grad_weight")
+        for a, b in zip((loss, lse, *plain), (got_loss, got_lse, *got)):
+            assert torch.equal(a, b)
