@@ -407,35 +407,58 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
             const float lse = in ? p.lse[n] : 0.0f, g = in ? p.row_grad[n] : 0.0f;
             float of_label = 0.0f;
 #pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                const int m = m_lane + i * 16;
-                if (m >= p.d_cols) continue;   // (tiles of 192 and 160 rows may pass the last panel)
-                float d[4];
+            for (int i = 0; i < MT; i += 2) {
+                constexpr int kBoth = SPLIT ? 3 : TN == 64 ? 2 : 1;   // arrays (16-bit types: two of up to 64 positions)
+                uint2 x[2][kBoth] = {};
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float q = __expf(acc[i][j][r] * p.scale - lse) - (label == i * 16 + r ? 1.0f : 0.0f);
-                    d[r] = in && m + r < p.m ? q * g : 0.0f;
-                    if (!SPLIT) of_label = label == i * 16 + r ? d[r] : of_label;
-                }
-                T *to_d = static_cast<T *>(p.d) + (m >> 8) * p.d_panel + (int64_t)n * 256 + (m & 255);
-                if constexpr (SPLIT) {
-                    bf16 x[4][3];
+                for (int h = 0; h < 2; ++h) {
+                    if (i + h == MT) break;
+                    float d[4];
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) split3(d[r], x[r]);
-#pragma unroll
-                    for (int s = 0; s < 3; ++s)
-                        *reinterpret_cast<uint2 *>(to_d + s * p.d_plane) =
-                            make_uint2(pack2(x[0][s], x[1][s]), pack2(x[2][s], x[3][s]));
-                } else {
-                    T x[4];
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) x[r] = (T)d[r];
-                    *reinterpret_cast<uint2 *>(to_d) = make_uint2(pack2(x[0], x[1]), pack2(x[2], x[3]));
-                    if (TN == 64 && p.d_arrays == 2) {
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) x[r] = (T)(d[r] - (float)x[r]);
-                        *reinterpret_cast<uint2 *>(to_d + p.d_plane) = make_uint2(pack2(x[0], x[1]), pack2(x[2], x[3]));
+                    for (int r = 0; r < 4; ++r) {
+                        const int at = (i + h) * 16 + r;
+                        const float q = __expf(acc[i + h][j][r] * p.scale - lse) - (label == at ? 1.0f : 0.0f);
+                        d[r] = in && m_lane + at < p.m ? q * g : 0.0f;
+                        if (!SPLIT) of_label = label == at ? d[r] : of_label;
                     }
+                    if constexpr (SPLIT) {
+                        bf16 y[4][3];
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) split3(d[r], y[r]);
+#pragma unroll
+                        for (int s = 0; s < 3; ++s) x[h][s] = make_uint2(pack2(y[0][s], y[1][s]), pack2(y[2][s], y[3][s]));
+                    } else {
+                        T y[4];
+#pragma unroll
+                        for (int s = 0; s < kBoth; ++s) {   // (the second: what rounding took)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) {
+                                y[r] = (T)d[r];
+                                d[r] -= (float)y[r];
+                            }
+                            x[h][s] = make_uint2(pack2(y[0], y[1]), pack2(y[2], y[3]));
+                        }
+                    }
+                }
+                // Neighbouring sixteens of lanes exchange a part, so that each has eight elements of one tile of 16 rows to
+                // store (of the last of an odd number of such tiles: four).  Four each: 77 us for 70 (1003 x 30011 x 1021 f16).
+                const bool whole = i + 1 < MT;
+                const int m = m_lane + i * 16 + (whole ? (part & 1) * 16 + (part >> 1) * 8 - part * 4 : 0);
+                if (whole) {
+#pragma unroll
+                    for (int s = 0; s < kBoth; ++s) {
+                        const auto first = __builtin_amdgcn_permlane16_swap(x[0][s].x, x[1][s].x, false, false);
+                        const auto second = __builtin_amdgcn_permlane16_swap(x[0][s].y, x[1][s].y, false, false);
+                        x[0][s] = make_uint2(first[0], second[0]);
+                        x[1][s] = make_uint2(first[1], second[1]);
+                    }
+                }
+                if (m >= p.d_cols) continue;   // (tiles of 192 and 160 rows may pass the last panel)
+                T *to_d = static_cast<T *>(p.d) + (m >> 8) * p.d_panel + (int64_t)n * 256 + (m & 255);
+#pragma unroll
+                for (int s = 0; s < kBoth; ++s) {
+                    if (whole) *reinterpret_cast<uint4 *>(to_d + s * p.d_plane) = make_uint4(x[0][s].x, x[0][s].y, x[1][s].x, x[1][s].y);
+                    else *reinterpret_cast<uint2 *>(to_d + s * p.d_plane) = x[0][s];
                 }
             }
             if (!SPLIT && p.residual && label >= 0 && label < MT * 16 && (label & 15) < 4 && m_lane + label < p.m)
