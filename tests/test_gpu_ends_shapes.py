@@ -1,9 +1,10 @@
-"""The head on sizes that run each shape of its products' tiles (256 x 256, 192 x 256, 160 x 256, 256 x 128,
+"""Operators by the variants that their sizes choose.  The head on sizes that run each shape of its products' tiles (256 x 256, 192 x 256, 160 x 256, 256 x 128,
 128 x 128; 256 x 64 is what up to 64 positions run) in each of the four products, last tiles that pass the
 operands' ends among them.  Definitions and bounds as in test_gpu_ends.py."""
 import pytest
 
-from tests.test_gpu_ends import handle, head_definition, head_inputs, torch, within  # noqa: F401  (torch is a fixture)
+from tests.test_gpu_ends import (distill_definition, generator, handle, head_definition, head_inputs, matrix,  # noqa: F401
+                                 torch, within)  # (torch is a fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -97,3 +98,23 @@ def test_what_lies_behind_the_table(torch, dtype, rows, vocab, hidden, pad):  # 
         within(plain[1], *gw, "grad_weight")
         for a, b in zip((loss, lse, *plain), (got_loss, got_lse, *got)):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("rows,vocab,top_k", [(2100, 1003, 8), (900, 12345, 20), (600, 30001, 8), (600, 50257, 33), (300, 70001, 600)])
+def test_distillation_from_row_to_row(torch, dtype, rows, vocab, top_k):  # noqa: F811
+    """More rows than workgroups run at once, so that each goes on from row to row; rows without an entry among them."""
+    g = generator(torch, rows + vocab)
+    z = matrix(torch, g, rows, vocab, dtype, 2.5, 1, 0)
+    index = torch.rand((rows, 4 * top_k), generator=g, device="cuda").argsort(1)[:, :top_k].int() * (vocab // (4 * top_k))
+    value = torch.randn((rows, top_k), generator=g, device="cuda") * 3
+    index[torch.rand((rows, top_k), generator=g, device="cuda") < 0.2] = -1
+    index[3::7] = -1
+    z[3::7] = float("nan")
+    row_grad = torch.rand(rows, generator=g, device="cuda") * 2
+    valid, loss, grad = distill_definition(torch, z, index, value, 2.0, row_grad, dtype)
+    with handle(torch, "distill", dtype, rows, vocab, 0, top_k) as e:
+        within(e.distill(z, index, value, 2.0), *loss, "loss")
+        got, got_grad = e.distill_grad(z, index, value, row_grad, 2.0)
+        within(got, *loss, "loss with gradient")
+        within(got_grad, *grad, "grad_logits")
