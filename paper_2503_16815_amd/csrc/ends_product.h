@@ -22,7 +22,13 @@
 // stretch of memory.
 //
 // Tiles are dealt out so that the workgroups of an XCD work on neighbouring ones, four wide: 12 rows of tiles
-// come into its L2 for 32 workgroups instead of 33 (131072 x 8192 x 4096: 890 to 1110 TFLOP/s by itself).
+// come into its L2 for 32 workgroups instead of 33 (131072 x 8192 x 4096: 890 to 1110 TFLOP/s by itself).  Where k is
+// split, an XCD has all tiles of a part before the next part's: what they read is theirs alone (hidden states' gradient of
+// 1024 positions, 8209 rows of 640 in 32 bits, 16 parts: 65 us; with each part's tiles on all XCDs 87, 272 MB fetched).
+//
+// Bound by the matrix units at the clock that the card keeps under them.  8192 positions, 50257 rows of 1600 elements, bf16, all
+// pieces: logits with softmax sums 1165 us (1130 TFLOP/s), derivative 1290 (1020: 824 MB are written), weights' gradient and
+// hidden states' gradient 1200 each (1100).
 //
 // 32-bit operands come as three 16-bit arrays whose sum they are (8 bits of the significand in
 // each); the six products of those arrays that matter at 24 bits are summed one after the other.
@@ -44,7 +50,7 @@ struct ProductArgs {
     int k;                           // a multiple of kStep
     int a_rows;                      // kSums: the k that a has rows of
     const int *k_dev;                // or the rows of another operand, rounded up to kStep
-    int splits;                      // of k, over blockIdx.y
+    int splits;                      // of k
     float scale;
     // kSoftmax, kDerivative: m counts rows of the vocabulary from m_first on, n packed positions
     int m_first;
@@ -170,17 +176,18 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / WN, wn = wave % WN;
     const int n_rows = p.n_dev ? *p.n_dev : p.n;
     const int tiles_m = (p.m + TM - 1) / TM, tiles_n = (n_rows + TN - 1) / TN;
-    // workgroup b runs on XCD b % 8; each XCD has an equal share of the tiles, in groups four wide
-    const int tiles = tiles_m * tiles_n, xcd = blockIdx.x & 7, share = tiles >> 3, more = tiles & 7;
+    // workgroup b runs on XCD b % 8; each XCD has an equal share of the parts' tiles, in groups four wide
+    const int tiles = tiles_m * tiles_n, items = tiles * p.splits, xcd = blockIdx.x & 7, share = items >> 3, more = items & 7;
     if ((int)(blockIdx.x >> 3) >= share + (xcd < more ? 1 : 0)) return;
-    const int tile = (int)(blockIdx.x >> 3) + xcd * share + (xcd < more ? xcd : more);
+    const int item = (int)(blockIdx.x >> 3) + xcd * share + (xcd < more ? xcd : more);
+    const int split = item / tiles, tile = item - split * tiles;
     const int group = tile / (tiles_m * 4), in_group = tile - group * tiles_m * 4;
     const int wide = min(tiles_n - group * 4, 4);
     const int tm = in_group / wide, tn = group * 4 + in_group - tm * wide;
     const int m0 = tm * TM, n0 = tn * TN;
 
     const int steps_all = (p.k_dev ? *p.k_dev + kStep - 1 : p.k) / kStep;
-    const int from = (int)((int64_t)steps_all * blockIdx.y / p.splits), to = (int)((int64_t)steps_all * (blockIdx.y + 1) / p.splits);
+    const int from = (int)((int64_t)steps_all * split / p.splits), to = (int)((int64_t)steps_all * (split + 1) / p.splits);
     const int steps = to - from, total = SPLIT ? steps * 6 : kTurned ? steps * p.d_arrays : steps;
 
     // where this thread's 16-byte pieces come from (rows past the operand's last one read that one)
@@ -441,7 +448,7 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
                     }
                 }
                 // Neighbouring sixteens of lanes exchange a part, so that each has eight elements of one tile of 16 rows to
-                // store (of the last of an odd number of such tiles: four).  Four each: 77 us for 70 (1003 x 30011 x 1021 f16).
+                // store (of the last of an odd number of such tiles: four).  Four each: 75 us for 70 (1003 x 30011 x 1021 f16).
                 const bool whole = i + 1 < MT;
                 const int m = m_lane + i * 16 + (whole ? (part & 1) * 16 + (part >> 1) * 8 - part * 4 : 0);
                 if (whole) {
@@ -475,7 +482,7 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
             }
         }
     } else if constexpr (E == kSums) {
-        float *sums = p.sums + blockIdx.y * p.sums_split;
+        float *sums = p.sums + split * p.sums_split;
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
             const int n = n_lane + j * 16;
