@@ -153,7 +153,8 @@ deft_status_t deft_head_loss(deft_ends_t *h, const deft_head_loss_t *a);
  * Rows without a valid label have a zero row in grad_hidden and no part in grad_weight.
  * Either gradient may be NULL, not both.
  * In 16-bit types d is rounded to the type before the two products, as their matrix instructions
- * take it (for 16-bit floats scaled by a power of two into their range); in 32 bits it is not.
+ * take it (scaled so that a row of the largest row_grad fills the range up to a power of two, and
+ * 16-bit floats into their range); in 32 bits it is not.
  */
 typedef struct {
     int32_t n_rows;

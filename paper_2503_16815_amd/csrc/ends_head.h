@@ -5,7 +5,9 @@
 //
 // Each row's g is taken apart, g = f 2^e with 1 <= f < 2.  d is rounded to the type with f alone (in 16-bit floats times
 // 2^14, so that softmax values down to 1e-9 keep their bits); the powers of two come back exactly, in
-// dh by the row, in dw with the transposed hidden states relative to the largest.  What the rounding takes from the
+// dh by the row, in dw with the transposed hidden states relative to the largest.  All f are divided by that of the largest
+// g, and both sums multiplied by it: where all g are one number, a mean's, the labels' entries, the largest of
+// d, so lie just below a power of two, where rounding takes least of them (up to half of what it takes just above).  What the rounding takes from the
 // label's entry, mostly the largest of its row, is added to dh afterwards in 32 bits.  Up to 64 positions, where dw is
 // bound by writing it, what the rounding takes from every entry is kept in a second array and multiplied too.
 //
@@ -35,8 +37,10 @@ struct RowsArgs {
     float *loss, *lse_out;          // the loss call: zeros for the others
     const float *lse, *row_grad;    // the gradient call: packed too
     int32_t *count, *row_of, *at_of, *label;   // [1], [n] each
-    float *lse_packed, *grad_packed, *power, *most;   // [n]: f times d_scale and 2^e; [1]: the largest power
+    float *lse_packed, *grad_packed, *power;   // [n]: f times d_scale and 2^e
+    float *most;                    // [4]: of the largest g, with f or, where d is kept in 32 bits, 1: 2^e, 1 / f, f 2^e, f
     float d_scale;
+    int whole;                      // d is kept in 32 bits
 };
 
 __global__ void __launch_bounds__(1024) rows_kernel(RowsArgs a)
@@ -74,7 +78,7 @@ __global__ void __launch_bounds__(1024) rows_kernel(RowsArgs a)
                     a.lse_packed[at] = a.lse[i];
                     a.grad_packed[at] = (taken ? ldexpf(g, -e) : g) * a.d_scale;
                     a.power[at] = taken ? ldexpf(1.0f, e) : 1.0f;
-                    if (taken) top = fmaxf(top, ldexpf(1.0f, e));
+                    if (taken) top = fmaxf(top, size);
                 }
             } else if (a.loss) {
                 a.loss[i] = 0.0f;
@@ -90,7 +94,14 @@ __global__ void __launch_bounds__(1024) rows_kernel(RowsArgs a)
     if (tid == 0) {
         *a.count = base;
         for (int w = 0; w < 16; ++w) top = fmaxf(top, wave_top[w]);
-        if (a.most) *a.most = top > 0.0f ? top : 1.0f;
+        if (a.most) {
+            const int e = top > 0.0f ? max(ilogbf(top), -100) : 0;
+            const float f = ldexpf(top, -e), by = a.whole || f < 1.0f ? 1.0f : f, power = ldexpf(1.0f, e);
+            a.most[0] = power;
+            a.most[1] = 1.0f / by;
+            a.most[2] = power * by;
+            a.most[3] = by;
+        }
     }
 }
 
@@ -291,7 +302,7 @@ __global__ void __launch_bounds__(256) join_few_kernel(FewArgs a)
 struct HiddenArgs {
     int n, hidden, splits;
     const int *at_of;
-    const float *sums, *power;
+    const float *sums, *power, *factor;
     const float *residual;          // times the label's row of the weights
     const int *label;
     const void *weight;
@@ -313,7 +324,7 @@ __global__ void __launch_bounds__(256) join_hidden_kernel(HiddenArgs a)
     if (row >= a.n) return;
     const int at = a.at_of[row];
     O *out = static_cast<O *>(a.out) + (int64_t)row * a.out_stride;
-    const float alpha = at >= 0 ? a.power[at] * a.scale : 0.0f;
+    const float alpha = at >= 0 ? a.power[at] * a.scale * *a.factor : 0.0f;
     for (int c = (blockIdx.y * kWave + lane) * 4; c < a.hidden; c += gridDim.y * kWave * 4) {
         f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
         if (at >= 0) {
@@ -620,6 +631,7 @@ struct Head {
         r.power = s.power;
         r.most = s.most;
         r.d_scale = d_scale;
+        r.whole = kSplit;
         rows_kernel<<<1, 1024, 0, st>>>(r);
         hipError_t e = hipGetLastError();
         if (e == hipSuccess && n > 0) e = positions(s, a.hidden_states, a.hidden_stride, n, a.hidden, true, a.grad_weight != nullptr, st);
@@ -636,6 +648,7 @@ struct Head {
                 e = logits(plan, s, a.weight, a.weight_stride, first, rows, n, a.hidden, a.logit_scale, &p, st);
                 p.lse = s.lse;
                 p.row_grad = s.grad;
+                p.row_factor = s.most + 1;
                 p.d = s.d;
                 p.residual = a.grad_hidden && !kSplit ? s.residual : nullptr;
                 p.d_cols = plan.piece;
@@ -658,7 +671,7 @@ struct Head {
                 q.k_dev = s.count;
                 q.splits = 1;
                 q.scale = a.logit_scale / d_scale;
-                q.out_scale = s.most;
+                q.out_scale = s.most + 2;
                 q.d_plane = n_up * plan.piece;
                 q.d_arrays = arrays;
                 q.add = a.accumulate;
@@ -698,6 +711,7 @@ struct Head {
         j.at_of = s.at_of;
         j.sums = s.sums;
         j.power = s.power;
+        j.factor = s.most + 3;
         if (!kSplit) {
             j.residual = s.residual;
             j.label = s.label;

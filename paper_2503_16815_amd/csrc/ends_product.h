@@ -59,7 +59,7 @@ struct ProductArgs {
     int parts_ld, parts_first;       // the number of the first tile's part
     float *z_label;                  // [n]
     const float *lse;                // [n]
-    const float *row_grad;           // [n], scaled into d's range
+    const float *row_grad, *row_factor;   // [n] and [1]: their product is scaled into d's range
     float *residual;                 // [n]: what rounding took from the label's derivative; or NULL
     void *d;                         // panels of 256 columns: [d_cols / 256][rows][256]
     int64_t d_panel, d_plane;        // elements between panels, between arrays
@@ -411,7 +411,7 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
             const int n = n_lane + j * 16;
             const bool in = n < n_rows;
             const int label = in ? p.label[n] - p.m_first - m_lane : -1;
-            const float lse = in ? p.lse[n] : 0.0f, g = in ? p.row_grad[n] : 0.0f;
+            const float lse = in ? p.lse[n] : 0.0f, g = in ? p.row_grad[n] * *p.row_factor : 0.0f;
             float of_label = 0.0f;
 #pragma unroll
             for (int i = 0; i < MT; i += 2) {

@@ -118,3 +118,24 @@ def test_distillation_from_row_to_row(torch, dtype, rows, vocab, top_k):  # noqa
         got, got_grad = e.distill_grad(z, index, value, row_grad, 2.0)
         within(got, *loss, "loss with gradient")
         within(got_grad, *grad, "grad_logits")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("factor", [1.02, 1.4, 1.98])
+def test_roundings_where_all_rows_count_alike(torch, dtype, factor):  # noqa: F811
+    """The weights' gradient of a mean: the labels' entries are rounded just below a power of two, whatever the mean's
+    factor.  (In the norm, with h the largest relative rounding / sqrt(3): the output's own 0.74 h, mantissas spread
+    evenly by their logarithm; the labels' entries 0.5 h / 0.9 for probabilities below 0.1; together 0.92 h, and a
+    seventh more at most.)"""
+    rows, vocab, hidden = 700, 9001, 320
+    h, w, labels, _ = head_inputs(torch, 21, rows, vocab, hidden, 0, 0, 0.0, dtype)
+    h = (h * 0.25).to(h.dtype)
+    row_grad = torch.full((rows,), factor / 4, device="cuda")
+    _, _, _, _, gw = head_definition(torch, h, w, labels, 1.0, row_grad, dtype)
+    at_most = {"bf16": 2.0 ** -8, "f16": 2.0 ** -11}[dtype] / 3 ** 0.5
+    with handle(torch, ("head_loss", "head_grad"), dtype, rows, vocab, hidden) as e:
+        lse = e.head_loss(h, w, labels)[1]
+        z = (h.double() * w[labels.long()].double()).sum(1)
+        assert float((z - lse.double()).exp().max()) < 0.1
+        got = e.head_grad(h, w, labels, lse, row_grad)[1]
+    assert float((got.double() - gw[0]).norm() / gw[0].norm()) <= 1.05 * at_most
