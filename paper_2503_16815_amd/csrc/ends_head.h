@@ -330,12 +330,12 @@ __global__ void __launch_bounds__(256) join_hidden_kernel(HiddenArgs a)
         if (at >= 0) {
             const float *sums = a.sums + (int64_t)at * a.sums_ld + c;
             int s = 0;
-            for (; s + 4 <= a.splits; s += 4) {   // (four loads under way)
-                f32x4 y[4];
+            for (; s + 8 <= a.splits; s += 8) {   // (eight loads under way)
+                f32x4 y[8];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) y[i] = *reinterpret_cast<const f32x4 *>(sums + (s + i) * a.sums_split);
+                for (int i = 0; i < 8; ++i) y[i] = *reinterpret_cast<const f32x4 *>(sums + (s + i) * a.sums_split);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) x += y[i];
+                for (int i = 0; i < 8; ++i) x += y[i];
             }
             for (; s < a.splits; ++s) x += *reinterpret_cast<const f32x4 *>(sums + s * a.sums_split);
             if (a.residual) {

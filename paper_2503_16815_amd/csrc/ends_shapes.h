@@ -8,7 +8,7 @@ constexpr int kStep = 64;            // elements of k per step of a product
 constexpr int kTile = 256;
 constexpr int64_t kPieceBytes = (int64_t)3 << 27;    // of d
 constexpr int64_t kWeightBytes = (int64_t)1 << 28;   // of a piece's rows, packed
-constexpr int kMaxSplits = 16;
+constexpr int kMaxSplits = 128;
 constexpr int kFew = 64;                             // positions that a tile of 64 holds
 
 inline int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
