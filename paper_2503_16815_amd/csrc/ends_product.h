@@ -31,7 +31,8 @@
 // hidden states' gradient 1200 each (1100).
 //
 // 32-bit operands come as three 16-bit arrays whose sum they are (8 bits of the significand in
-// each); the six products of those arrays that matter at 24 bits are summed one after the other.
+// each); the six products of those arrays that matter at 24 bits are summed one after the other, step by step (loss
+// and gradients of 2 x 91134 x 305 334 us, 40 x 30000 x 512 176; all steps of one product before the next 357 and 191).
 #pragma once
 #include "ends_shapes.h"
 
@@ -236,7 +237,7 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
         if (kTurnedA) {
             const int k = (from + at_step) * kStep;
             a_at = (int64_t)k * p.a_ld * 2;
-            if (at_step == 0 || k + kStep > p.a_rows) turned_a(min(p.a_rows - k, kStep));
+            if ((at_step == 0 && at_product == 0) || k + kStep > p.a_rows) turned_a(min(p.a_rows - k, kStep));
         }
         if (SPLIT) {
             a_at += ((0x021010 >> (4 * (5 - at_product))) & 15) * p.a_plane * 2;
@@ -248,8 +249,16 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
         b_from = descriptor(b_base + b_at);
     };
     const auto next_step = [&]() {
+        if (SPLIT) {   // (a step's products one after the other: its tiles are in the XCD's L2 then)
+            if (++at_product == 6) {
+                at_product = 0;
+                ++at_step;
+            }
+            aim();
+            return;
+        }
         ++at_step;
-        if ((SPLIT || kTurned) && at_step == steps) {
+        if (kTurned && at_step == steps) {
             at_step = 0;
             ++at_product;
             aim();
