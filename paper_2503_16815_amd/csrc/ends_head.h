@@ -19,7 +19,7 @@
 // units where positions are many, and by reading w where they are few.
 //
 // Loss and gradient: 8192 x 50257 x 1600 bf16 4.6 ms (1150 TFLOP/s over four products; a library's single product of that size
-// 1100), 8192 x 131072 x 4096 bf16 25.5 ms (1380; 1530), 1024 x 8209 x 640 f32 0.33 ms.  Loss alone of one position of 50257 x
+// 1100), 8192 x 131072 x 4096 bf16 25.5 ms (1380; 1530), 1024 x 8209 x 640 f32 0.30 ms.  Loss alone of one position of 50257 x
 // 1600 35 us, of 13 of 131072 x 4096 176 us (6.1 TB/s).
 #pragma once
 #include "ends_product.h"

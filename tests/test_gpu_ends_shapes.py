@@ -139,3 +139,20 @@ def test_roundings_where_all_rows_count_alike(torch, dtype, factor):  # noqa: F8
         assert float((z - lse.double()).exp().max()) < 0.1
         got = e.head_grad(h, w, labels, lse, row_grad)[1]
     assert float((got.double() - gw[0]).norm() / gw[0].norm()) <= 1.05 * at_most
+
+
+@pytest.mark.parametrize("rows", [1, 16, 17, 32, 33, 64])
+@pytest.mark.parametrize("vocab,hidden,pad,shift", [(1, 1, 0, 0), (127, 15, 1, 1), (129, 63, 0, 1), (1000, 64, 3, 0), (4099, 131, 0, 0), (300, 1600, 2, 3)])
+def test_few_logits_in_32_bits(torch, rows, vocab, hidden, pad, shift):  # noqa: F811
+    """The loss of up to 64 positions at the edges of its tiles; what lies between and behind the rows is never read."""
+    h, w, labels, row_grad = head_inputs(torch, rows * 7 + vocab, rows, vocab, hidden, pad, shift, 0.0, "f32")
+    if rows > 2:
+        labels[1] = -1
+    valid, loss, lse, _, _ = head_definition(torch, h, w, labels, 0.7, row_grad, "f32")
+    around = torch.full((vocab + 200, hidden + 5), float("nan"), device="cuda")
+    around[:vocab, :hidden] = w
+    h[~valid] = float("nan")
+    with handle(torch, ("head_loss",), "f32", rows, vocab, hidden) as e:
+        got = e.head_loss(h, around[:vocab, :hidden], labels, 0.7)
+        within(got[0], *loss, "loss")
+        within(got[1], *lse, "lse")
