@@ -72,12 +72,14 @@ __global__ void __launch_bounds__(1024) rows_kernel(RowsArgs a)
                 a.label[at] = label;
                 if (a.row_grad) {
                     const float g = a.row_grad[i], size = fabsf(g);
-                    // (zero, infinity and NaN stay as they are; the smallest numbers have f < 1)
-                    const int e = size > 0.0f && size < INFINITY ? max(ilogbf(size), -100) : -100;
-                    const bool taken = e > -100 || (size > 0.0f && size < INFINITY);
+                    // (Zero, infinity and NaN stay as they are, the smallest numbers have f < 1.  A zero's power is the least that
+                    // there is, so that its hidden states are never scaled up, past their type's range; that of infinity and NaN is
+                    // above all others: their hidden states stay as they are.)
+                    const bool taken = size > 0.0f && size < INFINITY;
+                    const int e = taken ? max(ilogbf(size), -100) : size == 0.0f ? -100 : 127;
                     a.lse_packed[at] = a.lse[i];
                     a.grad_packed[at] = (taken ? ldexpf(g, -e) : g) * a.d_scale;
-                    a.power[at] = taken ? ldexpf(1.0f, e) : 1.0f;
+                    a.power[at] = ldexpf(1.0f, e);
                     if (taken) top = fmaxf(top, size);
                 }
             } else if (a.loss) {
@@ -160,7 +162,7 @@ __global__ void __launch_bounds__(256) pack_kernel(PackArgs a)
 #pragma unroll
         for (int p = 0; p < P; ++p)
             *reinterpret_cast<T8 *>(static_cast<T *>(a.out) + p * a.out_plane + (int64_t)row * a.out_ld + col) = y[p];
-        const float scale = a.power && row < rows ? a.power[row] / *a.most : 1.0f;   // (a power of two up to 1, or 0)
+        const float scale = a.power && row < rows ? fminf(a.power[row] / *a.most, 1.0f) : 1.0f;   // (a power of two)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             if constexpr (P == 3) {
