@@ -154,7 +154,10 @@ deft_status_t deft_head_loss(deft_ends_t *h, const deft_head_loss_t *a);
  * Either gradient may be NULL, not both.
  * In 16-bit types d is rounded to the type before the two products, as their matrix instructions
  * take it (scaled so that a row of the largest row_grad fills the range up to a power of two, and
- * 16-bit floats into their range); in 32 bits it is not.
+ * 16-bit floats into their range); in 32 bits it is not.  In 16-bit floats a position whose row_grad
+ * is 2^-r of the largest has errors of its own beside, where values pass below the type's range:
+ * row_grad 2^(s - 38) in an element of d, and in grad_weight d 2^(t - 25) for each of its hidden
+ * states' elements, with s = r - 4, from 0 to 12, and t = r - s.
  */
 typedef struct {
     int32_t n_rows;

@@ -4,8 +4,11 @@
 //   d = g (exp(z - lse) - [v == label]);  dh = s d w;  dw = s d^T h
 //
 // Each row's g is taken apart, g = f 2^e with 1 <= f < 2.  d is rounded to the type with f alone (in 16-bit floats times
-// 2^14, so that softmax values down to 1e-9 keep their bits); the powers of two come back exactly, in
-// dh by the row, in dw with the transposed hidden states relative to the largest.  All f are divided by that of the largest
+// 2^14, so that softmax values down to 1e-9 keep their bits); the powers of two come back in
+// dh by the row, in dw with the transposed hidden states relative to the largest: exactly, but for what a 16-bit float cannot hold.
+// There a power 2^-r of the largest is divided: four octaves to the hidden states, the next twelve to d, whose row in dh
+// gets them back exactly too, the rest to the hidden states.  (All of it in the hidden states, r = 20, an element of 0.0137 was 0.)
+// All f are divided by that of the largest
 // g, and both sums multiplied by it: where all g are one number, a mean's, the labels' entries, the largest of
 // d, so lie just below a power of two, where rounding takes least of them (up to half of what it takes just above).  What the rounding takes from the
 // label's entry, mostly the largest of its row, is added to dh afterwards in 32 bits.  Up to 64 positions, where dw is
@@ -37,19 +40,20 @@ struct RowsArgs {
     float *loss, *lse_out;          // the loss call: zeros for the others
     const float *lse, *row_grad;    // the gradient call: packed too
     int32_t *count, *row_of, *at_of, *label;   // [1], [n] each
-    float *lse_packed, *grad_packed, *power;   // [n]: f times d_scale and 2^e
+    float *lse_packed, *grad_packed, *power;   // [n]: f times d_scale and 2^e (divided: f d_scale 2^-s and 2^(e + s))
     float *most;                    // [4]: of the largest g, with f or, where d is kept in 32 bits, 1: 2^e, 1 / f, f 2^e, f
     float d_scale;
     int whole;                      // d is kept in 32 bits
+    int divided;                    // d and the hidden states are 16-bit floats
 };
 
 __global__ void __launch_bounds__(1024) rows_kernel(RowsArgs a)
 {
     __shared__ int wave_count[16];
-    __shared__ float wave_top[16];
+    __shared__ float wave_top[16], wave_low[16];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     int base = 0;
-    float top = 0.0f;
+    float top = 0.0f, low = INFINITY;
     for (int first = 0; first < a.n; first += 1024) {
         const int i = first + tid;
         const int label = i < a.n ? a.labels[i] : -1;
@@ -80,7 +84,7 @@ __global__ void __launch_bounds__(1024) rows_kernel(RowsArgs a)
                     a.lse_packed[at] = a.lse[i];
                     a.grad_packed[at] = (taken ? ldexpf(g, -e) : g) * a.d_scale;
                     a.power[at] = ldexpf(1.0f, e);
-                    if (taken) top = fmaxf(top, size);
+                    if (taken) top = fmaxf(top, size), low = fminf(low, size);
                 }
             } else if (a.loss) {
                 a.loss[i] = 0.0f;
@@ -91,19 +95,33 @@ __global__ void __launch_bounds__(1024) rows_kernel(RowsArgs a)
         __syncthreads();
     }
     top = wave_max(top);
-    if (lane == 0) wave_top[wave] = top;
+    low = -wave_max(-low);
+    if (lane == 0) {
+        wave_top[wave] = top;
+        wave_low[wave] = low;
+    }
     __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 16; ++w) {
+        top = fmaxf(top, wave_top[w]);
+        low = fminf(low, wave_low[w]);
+    }
+    const int e = top > 0.0f ? max(ilogbf(top), -100) : 0;
     if (tid == 0) {
         *a.count = base;
-        for (int w = 0; w < 16; ++w) top = fmaxf(top, wave_top[w]);
         if (a.most) {
-            const int e = top > 0.0f ? max(ilogbf(top), -100) : 0;
             const float f = ldexpf(top, -e), by = a.whole || f < 1.0f ? 1.0f : f, power = ldexpf(1.0f, e);
             a.most[0] = power;
             a.most[1] = 1.0f / by;
             a.most[2] = power * by;
             a.most[3] = by;
         }
+    }
+    if (!a.divided || low >= ldexpf(1.0f, e - 4)) return;
+    for (int at = tid; at < base; at += 1024) {
+        const int own = ilogbf(a.power[at]), s = min(max(e - own - 4, 0), 12);
+        a.grad_packed[at] = ldexpf(a.grad_packed[at], -s);
+        a.power[at] = ldexpf(1.0f, own + s);
     }
 }
 
@@ -766,6 +784,7 @@ struct Head {
         r.most = s.most;
         r.d_scale = d_scale;
         r.whole = kSplit;
+        r.divided = kHalf;
         rows_kernel<<<1, 1024, 0, st>>>(r);
         hipError_t e = hipGetLastError();
         if (e == hipSuccess && n > 0) e = positions(s, a.hidden_states, a.hidden_stride, n, a.hidden, true, a.grad_weight != nullptr, st);
