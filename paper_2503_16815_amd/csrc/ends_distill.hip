@@ -74,9 +74,9 @@ __global__ void __launch_bounds__(kThreads) distill_kernel(deft_distill_t a)
     top = block_max(top, room);
     float part = 0.0f;
     for (int k = tid; k < a.top_k; k += kThreads)
-        if (index[k] >= 0) part += __expf(prob[k] - top);
+        if (prob[k] != -INFINITY) part += __expf(prob[k] - top);   // (a NaN, which is no maximum, makes the sum one)
     const float total = block_sum(part, room);
-    bad |= kept && top == -INFINITY && total != total;
+    bad |= kept && total == 0.0f;                                  // all of them -infinity
 
     // the student's softmax
     SoftSum s = {-INFINITY, 0.0f};
