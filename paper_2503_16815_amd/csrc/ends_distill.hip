@@ -9,13 +9,30 @@
 // 16 bytes of the next row are asked for as soon as the gradient of the present row's has been stored,
 // so memory is idle only during the row's two reductions.  Rows that are longer are read once more.
 // With the gradient, 64 entries of the teacher a row: 4096 x 50257 bf16 177 us, 4.7 TB/s read and written (a large copy 5.1);
-// 8192 x 131071 f16 978 us, 4.4 TB/s; rows too long for registers, 1024 x 200000 f32: 497 us, 4.9 TB/s with the second read.
+// 8192 x 131071 f16 966 us, 4.4 TB/s; rows too long for registers, 1024 x 200000 f32: 492 us, 5.0 TB/s with the second read.
+// The loss alone: 4096 x 50257 bf16 91 us, 4.5 TB/s; 8192 x 131071 f16 449 us, 4.8 TB/s.
 #include "ends.h"
 
 namespace deft {
 namespace {
 
 constexpr int kThreads = 512, kWaves = kThreads / kWave;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+
+// Exponentials are powers of two of (z - largest) log2(e) / T: the difference first, so that neither what a row's
+// logits have in common nor a logit at the end of the type's range costs any bits.  (-infinity less the lowest
+// value, which stands for a largest one where there is none, gives 0, and a NaN stays one.)
+constexpr float kLowest = -3.402823466e38f;
+
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// of running sums whose largest values are logits as they are, kLowest or more (NaN is in the sums alone); c = log2(e) / T
+__device__ __forceinline__ SoftSum soft_join2(SoftSum a, SoftSum b, float c)
+{
+    const float less = exp2_of(-fabsf((a.top - b.top) * c));
+    const bool first = a.top >= b.top;
+    return {first ? a.top : b.top, __builtin_fmaf(first ? b.sum : a.sum, less, first ? a.sum : b.sum)};
+}
 
 // Sum over the workgroup; every thread gets it.  `room` is read until the next barrier.
 __device__ __forceinline__ float block_sum(float x, float *room)
@@ -54,7 +71,7 @@ __global__ void __launch_bounds__(kThreads) distill_kernel(deft_distill_t a)
     const int64_t row = blockIdx.x;
     const T *z = static_cast<const T *>(a.logits) + row * a.logits_stride;
     T *grad = a.grad_logits ? static_cast<T *>(a.grad_logits) + row * a.grad_stride : nullptr;
-    const float inv_t = 1.0f / a.temperature;
+    const float c = kLog2e / a.temperature;
 
     // the teacher's entries
     int kept = 0, bad = 0;
@@ -62,7 +79,7 @@ __global__ void __launch_bounds__(kThreads) distill_kernel(deft_distill_t a)
     for (int k = tid; k < a.top_k; k += kThreads) {
         const int v = a.teacher_index[row * a.top_k + k];
         const bool in = v >= 0 && v < a.vocab;
-        const float u = in ? a.teacher_logit[row * a.top_k + k] * inv_t : -INFINITY;
+        const float u = in ? a.teacher_logit[row * a.top_k + k] : -INFINITY;
         index[k] = in ? v : -1;
         prob[k] = u;
         kept |= v != -1;
@@ -74,45 +91,43 @@ __global__ void __launch_bounds__(kThreads) distill_kernel(deft_distill_t a)
     top = block_max(top, room);
     float part = 0.0f;
     for (int k = tid; k < a.top_k; k += kThreads)
-        if (prob[k] != -INFINITY) part += __expf(prob[k] - top);   // (a NaN, which is no maximum, makes the sum one)
+        if (prob[k] != -INFINITY) part += exp2_of((prob[k] - top) * c);   // (a NaN, which is no maximum, makes the sum one)
     const float total = block_sum(part, room);
-    bad |= kept && total == 0.0f;                                  // all of them -infinity
+    bad |= kept && total == 0.0f;                                         // all of them -infinity
 
     // the student's softmax
-    SoftSum s = {-INFINITY, 0.0f};
+    SoftSum s = {kLowest, 0.0f};
     if (kept && !bad) {
         const int whole = a.vocab / n * n;
         for (int at = tid * n; at < whole; at += kThreads * n) {
             const typename Vec<T>::type x = *reinterpret_cast<const typename Vec<T>::type *>(z + at);
-            SoftSum b = {-INFINITY, 0.0f};
+            SoftSum b = {kLowest, 0.0f};
 #pragma unroll
-            for (int i = 0; i < n; ++i) b.top = fmaxf(b.top, (float)x[i] * inv_t);
-            if (b.top == -INFINITY) b.top = -3.0e38f;   // (exp(-inf - that) is 0, and NaN stays NaN)
+            for (int i = 0; i < n; ++i) b.top = fmaxf(b.top, (float)x[i]);
 #pragma unroll
-            for (int i = 0; i < n; ++i) b.sum += __expf((float)x[i] * inv_t - b.top);
-            s = soft_join(s, b);
+            for (int i = 0; i < n; ++i) b.sum += exp2_of(((float)x[i] - b.top) * c);
+            s = soft_join2(s, b, c);
         }
         for (int at = whole + tid; at < a.vocab; at += kThreads) {
-            const float x = (float)z[at] * inv_t;
-            const SoftSum b = {x == -INFINITY ? -3.0e38f : x, x == -INFINITY ? 0.0f : __expf(x - x)};
-            s = soft_join(s, b);
+            const float x = (float)z[at], at_least = fmaxf(x, kLowest);
+            s = soft_join2(s, SoftSum{at_least, exp2_of((x - at_least) * c)}, c);
         }
     }
     const float most = block_max(s.top, room);
-    const float sum = block_sum(s.sum == 0.0f ? 0.0f : s.sum * __expf(s.top - most), room);
+    const float sum = block_sum(s.sum == 0.0f ? 0.0f : s.sum * exp2_of((s.top - most) * c), room);
     bad |= kept && sum == 0.0f;
     const bool ok = kept && !bad;
-    const float lse = most + __logf(sum);
+    const float log_sum = __log2f(sum);
     if (tid == 0 && a.status) a.status[row] = bad ? DEFT_ERR_INVALID_ARG : DEFT_OK;
 
     // loss; prob becomes the teacher's probabilities
     float by = 0.0f;
     if (ok) {
-        const float log_total = __logf(total);
+        const float logs = (__log2f(total) - log_sum) * kLn2;
         for (int k = tid; k < a.top_k; k += kThreads) {
             const float u = prob[k] - top;
-            const float p = index[k] >= 0 ? __expf(u) / total : 0.0f;
-            if (p > 0.0f || p != p) by += p * (u - log_total - ((float)z[index[k]] * inv_t - lse));
+            const float p = index[k] >= 0 ? exp2_of(u * c) / total : 0.0f;
+            if (p > 0.0f || p != p) by += p * (u / a.temperature - ((float)z[index[k]] - most) / a.temperature - logs);
             prob[k] = p;
         }
     }
@@ -127,7 +142,7 @@ __global__ void __launch_bounds__(kThreads) distill_kernel(deft_distill_t a)
         if (index[k] < 0) continue;
         float p = 0.0f;
         for (int o = 0; o < a.top_k; ++o) p += index[o] == index[k] ? prob[o] : 0.0f;
-        fixed[j & 1] = g * (__expf((float)z[index[k]] * inv_t - lse) - p);
+        fixed[j & 1] = g * (exp2_of(__builtin_fmaf((float)z[index[k]] - most, c, -log_sum)) - p);
     }
     __syncthreads();
     const int whole = a.vocab / n * n;
@@ -136,12 +151,12 @@ __global__ void __launch_bounds__(kThreads) distill_kernel(deft_distill_t a)
         if (ok) {
             x = *reinterpret_cast<const typename Vec<T>::type *>(z + at);
 #pragma unroll
-            for (int i = 0; i < n; ++i) x[i] = (T)(g * __expf((float)x[i] * inv_t - lse));
+            for (int i = 0; i < n; ++i) x[i] = (T)(g * exp2_of(__builtin_fmaf((float)x[i] - most, c, -log_sum)));
         }
         *reinterpret_cast<typename Vec<T>::type *>(grad + at) = x;
     }
     for (int at = whole + tid; at < a.vocab; at += kThreads)
-        grad[at] = ok ? (T)(g * __expf((float)z[at] * inv_t - lse)) : (T)0.0f;
+        grad[at] = ok ? (T)(g * exp2_of(__builtin_fmaf((float)z[at] - most, c, -log_sum))) : (T)0.0f;
     __syncthreads();
     for (int k = tid, j = 0; k < a.top_k && ok; k += kThreads, ++j)
         if (index[k] >= 0) grad[index[k]] = (T)fixed[j & 1];
@@ -150,19 +165,25 @@ __global__ void __launch_bounds__(kThreads) distill_kernel(deft_distill_t a)
 // ---- rows that stay in registers -------------------------------------------------------------
 
 constexpr int kMarkBits = 1 << 17;   // of the map that shows whether an index occurs twice
-constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
-__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+// (w - top) c as one instruction, fma(w, c, -product), which leaves the product's rounding in every power alike:
+// they are 2^rounding times as large.  Not where that could be far from 1, nor where the product is not finite.  (The
+// difference first is an instruction more, for 16-bit floats, whose widening the fma takes with it, two.  Loss alone of 8192 x 131071
+// f16: 449 us so, 489 with the difference; with the gradient 966 and 990; 4096 x 8000 bf16 28.3 and 28.9.)
+struct Scaled {
+    float product, rounding;
+    bool far;
+    __device__ __forceinline__ Scaled(float top, float c) : product(top * c)
+    {
+        far = !(fabsf(product) < 0x1p20f);
+        rounding = __builtin_fmaf(top, c, -product);
+    }
+    __device__ __forceinline__ float shrink() const { return exp2_of(-rounding); }
+};
 
-__device__ __forceinline__ SoftSum soft_join2(SoftSum a, SoftSum b)   // with powers of two
+__device__ __forceinline__ SoftSum wave_join2(SoftSum s, int from, float c)
 {
-    const float top = fmaxf(a.top, b.top);
-    return {top, (a.top == top ? a.sum : a.sum * exp2_of(a.top - top)) + (b.top == top ? b.sum : b.sum * exp2_of(b.top - top))};
-}
-
-__device__ __forceinline__ SoftSum wave_join2(SoftSum s, int from)
-{
-    for (int d = from; d > 0; d >>= 1) s = soft_join2(s, SoftSum{__shfl_xor(s.top, d), __shfl_xor(s.sum, d)});
+    for (int d = from; d > 0; d >>= 1) s = soft_join2(s, SoftSum{__shfl_xor(s.top, d), __shfl_xor(s.sum, d)}, c);
     return s;
 }
 
@@ -188,9 +209,19 @@ __device__ __forceinline__ void widen(i32x4 v, float (&x)[8], f16)
     for (int i = 0; i < 8; ++i) x[i] = (float)h[i];
 }
 
+template <typename T, int N>
+__device__ __forceinline__ void narrow(const float (&x)[N], i32x4 &v, T)
+{
+    typedef T V __attribute__((ext_vector_type(N)));
+    V y;
+#pragma unroll
+    for (int i = 0; i < N; ++i) y[i] = (T)x[i];
+    v = __builtin_bit_cast(i32x4, y);
+}
+
 // Each lane holds NV vectors of the row, kRowThreads vectors apart, from the row's first 16-byte boundary on (a wave's
 // vectors that straddle such boundaries cost a tenth of the time), and one of the elements before and behind them;
-// the k-th lane the teacher's k-th entry.  Logits are scaled by log2(e) / T as they are used.
+// the k-th lane the teacher's k-th entry.
 template <typename T, int kRowThreads, int NV, bool GRAD>
 __global__ void __launch_bounds__(kRowThreads, 4) distill_row_kernel(deft_distill_t a)
 {
@@ -204,7 +235,7 @@ __global__ void __launch_bounds__(kRowThreads, 4) distill_row_kernel(deft_distil
     __shared__ int same_index[kRowThreads];
     __shared__ float same_prob[kRowThreads];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const float c = kLog2e / a.temperature;
+    const float c = kLog2e / a.temperature, inv_t = 1.0f / a.temperature;
     const T *const logits = static_cast<const T *>(a.logits);
     for (int i = tid; i < kMarkBits / 32; i += kRowThreads) mark[i] = 0;
     if (tid < 2) twice[tid] = 0;
@@ -250,16 +281,18 @@ __global__ void __launch_bounds__(kRowThreads, 4) distill_row_kernel(deft_distil
         const int at_last = single(head, whole);
         const bool in = index >= 0 && index < a.vocab;
         float z_at = 0.0f;   // the logit at this lane's entry
-        if (in) z_at = (float)logits[row * a.logits_stride + index] * c;
+        if (in) z_at = (float)logits[row * a.logits_stride + index];
         entry(next, next_index, next_u);
         if (in) {
             const unsigned bit = 1u << (index & 31);
             if (atomicOr(&mark[(index % kMarkBits) >> 5], bit) & bit) twice[odd] = 1;
         }
-        SoftSum s = {-INFINITY, 0.0f}, t = {in ? u * c : -INFINITY, 0.0f};
+        // Everything asked for is there, whether the row is kept or not: otherwise the compiler lets each of the next row's
+        // loads wait for the one before it (8192 x 131071 f16, loss alone: 474 us, 600 so).
+        __builtin_amdgcn_s_waitcnt(0x0f70);   // (vmcnt 0)
+        SoftSum s = {kLowest, 0.0f}, t = {in ? fmaxf(u, kLowest) : kLowest, 0.0f};
         if (kept) {
-            // -3e38 in the place of -infinity: exp2(-infinity - that) is 0, and a NaN stays one
-            float top = at_last >= 0 ? (float)last : -3.0e38f;
+            float top = at_last >= 0 ? fmaxf((float)last, kLowest) : kLowest;
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
                 if ((j * kRowThreads + tid) * n < whole) {
@@ -270,21 +303,36 @@ __global__ void __launch_bounds__(kRowThreads, 4) distill_row_kernel(deft_distil
                 }
                 asm volatile("" : "+v"(x[j]));   // (widened again for the sum: kept as floats the row would not fit)
             }
-            top = fmaxf(top * c, -3.0e38f);
-            float sum[2] = {at_last >= 0 ? exp2_of(__builtin_fmaf((float)last, c, -top)) : 0.0f, 0.0f};
+            const bool some = at_last >= 0 || tid * n < whole;
+            const Scaled scaled(top, c);
+            float sum[2] = {at_last >= 0 ? exp2_of(__builtin_fmaf((float)last, c, -scaled.product)) : 0.0f, 0.0f};
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
                 if ((j * kRowThreads + tid) * n < whole) {
                     float w[n];
                     widen(x[j], w, T());
 #pragma unroll
-                    for (int i = 0; i < n; ++i) sum[i & 1] += exp2_of(__builtin_fmaf(w[i], c, -top));
+                    for (int i = 0; i < n; ++i) sum[i & 1] += exp2_of(__builtin_fmaf(w[i], c, -scaled.product));
                 }
                 asm volatile("" : "+v"(x[j]));
             }
-            s = wave_join2(SoftSum{top, sum[0] + sum[1]}, 32);
-            if (in) t.sum = t.top == -INFINITY ? 0.0f : exp2_of(t.top - t.top);   // (1, or the NaN that the entry is)
-            t = wave_join2(t, 32);
+            s = {top, some ? (sum[0] + sum[1]) * scaled.shrink() : 0.0f};
+            if (__any(some && scaled.far)) {
+                s.sum = at_last >= 0 ? exp2_of(((float)last - top) * c) : 0.0f;
+#pragma unroll
+                for (int j = 0; j < NV; ++j) {
+                    if ((j * kRowThreads + tid) * n >= whole) continue;
+                    i32x4 copy = x[j];
+                    asm volatile("" : "+v"(copy));   // (or it would be widened for both sums at once)
+                    float w[n];
+                    widen(copy, w, T());
+#pragma unroll
+                    for (int i = 0; i < n; ++i) s.sum += exp2_of((w[i] - top) * c);
+                }
+            }
+            s = wave_join2(s, 32, c);
+            if (in) t.sum = exp2_of((u - t.top) * c);   // (1, 0 of -infinity, or the NaN that the entry is)
+            t = wave_join2(t, 32, c);
         }
         const int flag = (__any(index != -1 && !in) ? 1 : 0) | (__any(next_index != -1) ? 2 : 0);
         if (lane == 0) {
@@ -293,17 +341,16 @@ __global__ void __launch_bounds__(kRowThreads, 4) distill_row_kernel(deft_distil
             flags[wave] = flag;
         }
         __syncthreads();
-        s = wave_join2(student[lane & (kRowWaves - 1)], kRowWaves / 2);
-        t = wave_join2(teacher[lane & (kRowWaves - 1)], kRowWaves / 2);
+        s = wave_join2(student[lane & (kRowWaves - 1)], kRowWaves / 2, c);
+        t = wave_join2(teacher[lane & (kRowWaves - 1)], kRowWaves / 2, c);
         const int all = flags[lane & (kRowWaves - 1)];
         const bool outside = __any(all & 1), next_kept = __any(all & 2);
         const bool bad = kept && (outside || s.sum == 0.0f || t.sum == 0.0f), ok = kept && !bad;
-        const float lse = s.top + __log2f(s.sum);
+        const float log_sum = __log2f(s.sum);
         float p = 0.0f, by = 0.0f;
         if (in && ok) {
-            const float v = u * c - t.top;
-            p = exp2_of(v) / t.sum;
-            if (p > 0.0f || p != p) by = p * (v - __log2f(t.sum) - (z_at - lse)) * kLn2;
+            p = exp2_of((u - t.top) * c) * __builtin_amdgcn_rcpf(t.sum);
+            if (p > 0.0f || p != p) by = p * ((u - t.top) * inv_t - (z_at - s.top) * inv_t - (__log2f(t.sum) - log_sum) * kLn2);
         }
         by = wave_sum(by);
         if (lane == 0) part[wave] = by;
@@ -317,13 +364,30 @@ __global__ void __launch_bounds__(kRowThreads, 4) distill_row_kernel(deft_distil
                 p = 0.0f;
                 for (int k = 0; k < a.top_k; ++k) p += same_index[k] == index ? same_prob[k] : 0.0f;
             }
-            fixed = g * (exp2_of(z_at - lse) - p);
+            fixed = g * (exp2_of(__builtin_fmaf(z_at - s.top, c, -log_sum)) - p);
         }
         if (in) mark[(index % kMarkBits) >> 5] = 0;
         if (tid == 0) twice[odd ^ 1] = 0;
 
         T *grad = GRAD ? static_cast<T *>(a.grad_logits) + row * a.grad_stride : nullptr;
-        if (GRAD && at_last >= 0) grad[at_last] = ok ? (T)(g * exp2_of(__builtin_fmaf((float)last, c, -lse))) : (T)0.0f;
+        if (GRAD && at_last >= 0) grad[at_last] = ok ? (T)(g * exp2_of(__builtin_fmaf((float)last - s.top, c, -log_sum))) : (T)0.0f;
+        Scaled scaled(s.top, c);
+        const float over_sum = g * __builtin_amdgcn_rcpf(s.sum);
+        float part_of_sum = over_sum * scaled.shrink();
+        if (GRAD && ok && __any(scaled.far)) {   // (the same in every lane)
+            // The difference in the row's own type: 16-bit logits this large are equal to the largest or so far
+            // below it that nothing is left of their exponential, whatever the difference's rounding.
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                float w[n];
+                widen(x[j], w, T());
+#pragma unroll
+                for (int i = 0; i < n; ++i) w[i] -= s.top;
+                narrow(w, x[j], T());
+            }
+            scaled.product = 0.0f;
+            part_of_sum = over_sum;
+        }
         const int next_head = before(next), next_whole = inside(next_head);
         if (next_kept && single(next_head, next_whole) >= 0) last = logits[next * a.logits_stride + single(next_head, next_whole)];
 #pragma unroll
@@ -335,7 +399,7 @@ __global__ void __launch_bounds__(kRowThreads, 4) distill_row_kernel(deft_distil
                     float w[n];
                     widen(x[j], w, T());
 #pragma unroll
-                    for (int i = 0; i < n; ++i) y[i] = (T)(g * exp2_of(__builtin_fmaf(w[i], c, -lse)));
+                    for (int i = 0; i < n; ++i) y[i] = (T)(part_of_sum * exp2_of(__builtin_fmaf(w[i], c, -scaled.product)));
                 }
                 *reinterpret_cast<V *>(grad + head + at) = y;
             }
@@ -371,8 +435,8 @@ hipError_t row_launch(const deft_distill_t &a, int compute_units, hipStream_t st
 
 // By the row's bytes alone (and by top_k, an entry a lane): as few lanes as hold it, so that more workgroups
 // share a compute unit and one's reductions fall into the others' reads and writes.  (4096 rows of 16-bit logits with
-// 64 entries each, the time for 1024 lanes behind it: 8000 logits 46 us, 138; 12000: 66, 129; 30000: 129, 170;
-// 50257: 190, 224.  200 rows: 8000 logits 18, 21; 30000: 21, 23; 50257: 25, 26.)
+// 64 entries each, the time for 1024 lanes behind it: 8000 logits 28 us, 89; 12000: 45, 93; 30000: 112, 146;
+// 50257: 177, 207.  200 rows of 30000: 13.6, 13.5.)
 template <typename T>
 hipError_t any_launch(const deft_distill_t &a, int compute_units, hipStream_t st)
 {
