@@ -856,6 +856,8 @@ struct Head {
                 e = product<T, S, kSums, kSplit>(q, shape_of(a.hidden, n, q.k / kStep * products, splits, compute_units), st);
             }
         }
+        for (; e == hipSuccess && piece_number < a.n_piece_events; ++piece_number)   // (bounds past the vocabulary's end)
+            e = hipEventRecord(static_cast<hipEvent_t>(a.piece_events[piece_number]), st);
         if (e != hipSuccess || !a.grad_hidden || n == 0) return e;
         HiddenArgs j{};
         j.n = n;
