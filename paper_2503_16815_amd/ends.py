@@ -22,6 +22,8 @@ OPERATORS = {"embed": 1, "embed_grad": 2, "head_loss": 4, "head_grad": 8, "disti
 EXPORTS = ("deft_ends_create", "deft_ends_destroy", "deft_ends_get_info", "deft_embed", "deft_embed_grad",
            "deft_head_loss", "deft_head_grad", "deft_distill")
 
+_MOST = 2 ** 31 - 1   # of a 32-bit field (ctypes cuts what is larger without a word)
+
 _i32, _i64, _f32, _vp = ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_void_p
 
 
@@ -117,6 +119,10 @@ class DeftEnds:
         self._lib = load_library()
         if dtype not in DTYPES:
             raise ValueError(f"dtype is one of {list(DTYPES)}: got {dtype}")
+        for name, value in (("max_rows", max_rows), ("max_vocab", max_vocab), ("max_hidden", max_hidden),
+                            ("max_top_k", max_top_k), ("device", device)):
+            if not -_MOST <= value <= _MOST:
+                raise ValueError(f"{name} does not fit 32 bits: got {value}")
         mask = 0
         for name in ((operators,) if isinstance(operators, str) else operators):
             if name not in OPERATORS:
@@ -275,6 +281,8 @@ class DeftEnds:
         if not isinstance(t, torch.Tensor) or t.dim() != 2 or t.dtype != self.dtype or t.get_device() != self._index:
             raise ValueError(f"{name}: a matrix of {self.dtype} on {self.device} is wanted")
         n, w = t.shape
+        if n > _MOST or w > _MOST:
+            raise ValueError(f"{name}: sizes of 32 bits are wanted, got {(n, w)}")
         if (rows is not None and n != rows) or (width is not None and w != width):
             raise ValueError(f"{name}: shape {(n, w)} does not fit {(rows, width)}")
         if not t.is_contiguous() and ((w > 1 and t.stride(1) != 1) or (n > 1 and t.stride(0) < w)):
@@ -285,7 +293,7 @@ class DeftEnds:
         if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.get_device() != self._index or not t.is_contiguous():
             raise ValueError(f"{name}: a contiguous tensor of {dtype} on {self.device} is wanted")
         got = t.shape
-        if len(got) != len(shape) or any(s is not None and s != g for s, g in zip(shape, got)):
+        if len(got) != len(shape) or any(g > _MOST or (s is not None and s != g) for s, g in zip(shape, got)):
             raise ValueError(f"{name}: shape {tuple(got)} does not fit {shape}")
         return got
 
