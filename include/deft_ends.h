@@ -149,8 +149,9 @@ deft_status_t deft_head_loss(deft_ends_t *h, const deft_head_loss_t *a);
  * the vocabulary at a time; the rows of grad_weight are final piece by piece, in order: where
  * piece_events is given, its element i (a hipEvent_t) is recorded on the stream once the rows
  * below (i + 1) * vocab_piece are written (deft_ends_get_info), so that the communication of a
- * bucket can begin while the next one is computed (elements past the last piece: once all are).  Such
- * a call must not be captured.
+ * bucket can begin while the next one is computed (elements past the last piece: once all are; of a
+ * table that other calls add into afterwards, a bucket is ready once they have).  Such a call must not
+ * be captured.
  * Rows without a valid label have a zero row in grad_hidden and no part in grad_weight.
  * Either gradient may be NULL, not both.
  * In 16-bit types d is rounded to the type before the two products, as their matrix instructions

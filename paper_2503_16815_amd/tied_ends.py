@@ -8,7 +8,10 @@ it where positions are distilled, and the embedding, the last thing of the backw
 program runs those parts of a step around a stand-in for the model's layers (one dense layer in torch),
 measures the forward and the backward window, cuts the table's gradient into buckets by pieces of the
 vocabulary, and lets the exact solver place them in the windows of k iterations (Sec. III.A, III.B
-of the paper).  Inputs are synthetic.
+of the paper).  No row of a shared table is final before the embedding's part has been added, so all buckets
+are ready at the end of the backward pass, and the windows are those that follow it; the events of the head's
+pieces tell when its part of them is written (of a head with a table of its own: when the bucket is ready).  Inputs
+are synthetic.
 """
 from __future__ import annotations
 
@@ -50,7 +53,8 @@ class Step:
     def backward(self, tokens, labels, x, hidden, lse, row_grad, distilled=None, merge=False, piece_events=None):
         """Gradients of sum(row_grad * loss), and of the distilled positions' losses where `distilled` is (positions,
         teacher_index, teacher_logit, row_grad, temperature).  merge: the table's gradient of an earlier iteration,
-        whose update is delayed, is added to."""
+        whose update is delayed, is added to.  piece_events: recorded as the head's part of each piece of the table's
+        gradient is written; the distilled positions' part and the embedding's are added to all pieces after that."""
         grad_hidden, grad_table = self.ends.head_grad(hidden, self.table, labels, lse, row_grad, grad_weight=self.grad_table,
                                                       accumulate=merge, piece_events=piece_events)
         extra = None
@@ -68,16 +72,17 @@ class Step:
 
 
 def schedule(step: Step, forward_us: float, backward_us: float, k: int, link_gbs: float):
-    """The table's gradient placed by the exact solver in the backward and forward windows of k iterations; times in
-    10 us units, value = communication time (Sec. III.B, Problem 1).  A piece of the vocabulary is a bucket, cut further
-    where it would take more than a quarter of the smaller window (Sec. III.D: a bucket has to fit)."""
+    """The table's gradient placed by the exact solver in the forward and backward windows of the k iterations after
+    the one that computed it, at whose end it is ready; times in 10 us units, value = communication time (Sec. III.B,
+    Problem 1).  A piece of the vocabulary is a bucket, cut further where it would take more than a quarter of the
+    smaller window (Sec. III.D: a bucket has to fit)."""
     vocab, hidden = step.table.shape
     unit = 10.0
     row_us = hidden * step.table.element_size() / (link_gbs * 1e3)
     piece = min(step.ends.info().vocab_piece, vocab, max(1, int(min(forward_us, backward_us) / 4 / row_us)))
     rows = [min(piece, vocab - at) for at in range(0, vocab, piece)]
     item = np.array([[max(1, round(r * row_us / unit)) for r in rows]], np.int32)
-    caps = np.array([[max(1, int(t / unit)) for t in (backward_us, forward_us)] * k], np.int32)
+    caps = np.array([[max(1, int(t / unit)) for t in (forward_us, backward_us)] * k], np.int32)
     kb = W.KnapsackBatch("tied_ends", W.MODE_SEQUENTIAL, 1, item.shape[1], 2 * k, np.array([item.shape[1]], np.int32),
                          np.array([2 * k], np.int32), item, item.copy(), caps)
     return kb, binding.solve(kb)
@@ -105,18 +110,19 @@ def main(argv=None) -> int:
     pieces = -(-a.vocab // step.ends.info().vocab_piece)
     for n in range(a.steps):
         marks = [torch.cuda.Event(enable_timing=True) for _ in range(3)]
-        ready = [torch.cuda.Event(enable_timing=True) for _ in range(pieces)]
+        head_part = [torch.cuda.Event(enable_timing=True) for _ in range(pieces)]
         marks[0].record()
         x, hidden, loss, lse = step.forward(tokens, labels)
         marks[1].record()
-        step.backward(tokens, labels, x, hidden, lse, row_grad, distilled, merge=n % a.k != 0, piece_events=ready)
-        marks[2].record()
+        step.backward(tokens, labels, x, hidden, lse, row_grad, distilled, merge=n % a.k != 0, piece_events=head_part)
+        marks[2].record()   # (every piece of the table's gradient is final)
     torch.cuda.synchronize()
     forward_us, backward_us = (1e3 * marks[i].elapsed_time(marks[i + 1]) for i in range(2))
     kb, out = schedule(step, forward_us, backward_us, a.k, a.link_gbs)
     print(json.dumps({
         "loss": float(loss.sum() / (a.rows - 1)), "forward_us": forward_us, "backward_us": backward_us,
-        "pieces_ready_us": [1e3 * marks[1].elapsed_time(e) for e in ready], "unit_us": 10,
+        "head_part_us": [1e3 * marks[1].elapsed_time(e) for e in head_part], "pieces_ready_us": [backward_us] * pieces,
+        "unit_us": 10,
         "bucket_times": kb.weights[0].tolist(), "windows": kb.capacities[0].tolist(),
         "window_of_bucket": out.assignment[0].tolist(), "time_hidden": int(out.total_value[0])}))
     return 0
