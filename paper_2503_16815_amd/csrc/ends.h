@@ -47,6 +47,10 @@ template <> struct Vec<bf16> {
     static constexpr int n = 8;
 };
 
+// What stands for the largest of values that are all -infinity, or of none: -infinity less this gives an exponential of 0,
+// and no finite value is below it.
+constexpr float kLowest = -3.402823466e38f;
+
 // A running softmax sum: the largest value so far and the sum of exp(value - largest).  -infinity
 // adds nothing to it; a NaN or +infinity makes the sum NaN, as the definition does.
 struct SoftSum {

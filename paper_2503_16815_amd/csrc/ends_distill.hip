@@ -20,10 +20,7 @@ constexpr int kThreads = 512, kWaves = kThreads / kWave;
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 // Exponentials are powers of two of (z - largest) log2(e) / T: the difference first, so that neither what a row's
-// logits have in common nor a logit at the end of the type's range costs any bits.  (-infinity less the lowest
-// value, which stands for a largest one where there is none, gives 0, and a NaN stays one.)
-constexpr float kLowest = -3.402823466e38f;
-
+// logits have in common nor a logit at the end of the type's range costs any bits.
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // of running sums whose largest values are logits as they are, kLowest or more (NaN is in the sums alone); c = log2(e) / T

@@ -402,7 +402,7 @@ __global__ void __launch_bounds__(256) few_logits_kernel(FewLogitsArgs a)
             }
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
-        if (top == -INFINITY) top = -3.0e38f;   // (no row of the vocabulary here, or all -infinity)
+        if (top == -INFINITY) top = kLowest;   // (no row of the vocabulary here, or all -infinity)
 #pragma unroll
         for (int i = 0; i < kFewTiles; ++i)
 #pragma unroll

@@ -397,7 +397,7 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
                 }
             s.top = fmaxf(s.top, __shfl_xor(s.top, 16));
             s.top = fmaxf(s.top, __shfl_xor(s.top, 32));
-            const float top = s.top == -INFINITY ? -3.0e38f : s.top;   // (no row of the vocabulary here, or all -infinity)
+            const float top = s.top == -INFINITY ? kLowest : s.top;   // (no row of the vocabulary here, or all -infinity)
 #pragma unroll
             for (int i = 0; i < MT; ++i)
 #pragma unroll
