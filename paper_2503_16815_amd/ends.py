@@ -95,6 +95,8 @@ def _on_stream(method):
     def call(self, *args, stream: Optional[torch.cuda.Stream] = None, **kwargs):
         if stream is None:
             return method(self, *args, **kwargs)
+        if stream.device_index != self._index:   # (its device's current stream would be taken instead)
+            raise ValueError(f"stream: one of {self.device} is wanted, got one of device {stream.device_index}")
         with torch.cuda.stream(stream):
             out = method(self, *args, **kwargs)
         for t in (*args, *kwargs.values()):
