@@ -250,15 +250,16 @@ class DeftEnds:
                      row_grad: torch.Tensor, temperature: float = 1.0, grad_logits: Optional[torch.Tensor] = None,
                      status: Optional[torch.Tensor] = None):
         """(loss, grad_logits) in one pass over the logits; grad_logits may be the logits themselves."""
-        self._words("row_grad", row_grad, torch.float32, (logits.shape[0],))
-        return self._distill(logits, teacher_index, teacher_logit, row_grad, temperature, grad_logits, status)
+        return self._distill(logits, teacher_index, teacher_logit, row_grad, temperature, grad_logits, status, True)
 
-    def _distill(self, logits, teacher_index, teacher_logit, row_grad, temperature, grad_logits, status):
+    def _distill(self, logits, teacher_index, teacher_logit, row_grad, temperature, grad_logits, status, with_grad=False):
         n, vocab = self._rows("logits", logits, None, None)
+        if with_grad:
+            self._words("row_grad", row_grad, torch.float32, (n,))
         top_k = self._words("teacher_index", teacher_index, torch.int32, (n, None))[1]
         self._words("teacher_logit", teacher_logit, torch.float32, (n, top_k))
         loss = torch.empty(n, dtype=torch.float32, device=self.device)
-        if row_grad is not None:
+        if with_grad:
             if grad_logits is None:
                 grad_logits = torch.empty((n, vocab), dtype=self.dtype, device=self.device)
             self._rows("grad_logits", grad_logits, n, vocab)
