@@ -121,6 +121,9 @@ deft_status_t deft_embed_grad(deft_ends_t *h, const deft_embed_grad_t *e);
  * deft_head_loss: z[n][v] = logit_scale * <hidden[n], weight[v]> over the whole vocabulary, never
  * kept;  lse[n] = log sum_v exp(z[n][v]),  loss[n] = lse[n] - z[n][labels[n]].
  * A label of -1 gives loss and lse 0; one outside 0 .. vocab-1 too, and status INVALID_ARG.
+ * Where hidden states or weights are infinite, 32-bit logits of more than 64 positions may be NaN in
+ * the place of an infinity (an operand is multiplied in three parts, zeros among them); so may the
+ * gradients.
  */
 typedef struct {
     int32_t n_rows;
@@ -156,10 +159,11 @@ deft_status_t deft_head_loss(deft_ends_t *h, const deft_head_loss_t *a);
  * Either gradient may be NULL, not both.
  * In 16-bit types d is rounded to the type before the two products, as their matrix instructions
  * take it (scaled so that a row of the largest row_grad fills the range up to a power of two, and
- * 16-bit floats into their range); in 32 bits it is not.  In 16-bit floats a position whose row_grad
- * is 2^-r of the largest has errors of its own beside, where values pass below the type's range:
- * row_grad 2^(s - 38) in an element of d, and in grad_weight d 2^(t - 25) for each of its hidden
- * states' elements, with s = r - 4, from 0 to 12, and t = r - s.
+ * 16-bit floats into their range), so that grad_weight is off by somewhat more than its own rounding
+ * (a tenth to a seventh more, in the norm); in 32 bits it is not.  In 16-bit floats a position whose
+ * row_grad is 2^-r of the largest has errors of its own beside, where values pass below the type's
+ * range: row_grad 2^(s - 38) in an element of d, and in grad_weight d 2^(t - 25) for each of its
+ * hidden states' elements, with s = r - 4, from 0 to 12, and t = r - s.
  */
 typedef struct {
     int32_t n_rows;
@@ -193,8 +197,8 @@ deft_status_t deft_head_grad(deft_ends_t *h, const deft_head_grad_t *a);
  *   grad_logits[n] = row_grad[n] * temperature * (q - p at its indices)
  * grad_logits may be the logits themselves, with the same stride; NULL computes the loss alone.
  * Entries of a row may be fewer than top_k (the others -1, anywhere) and in any order; an index
- * that occurs twice counts with the sum of its entries.  A row without any entry gives zeros.  An
- * index outside -1 .. vocab-1, or a row whose kept entries (or whose logits) are all -infinity, has
+ * that occurs twice is two terms of the loss and counts with the sum of its p in the gradient.  A row
+ * without any entry gives zeros.  An index outside -1 .. vocab-1, or a row whose kept entries (or whose logits) are all -infinity, has
  * no such softmax: zeros, and status INVALID_ARG.
  */
 typedef struct {

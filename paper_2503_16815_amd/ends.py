@@ -112,7 +112,13 @@ class DeftEnds:
     `operators` names what the handle serves (keys of OPERATORS): it holds no scratch memory for
     others.  Outputs are allocated unless given; calls run on `stream` (default: torch's current
     stream) and return without waiting.  Tensors of a call on another stream than their own are
-    recorded there.  Tokens, labels and indices are int32, -1 for nothing.
+    recorded there.  The scratch memory is one call's at a time: a handle's calls go to one stream, or
+    the next stream waits for the one before; work on two streams at once takes two handles.  Tokens,
+    labels and indices are int32, -1 for nothing.
+
+    Gradients are the *_grad calls' results.  torch's automatic differentiation does not see any of these
+    calls: what they give carries no graph, also of inputs that require a gradient, and what they
+    write into (out, grad_table, grad_weight, grad_logits) is not marked as changed.
     """
 
     def __init__(self, operators: Iterable[str], dtype: torch.dtype, max_rows: int, max_vocab: int, max_hidden: int = 0,
