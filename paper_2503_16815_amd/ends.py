@@ -146,7 +146,7 @@ class DeftEnds:
     def close(self) -> None:
         if getattr(self, "_h", None) is not None and self._h:
             self._lib.deft_ends_destroy(self._h)
-            self._h = _vp()
+            self._h = None   # (at the interpreter's end the module's names are gone)
 
     __del__ = close
 
