@@ -7,7 +7,7 @@ from tests.test_gpu_ends import ALL, distill_definition, generator, handle, torc
 
 pytestmark = pytest.mark.gpu
 
-SIZES = [100, 8003, 50257, 140001]
+SIZES = [100, 8003, 12345, 30001, 50257, 100003, 140001]   # (every width of workgroup, by 32- or by 16-bit logits)
 
 
 @pytest.mark.parametrize("dtype", ALL)
