@@ -12,7 +12,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdeft_knapsack.so")
 PKG = "paper_2503_16815_amd"
 SOURCES = ["seq_lds.hip", "seq_lds_rec.hip", "seq_lds_pool.hip", "seq_bits.hip", "seq_bits_long.hip", "seq_bits_queues.hip", "seq_bits_long_queues.hip", "seq_enum.hip", "joint2.hip", "seq_global.hip", "greedy.hip", "schedule_sim.hip", "api.hip", "profile.hip", "static_scratch.hip", "calibrate.hip",
-           "ends_api.hip", "ends_embed.hip", "ends_head.hip", "ends_head_bf16.hip", "ends_head_f16.hip", "ends_head_f32.hip", "ends_distill.hip"]
+           "ends_api.hip", "ends_embed.hip", "ends_head.hip", "ends_head_bf16.hip", "ends_head_f16.hip", "ends_head_f32.hip", "ends_distill.hip",
+           "block_api.hip", "block_checkpoint.hip", "block_ffn.hip", "block_ffn_bf16.hip", "block_ffn_f16.hip", "block_ffn_f32.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wall", "-Wextra", "-Wno-unused-command-line-argument", "-Wno-inline-asm"]

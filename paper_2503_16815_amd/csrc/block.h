@@ -1,0 +1,103 @@
+// What the operators of a layer's feed-forward block share: the arguments of its products' epilogues, checkpoints in
+// device code, and the launch interface between the C ABI (block_api.hip) and the kernels.
+#pragma once
+#include "../../include/deft_block.h"
+#include "ends.h"
+
+namespace deft {
+
+// Beside the operands (ends_product.h).  Panels have 256 columns: [columns / 256][rows][256].
+struct FfnArgs {
+    const void *a2;                  // kGate: the other projection's rows; kInput: those that the second half of b multiplies
+    int64_t a2_ld, a2_plane;
+    int64_t a_panel;                 // kOuter: elements between a's panels (256: rows as they are)
+    int64_t d_half;                  // kInput: elements between b's halves
+    // kGate, kGateGrad
+    int activation;
+    int cols_up;                     // columns of the panels of h, and of each half of d's
+    void *h, *d;                     // panels: hidden activations; derivatives by gate, and behind them by up; or NULL
+    int64_t panel, h_plane, d_plane; // elements between panels, between arrays
+    deft_saved_t saved;              // the projections
+    const float *factor;             // a power of two that d is held times, and its reciprocal; or NULL
+    // kOut, kInput, kOuter: rows n < half go to the first, the others, less `half`, to the second
+    void *out[2];                    // or NULL
+    int64_t out_ld[2];
+    int half, rows;                  // rows that each has
+};
+
+constexpr int kGroup = DEFT_CHECKPOINT_GROUP;
+
+constexpr float kCodes8 = 127.0f, kCodes16 = 32767.0f;   // the largest codes
+
+// The scale of a group: the smallest number of 8 significant bits, at least 2^-126, `most` times which reaches `top`.
+__device__ __forceinline__ float checkpoint_scale(float top, float most)
+{
+    const auto up8 = [](float x) { return __uint_as_float((__float_as_uint(x) + 0xffffu) & 0xffff0000u); };
+    const float s = up8(fmaxf(top / most, 1.17549435e-38f));
+    // (where the quotient's rounding went down to a number of 8 bits)
+    return fmaf(s, most, -top) < 0.0f ? __uint_as_float(__float_as_uint(s) + 0x10000u) : s;
+}
+
+__device__ __forceinline__ bool is_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
+
+// The whole number nearest to x / s, ties to the even one, given 1 / s: x - q s is exact, and tells where the quotient's
+// rounding brought x / s onto a half or away from one.
+__device__ __forceinline__ int checkpoint_code(float x, float s, float inverse)
+{
+    const float q = __builtin_rintf(x * inverse), twice = 2.0f * fmaf(-q, s, x);
+    const int code = (int)q, odd = code & 1;
+    const int more = twice > s || (odd && twice == s), less = twice < -s || (odd && twice == -s);
+    return is_finite(x) ? code + more - less : -128;
+}
+
+// The same up to the half of a step that x itself, a sum in 32 bits, is unsure of.
+__device__ __forceinline__ int checkpoint_code_of_sum(float x, float inverse, float most)
+{
+    return is_finite(x) ? (int)__builtin_rintf(fminf(fmaxf(x * inverse, -most), most)) : -(int)most - 1;
+}
+
+// What a code stands for, up to `most`, the largest number of its type: the nearest multiple of s may lie beyond.
+__device__ __forceinline__ float checkpoint_value(int code, float s, int none, float most)
+{
+    return code == none ? __builtin_nanf("") : fminf(fmaxf((float)code * s, -most), most);
+}
+
+// ---- launches (each returns hipGetLastError() of its launches) ------------------------------
+
+// `x`: its checkpoint as an operand of P arrays of T (ends_operands.h): rows up to a tile, zeros beyond the source.
+struct RestoreArgs {
+    int rows, cols;                  // of the checkpoint
+    int rows_to, cols_to;            // that are written, zeros beyond
+    deft_checkpoint_t from;
+    void *out;
+    int64_t out_ld, out_plane;
+};
+hipError_t checkpoint_launch(int dtype, const deft_checkpoint_call_t &a, hipStream_t st);
+hipError_t restore_launch(int dtype, const deft_restore_call_t &a, hipStream_t st);
+hipError_t restore_operand_launch(int dtype, const RestoreArgs &a, hipStream_t st);
+
+// 16-bit floats: the power of two that brings the largest finite magnitude of x to 1 .. 2, and its reciprocal.
+struct FactorArgs {
+    int rows, cols;
+    const f16 *x;
+    int64_t x_stride;
+    float *parts;    // [kFactorParts]
+    float *factor;   // [2]
+};
+constexpr int kFactorParts = 256;
+hipError_t ffn_factor_launch(const FactorArgs &a, hipStream_t st);
+
+struct FfnPlan {
+    int64_t scratch_bytes = 0;
+    int max_rows = 0, max_hidden = 0, max_inner = 0;
+    int planes = 1;                  // 16-bit arrays that an operand is held in: 1, or 3 for 32-bit types
+    bool grad = false;
+    // offsets into the scratch memory
+    int64_t floats, x, grad_y, w_gate, w_up, w_down, h, d, gate, up, sums;
+};
+void ffn_plan(int dtype, int max_rows, int max_hidden, int max_inner, bool grad, int compute_units, FfnPlan *plan);
+hipError_t ffn_prepare();            // kernel attributes, on the current device
+hipError_t ffn_launch(const FfnPlan &plan, int dtype, const deft_ffn_t &a, void *scratch, int compute_units, hipStream_t st);
+hipError_t ffn_grad_launch(const FfnPlan &plan, int dtype, const deft_ffn_grad_t &a, void *scratch, int compute_units, hipStream_t st);
+
+}  // namespace deft

@@ -1,0 +1,383 @@
+// The gated feed-forward block and its gradient.
+//
+//   gate = x Wg^T;  up = x Wu^T;  h = act(gate) * up;  y = h Wd^T
+//   d = dy Wd;  d_gate = d * up * act'(gate);  d_up = d * act(gate)
+//   dWd = dy^T h;  dWg = d_gate^T x;  dWu = d_up^T x;  dx = d_gate Wg + d_up Wu
+//
+// Both projections are one product (rows of the two matrices alternate in a tile), which leaves h behind, and gate and up
+// as the caller keeps them; y is the second.  The backward pass takes four: the derivative by h, whose epilogue reads gate and
+// up and leaves d_gate, d_up and h behind; dWd; dWg and dWu together; dx, which sums over both.  Where nothing was kept
+// the first product comes again.  9 products of 2 n H I operations (11): bound by the matrix units where rows are many.
+//
+// h, d_gate and d_up are written once, in panels of 256 columns, and read as they are by both products that need them, by
+// one of them through transposing LDS reads; so are the matrices and x.  Where the card would be left idle a sum is cut into
+// parts, which are joined in one order.
+//
+// 16-bit floats hold d_gate and d_up times a power of two that brings the largest of dy to 1 .. 2: the gradient of a mean over many
+// tokens is far below 1, and so out of their range's reach of 2^-14.
+#pragma once
+#include "block.h"
+#include "ends_operands.h"
+
+namespace deft {
+namespace {
+
+constexpr unsigned kNoGate = 1u << kMiddle | 1u << kLow, kNoOther = 1u << kLow;   // shapes without a kernel
+
+struct JoinArgs {
+    FfnArgs ffn;
+    int m, n, splits, add;
+    const float *sums;               // [splits][n][sums_ld]
+    int64_t sums_ld, sums_split;
+};
+
+template <typename O>
+__global__ void __launch_bounds__(256) join_out_kernel(JoinArgs a)
+{
+    const int64_t pieces = (a.m + kEight - 1) / kEight, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t n = at / pieces;
+    if (n >= a.n) return;
+    O *row = out_row<O>(a.ffn, (int)n);
+    if (!row) return;
+    const int m = (int)(at - n * pieces) * kEight;
+    const float *sums = a.sums + n * a.sums_ld + m;
+    float x[kEight] = {};
+    int s = 0;
+    for (; s + 4 <= a.splits; s += 4) {   // (eight loads under way)
+        float y[4][kEight];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) load_eight(sums + (s + i) * a.sums_split, 0, kEight, y[i]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int r = 0; r < kEight; ++r) x[r] += y[i][r];
+    }
+    for (; s < a.splits; ++s) {
+        float y[kEight];
+        load_eight(sums + s * a.sums_split, 0, kEight, y);
+#pragma unroll
+        for (int r = 0; r < kEight; ++r) x[r] += y[r];
+    }
+    store_out(row, m, a.m, x, a.ffn.factor ? a.ffn.factor[1] : 1.0f, a.add);
+}
+
+// One call's view of the scratch memory.
+struct FfnScratch {
+    float *factor, *parts, *sums;
+    char *x, *grad_y, *w_gate, *w_up, *w_down, *h, *d, *gate, *up;
+    FfnScratch(const FfnPlan &plan, void *scratch)
+    {
+        char *s = static_cast<char *>(scratch);
+        factor = reinterpret_cast<float *>(s + plan.floats);
+        parts = factor + 64;
+        x = s + plan.x;
+        grad_y = s + plan.grad_y;
+        w_gate = s + plan.w_gate;
+        w_up = s + plan.w_up;
+        w_down = s + plan.w_down;
+        h = s + plan.h;
+        d = s + plan.d;
+        gate = s + plan.gate;
+        up = s + plan.up;
+        sums = reinterpret_cast<float *>(s + plan.sums);
+    }
+};
+
+struct Operand {
+    const void *p;
+    int64_t ld, plane;
+};
+
+template <typename S, typename T, int P>
+struct Ffn {
+    static constexpr bool kSplit = P == 3, kHalf16 = __is_same(T, f16);
+
+    template <int E>
+    static hipError_t product(const ProductArgs &p, Shape shape, hipStream_t st)
+    {
+        switch (shape) {
+        case kMiddle:
+            if constexpr (E != kGate) return product_shape<T, S, E, 2, 4, 6, 4, kSplit>(p, st);
+            return hipErrorInvalidValue;
+        case kHalf: return product_shape<T, S, E, 4, 2, 4, 4, kSplit>(p, st);
+        case kSmall: return product_shape<T, S, E, 2, 2, 4, 4, kSplit>(p, st);
+        case kNarrow: return product_shape<T, S, E, 4, 2, 4, 2, kSplit>(p, st);
+        case kLarge: return product_shape<T, S, E, 2, 4, 8, 4, kSplit>(p, st);
+        default: return hipErrorInvalidValue;
+        }
+    }
+
+    template <int E>
+    static hipError_t allow()
+    {
+        hipError_t e = allow_shape<T, S, E, 2, 4, 8, 4, kSplit>();
+        if constexpr (E != kGate)
+            if (e == hipSuccess) e = allow_shape<T, S, E, 2, 4, 6, 4, kSplit>();
+        if (e == hipSuccess) e = allow_shape<T, S, E, 4, 2, 4, 4, kSplit>();
+        if (e == hipSuccess) e = allow_shape<T, S, E, 2, 2, 4, 4, kSplit>();
+        if (e == hipSuccess) e = allow_shape<T, S, E, 4, 2, 4, 2, kSplit>();
+        return e;
+    }
+
+    static hipError_t prepare()
+    {
+        hipError_t e = allow<kGate>();
+        if (e == hipSuccess) e = allow<kGateGrad>();
+        if (e == hipSuccess) e = allow<kOut>();
+        if (e == hipSuccess) e = allow<kInput>();
+        if (e == hipSuccess) e = allow<kOuter>();
+        return e;
+    }
+
+    // Rows as the products read them: where they are, or packed.  `along`: a product has their elements as its k, beside those
+    // that have them as m or n (whole pieces of 16 bytes are enough for these).
+    static hipError_t operand(const void *p, int64_t stride, int rows, int cols, bool along, void *packed, Operand *out, hipStream_t st)
+    {
+        if (!kSplit && in_place(p, stride, cols, along ? kStep : 8)) {
+            *out = {p, stride, 0};
+            return hipSuccess;
+        }
+        PackArgs a{};
+        a.src = p;
+        a.src_stride = stride;
+        a.rows = rows;
+        a.cols = cols;
+        a.out = packed;
+        a.out_ld = up(cols, kStep);
+        a.out_plane = up(rows, kTile) * a.out_ld;
+        *out = {packed, a.out_ld, a.out_plane};
+        pack_rows_kernel<S, T, P><<<(unsigned)(up(a.out_plane >> 3, 1024) / 1024), 256, 0, st>>>(a);
+        return hipGetLastError();
+    }
+
+    static hipError_t restored(const deft_checkpoint_t &from, int rows, int cols, int dtype, void *packed, Operand *out, hipStream_t st)
+    {
+        RestoreArgs a{};
+        a.rows = rows;
+        a.cols = cols;
+        a.rows_to = (int)up(rows, kTile);
+        a.cols_to = (int)up(cols, kStep);
+        a.from = from;
+        a.out = packed;
+        a.out_ld = a.cols_to;
+        a.out_plane = (int64_t)a.rows_to * a.cols_to;
+        *out = {packed, a.out_ld, a.out_plane};
+        return restore_operand_launch(dtype, a, st);
+    }
+
+    static FfnArgs panels(const FfnScratch &s, int n, int inner, int activation)
+    {
+        FfnArgs f{};
+        f.activation = activation;
+        f.cols_up = (int)up(inner, 256);
+        f.panel = up(n, kTile) * 256;
+        f.h_plane = f.cols_up / 256 * f.panel;
+        f.d_plane = 2 * f.h_plane;
+        f.h = s.h;
+        f.half = f.rows = INT32_MAX;
+        f.a_panel = 256;
+        return f;
+    }
+
+    static hipError_t gate(const FfnArgs &f, const Operand &x, const Operand &w_gate, const Operand &w_up, int n, int hidden, int inner, int compute_units,
+                           hipStream_t st)
+    {
+        ProductArgs p{};
+        p.a = w_gate.p;
+        p.a_ld = w_gate.ld;
+        p.a_plane = w_gate.plane;
+        p.b = x.p;
+        p.b_ld = x.ld;
+        p.b_plane = x.plane;
+        p.m = inner;
+        p.n = n;
+        p.k = (int)up(hidden, kStep);
+        p.splits = 1;
+        p.ffn = f;
+        p.ffn.a2 = w_up.p;
+        p.ffn.a2_ld = w_up.ld;
+        p.ffn.a2_plane = w_up.plane;
+        return product<kGate>(p, shape_of(2 * (int64_t)inner, n, (int64_t)(p.k / kStep) * (kSplit ? 6 : 1), 1, compute_units, kNoGate), st);
+    }
+
+    // A product whose sums are the result: cut into parts where that is quicker.
+    template <int E>
+    static hipError_t summed(ProductArgs &p, const FfnScratch &s, int compute_units, hipStream_t st)
+    {
+        const int64_t steps = (int64_t)(p.k / kStep) * (kSplit ? 6 : 1) * (E == kInput ? 2 : 1);
+        p.splits = splits_of(p.m, p.n, steps, compute_units, kNoOther);
+        p.sums = s.sums;
+        p.sums_ld = up(p.m, kEight);
+        p.sums_split = p.n * p.sums_ld;
+        const hipError_t e = product<E>(p, shape_of(p.m, p.n, steps, p.splits, compute_units, kNoOther), st);
+        if (e != hipSuccess || p.splits == 1) return e;
+        JoinArgs j{};
+        j.ffn = p.ffn;
+        j.m = p.m;
+        j.n = p.n;
+        j.splits = p.splits;
+        j.add = p.add;
+        j.sums = p.sums;
+        j.sums_ld = p.sums_ld;
+        j.sums_split = p.sums_split;
+        join_out_kernel<S><<<(unsigned)(up((int64_t)p.n * ((p.m + kEight - 1) / kEight), 256) / 256), 256, 0, st>>>(j);
+        return hipGetLastError();
+    }
+
+    static hipError_t forward(const FfnPlan &, const deft_ffn_t &a, const FfnScratch &s, int compute_units, hipStream_t st)
+    {
+        Operand x, w_gate, w_up, w_down;
+        hipError_t e = operand(a.x, a.x_stride, a.n_rows, a.hidden, true, s.x, &x, st);
+        if (e == hipSuccess) e = operand(a.w_gate, a.w_gate_stride, a.inner, a.hidden, true, s.w_gate, &w_gate, st);
+        if (e == hipSuccess) e = operand(a.w_up, a.w_up_stride, a.inner, a.hidden, true, s.w_up, &w_up, st);
+        if (e == hipSuccess) e = operand(a.w_down, a.w_down_stride, a.hidden, a.inner, true, s.w_down, &w_down, st);
+        if (e != hipSuccess) return e;
+        FfnArgs f = panels(s, a.n_rows, a.inner, a.activation);
+        f.saved = a.save;
+        e = gate(f, x, w_gate, w_up, a.n_rows, a.hidden, a.inner, compute_units, st);
+        if (e != hipSuccess) return e;
+        ProductArgs p{};
+        p.a = w_down.p;
+        p.a_ld = w_down.ld;
+        p.a_plane = w_down.plane;
+        p.b = s.h;
+        p.b_ld = 256;
+        p.b_plane = f.h_plane;
+        p.d_panel = f.panel;
+        p.m = a.hidden;
+        p.n = a.n_rows;
+        p.k = (int)up(a.inner, kStep);
+        p.ffn = f;
+        p.ffn.out[0] = a.y;
+        p.ffn.out_ld[0] = a.y_stride;
+        return summed<kOut>(p, s, compute_units, st);
+    }
+
+    static hipError_t backward(const FfnPlan &, const deft_ffn_grad_t &a, const FfnScratch &s, int compute_units, hipStream_t st)
+    {
+        const int n = a.n_rows;
+        const bool of_gate = a.grad_gate || a.grad_up, by_projections = of_gate || a.grad_x;
+        Operand x{}, grad_y{}, w_gate{}, w_up{}, w_down{};
+        FfnArgs f = panels(s, n, a.inner, a.activation);
+        hipError_t e = hipSuccess;
+        if (n > 0) {
+            const bool again = a.saved.kind == DEFT_SAVE_NONE;
+            e = operand(a.grad_y, a.grad_y_stride, n, a.hidden, true, s.grad_y, &grad_y, st);
+            if (e == hipSuccess && (again || of_gate))
+                e = a.x ? operand(a.x, a.x_stride, n, a.hidden, again, s.x, &x, st)
+                        : restored(a.packed_x, n, a.hidden, kSplit ? DEFT_F32 : kHalf16 ? DEFT_F16 : DEFT_BF16, s.x, &x, st);
+            if (e == hipSuccess && (again || a.grad_x)) e = operand(a.w_gate, a.w_gate_stride, a.inner, a.hidden, again, s.w_gate, &w_gate, st);
+            if (e == hipSuccess && (again || a.grad_x)) e = operand(a.w_up, a.w_up_stride, a.inner, a.hidden, again, s.w_up, &w_up, st);
+            if (e == hipSuccess && by_projections) e = operand(a.w_down, a.w_down_stride, a.hidden, a.inner, false, s.w_down, &w_down, st);
+            if (e != hipSuccess) return e;
+            if (again) {
+                const int64_t ld = up(a.inner, kStep);
+                f.saved.kind = DEFT_SAVE_FULL;
+                f.saved.gate = {s.gate, ld, s.gate + up(n, kTile) * ld * (int64_t)sizeof(S), ld / kGroup};
+                f.saved.up = {s.up, ld, s.up + up(n, kTile) * ld * (int64_t)sizeof(S), ld / kGroup};
+                FfnArgs g = f;
+                if (by_projections) g.h = nullptr;
+                e = gate(g, x, w_gate, w_up, n, a.hidden, a.inner, compute_units, st);
+            } else {
+                f.saved = a.saved;
+            }
+            if constexpr (kHalf16) {
+                if (e == hipSuccess && by_projections) {
+                    e = ffn_factor_launch({n, a.hidden, static_cast<const f16 *>(a.grad_y), a.grad_y_stride, s.parts, s.factor}, st);
+                    f.factor = s.factor;
+                }
+            }
+            if (e == hipSuccess && (by_projections || !again)) {   // (else the product above has left h)
+                ProductArgs p{};
+                p.a = w_down.p;
+                p.a_ld = w_down.ld;
+                p.a_plane = w_down.plane;
+                p.a_rows = a.hidden;
+                p.b = grad_y.p;
+                p.b_ld = grad_y.ld;
+                p.b_plane = grad_y.plane;
+                p.m = a.inner;
+                p.n = n;
+                p.k = by_projections ? (int)up(a.hidden, kStep) : 0;
+                p.splits = 1;
+                p.ffn = f;
+                p.ffn.h = a.grad_down ? s.h : nullptr;
+                p.ffn.d = by_projections ? s.d : nullptr;
+                e = product<kGateGrad>(p, shape_of(a.inner, n, (int64_t)(p.k / kStep) * (kSplit ? 6 : 1), 1, compute_units, kNoOther), st);
+            }
+        }
+        const bool weights = n > 0 || !a.accumulate;
+        ProductArgs q{};   // of the matrices' gradients
+        q.k = (int)up(n, kStep);
+        q.add = a.accumulate;
+        q.ffn = f;
+        if (e == hipSuccess && a.grad_down && weights) {
+            ProductArgs p = q;
+            p.a = s.h;
+            p.a_ld = 256;
+            p.a_plane = f.h_plane;
+            p.a_rows = p.k;
+            p.ffn.a_panel = f.panel;
+            p.b = grad_y.p;
+            p.b_ld = grad_y.ld;
+            p.b_plane = grad_y.plane;
+            p.b_rows = n;
+            p.d_panel = 256;
+            p.m = a.inner;
+            p.n = a.hidden;
+            p.ffn.out[0] = a.grad_down;
+            p.ffn.out_ld[0] = a.grad_down_stride;
+            p.ffn.factor = nullptr;
+            e = summed<kOuter>(p, s, compute_units, st);
+        }
+        if (e == hipSuccess && a.events) e = hipEventRecord(static_cast<hipEvent_t>(a.events[0]), st);
+        if (e == hipSuccess && of_gate && weights) {
+            ProductArgs p = q;
+            p.a = x.p;
+            p.a_ld = x.ld;
+            p.a_plane = x.plane;
+            p.a_rows = n;
+            p.b = s.d;
+            p.b_ld = 256;
+            p.b_plane = f.d_plane;
+            p.b_rows = p.k;
+            p.d_panel = f.panel;
+            p.m = a.hidden;
+            p.n = 2 * f.cols_up;
+            p.ffn.out[0] = a.grad_gate;
+            p.ffn.out_ld[0] = a.grad_gate_stride;
+            p.ffn.out[1] = a.grad_up;
+            p.ffn.out_ld[1] = a.grad_up_stride;
+            p.ffn.half = f.cols_up;
+            p.ffn.rows = a.inner;
+            e = summed<kOuter>(p, s, compute_units, st);
+        }
+        if (e == hipSuccess && a.events) e = hipEventRecord(static_cast<hipEvent_t>(a.events[1]), st);
+        if (e == hipSuccess && a.grad_x && n > 0) {
+            ProductArgs p{};
+            p.a = w_gate.p;
+            p.a_ld = w_gate.ld;
+            p.a_plane = w_gate.plane;
+            p.a_rows = a.inner;
+            p.b = s.d;
+            p.b_ld = 256;
+            p.b_plane = f.d_plane;
+            p.d_panel = f.panel;
+            p.m = a.hidden;
+            p.n = n;
+            p.k = (int)up(a.inner, kStep);
+            p.ffn = f;
+            p.ffn.a2 = w_up.p;
+            p.ffn.a2_ld = w_up.ld;
+            p.ffn.a2_plane = w_up.plane;
+            p.ffn.d_half = f.h_plane;
+            p.ffn.out[0] = a.grad_x;
+            p.ffn.out_ld[0] = a.grad_x_stride;
+            e = summed<kInput>(p, s, compute_units, st);
+        }
+        return e;
+    }
+};
+
+}  // namespace
+}  // namespace deft

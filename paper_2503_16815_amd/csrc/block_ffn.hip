@@ -1,0 +1,114 @@
+// The feed-forward block's scratch memory, and its calls by type (each type's kernels are a file of their own).
+#include "block.h"
+#include "ends_shapes.h"
+
+namespace deft {
+namespace {
+
+// The largest finite magnitude of the rows that a workgroup has.
+__global__ void __launch_bounds__(256) largest_kernel(FactorArgs a)
+{
+    __shared__ float of_wave[4];
+    float top = 0.0f;
+    for (int row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const f16 *x = a.x + (int64_t)row * a.x_stride;
+        for (int c = threadIdx.x; c < a.cols; c += 256) {
+            const float v = fabsf((float)x[c]);
+            top = fmaxf(top, is_finite(v) ? v : 0.0f);
+        }
+    }
+    top = wave_max(top);
+    if ((threadIdx.x & 63) == 0) of_wave[threadIdx.x >> 6] = top;
+    __syncthreads();
+    if (threadIdx.x == 0) a.parts[blockIdx.x] = fmaxf(fmaxf(of_wave[0], of_wave[1]), fmaxf(of_wave[2], of_wave[3]));
+}
+
+__global__ void __launch_bounds__(64) factor_kernel(FactorArgs a)
+{
+    float top = 0.0f;
+    for (int i = threadIdx.x; i < kFactorParts; i += 64) top = fmaxf(top, a.parts[i]);
+    top = wave_max(top);
+    if (threadIdx.x == 0) {
+        const int e = top > 0.0f ? ilogbf(top) : 0;
+        a.factor[0] = ldexpf(1.0f, -e);
+        a.factor[1] = ldexpf(1.0f, e);
+    }
+}
+
+}  // namespace
+
+hipError_t ffn_factor_launch(const FactorArgs &a, hipStream_t st)
+{
+    largest_kernel<<<kFactorParts, 256, 0, st>>>(a);
+    factor_kernel<<<1, 64, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+#define DEFT_FFN_TYPE(NAME)                                                             \
+    hipError_t ffn_prepare_##NAME();                                                    \
+    hipError_t ffn_##NAME(const FfnPlan &, const deft_ffn_t &, void *, int, hipStream_t); \
+    hipError_t ffn_grad_##NAME(const FfnPlan &, const deft_ffn_grad_t &, void *, int, hipStream_t);
+DEFT_FFN_TYPE(bf16)
+DEFT_FFN_TYPE(f16)
+DEFT_FFN_TYPE(f32)
+
+void ffn_plan(int dtype, int max_rows, int max_hidden, int max_inner, bool grad, int compute_units, FfnPlan *plan)
+{
+    const int64_t n = up(max_rows, kTile), hidden = up(max_hidden, kTile), inner = up(max_inner, kTile);
+    plan->max_rows = max_rows;
+    plan->max_hidden = max_hidden;
+    plan->max_inner = max_inner;
+    plan->grad = grad;
+    plan->planes = dtype == DEFT_F32 ? 3 : 1;
+    int64_t at = 0;
+    const auto take = [&](int64_t bytes) {
+        const int64_t here = at;
+        at += up(bytes, 256);
+        return here;
+    };
+    const int64_t element = 2 * plan->planes, own = dtype == DEFT_F32 ? 4 : 2;
+    plan->floats = take((64 + kFactorParts) * 4);
+    // (whether a call's rows can be read in place is known when it is made)
+    plan->x = take(n * up(max_hidden, kStep) * element);
+    plan->w_gate = take(inner * up(max_hidden, kStep) * element);
+    plan->w_up = take(inner * up(max_hidden, kStep) * element);
+    plan->w_down = take(hidden * up(max_inner, kStep) * element);
+    plan->h = take(n * inner * element);
+    int64_t most = n * hidden;   // sums of one part
+    if (grad) {
+        plan->grad_y = take(n * up(max_hidden, kStep) * element);
+        plan->d = take(2 * n * inner * element);
+        const int64_t kept = n * up(max_inner, kStep) * own + n * (up(max_inner, kStep) / kGroup) * 2;   // and scales
+        plan->gate = take(kept);
+        plan->up = take(kept);
+        most = most > 2 * inner * hidden ? most : 2 * inner * hidden;
+    }
+    // parts of sums: parts * tiles stays within twice the compute units
+    const int64_t tiles = 2 * (int64_t)compute_units * kTile * kTile;
+    plan->sums = take((tiles < most * kMaxSplits ? tiles : most * kMaxSplits) * 4);
+    plan->scratch_bytes = at;
+}
+
+hipError_t ffn_prepare()
+{
+    hipError_t e = ffn_prepare_bf16();
+    if (e == hipSuccess) e = ffn_prepare_f16();
+    if (e == hipSuccess) e = ffn_prepare_f32();
+    return e;
+}
+
+hipError_t ffn_launch(const FfnPlan &plan, int dtype, const deft_ffn_t &a, void *scratch, int compute_units, hipStream_t st)
+{
+    if (dtype == DEFT_F32) return ffn_f32(plan, a, scratch, compute_units, st);
+    if (dtype == DEFT_F16) return ffn_f16(plan, a, scratch, compute_units, st);
+    return ffn_bf16(plan, a, scratch, compute_units, st);
+}
+
+hipError_t ffn_grad_launch(const FfnPlan &plan, int dtype, const deft_ffn_grad_t &a, void *scratch, int compute_units, hipStream_t st)
+{
+    if (dtype == DEFT_F32) return ffn_grad_f32(plan, a, scratch, compute_units, st);
+    if (dtype == DEFT_F16) return ffn_grad_f16(plan, a, scratch, compute_units, st);
+    return ffn_grad_bf16(plan, a, scratch, compute_units, st);
+}
+
+}  // namespace deft

@@ -47,6 +47,29 @@ template <> struct Vec<bf16> {
     static constexpr int n = 8;
 };
 
+// A float as a sum of three bf16: the first two cut off (so that they are exact and cannot
+// overflow), the last rounded.  What is not finite stays in the first.
+__device__ __forceinline__ void split3(float x, bf16 (&p)[3])
+{
+    const auto cut = [](float f) { return __uint_as_float(__float_as_uint(f) & 0xffff0000u); };
+    const bool finite = (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u;
+    const float first = finite ? cut(x) : x;
+    const float rest = finite ? x - first : 0.0f;
+    const float second = cut(rest);
+    p[0] = (bf16)first;
+    p[1] = (bf16)second;
+    p[2] = (bf16)(rest - second);
+}
+
+__device__ __forceinline__ unsigned pack2(f16 a, f16 b)
+{
+    return (unsigned)__builtin_bit_cast(unsigned short, a) | (unsigned)__builtin_bit_cast(unsigned short, b) << 16;
+}
+__device__ __forceinline__ unsigned pack2(bf16 a, bf16 b)
+{
+    return (unsigned)__builtin_bit_cast(unsigned short, a) | (unsigned)__builtin_bit_cast(unsigned short, b) << 16;
+}
+
 // What stands for the largest of values that are all -infinity, or of none: -infinity less this gives an exponential of 0,
 // and no finite value is below it.
 constexpr float kLowest = -3.402823466e38f;

@@ -25,7 +25,7 @@
 // 1100), 8192 x 131072 x 4096 bf16 25.5 ms (1380; 1530), 1024 x 8209 x 640 f32 0.30 ms.  Loss alone of one position of 50257 x
 // 1600 35 us, of 13 of 131072 x 4096 176 us (6.1 TB/s).
 #pragma once
-#include "ends_product.h"
+#include "ends_operands.h"
 #include "ends_shapes.h"
 
 namespace deft {
@@ -125,19 +125,7 @@ __global__ void __launch_bounds__(1024) rows_kernel(RowsArgs a)
     }
 }
 
-// ---- operands as the products read them ------------------------------------------------------
-
-struct PackArgs {
-    const void *src;
-    int64_t src_stride;
-    int rows, cols;
-    const int *row_of, *rows_dev;   // packed positions, or NULL
-    void *out;                      // [rows up to a tile][out_ld], zeros beyond the source
-    int64_t out_ld, out_plane;
-    void *out_t;                    // [cols][t_ld]; or NULL
-    int64_t t_ld, t_plane;
-    const float *power, *most;      // out_t's columns are scaled by power[row] / most; or NULL
-};
+// ---- operands with a transposed copy ------------------------------------------------------------
 
 template <typename S, typename T, int P>
 __global__ void __launch_bounds__(256) pack_kernel(PackArgs a)
@@ -205,54 +193,6 @@ __global__ void __launch_bounds__(256) pack_kernel(PackArgs a)
             for (int i = 0; i < 8; ++i) y[i] = tile[p][r + i][c];
             *reinterpret_cast<T8 *>(static_cast<T *>(a.out_t) + p * a.t_plane + (int64_t)(col0 + c) * a.t_ld + row0 + r) = y;
         }
-    }
-}
-
-// The same without a transposed copy: 16 bytes a thread, four at a time, one row's after the other.  Bound by memory (30011
-// rows of 1021 16-bit elements, 1026 apart: 24.5 us, 5.0 TB/s read and written; in tiles of 64 x 64 33 us).
-template <typename S, typename T, int P>
-__global__ void __launch_bounds__(256) pack_rows_kernel(PackArgs a)
-{
-    typedef S S8 __attribute__((ext_vector_type(8), aligned(sizeof(S))));
-    typedef T T8 __attribute__((ext_vector_type(8)));
-    const unsigned pieces = (unsigned)(a.out_ld >> 3), first = blockIdx.x * 1024 + threadIdx.x;
-    const int rows = a.rows_dev ? *a.rows_dev : a.rows, rows_up = (rows + kTile - 1) / kTile * kTile;
-    S x[4][8] = {};
-    unsigned row[4], col[4];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        row[q] = (first + q * 256) / pieces;
-        col[q] = ((first + q * 256) - row[q] * pieces) * 8;
-        if (row[q] >= (unsigned)rows) continue;
-        const S *from = static_cast<const S *>(a.src) + (int64_t)(a.row_of ? a.row_of[row[q]] : (int)row[q]) * a.src_stride + col[q];
-        if ((int)col[q] + 8 <= a.cols) {
-            const S8 v = *reinterpret_cast<const S8 *>(from);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[q][i] = v[i];
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if ((int)col[q] + i < a.cols) x[q][i] = from[i];
-        }
-    }
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        if (row[q] >= (unsigned)rows_up) continue;
-        T8 y[P];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if constexpr (P == 3) {
-                bf16 s[3];
-                split3(x[q][i], s);
-#pragma unroll
-                for (int p = 0; p < 3; ++p) y[p][i] = s[p];
-            } else {
-                y[0][i] = x[q][i];
-            }
-        }
-#pragma unroll
-        for (int p = 0; p < P; ++p)
-            *reinterpret_cast<T8 *>(static_cast<T *>(a.out) + p * a.out_plane + (int64_t)row[q] * a.out_ld + col[q]) = y[p];
     }
 }
 
@@ -488,15 +428,6 @@ __global__ void __launch_bounds__(256) join_hidden_kernel(HiddenArgs a)
 
 // ---- launches -------------------------------------------------------------------------------
 
-template <typename T, typename O, int E, int WM, int WN, int MT, int NT, bool SPLIT>
-hipError_t product_shape(const ProductArgs &p, hipStream_t st)
-{
-    constexpr int TM = WM * MT * 16, TN = WN * NT * 16, kLds = product_lds(TM, TN, WM * WN * kWave);
-    const int grid = ((p.m + TM - 1) / TM) * ((p.n + TN - 1) / TN) * p.splits;
-    product_kernel<T, O, E, WM, WN, MT, NT, SPLIT><<<grid, WM * WN * kWave, kLds, st>>>(p);
-    return hipGetLastError();
-}
-
 template <typename T, typename O, int E, bool SPLIT>
 hipError_t product(const ProductArgs &p, Shape shape, hipStream_t st)
 {
@@ -510,13 +441,6 @@ hipError_t product(const ProductArgs &p, Shape shape, hipStream_t st)
         return hipErrorInvalidValue;   // (few_logits_kernel)
     default: return product_shape<T, O, E, 2, 4, 8, 4, SPLIT>(p, st);
     }
-}
-
-template <typename T, typename O, int E, int WM, int WN, int MT, int NT, bool SPLIT>
-hipError_t allow_shape()
-{
-    return hipFuncSetAttribute(reinterpret_cast<const void *>(&product_kernel<T, O, E, WM, WN, MT, NT, SPLIT>),
-                               hipFuncAttributeMaxDynamicSharedMemorySize, product_lds(WM * MT * 16, WN * NT * 16, WM * WN * kWave));
 }
 
 template <typename T, typename O, int E, bool SPLIT>
@@ -571,13 +495,6 @@ struct Scratch {
         sums = reinterpret_cast<float *>(s + plan.sums);
     }
 };
-
-// Whether a product can read rows of the weights where they are: whole steps of k (the next row's
-// elements, or what lies between rows, must not come in), 16-byte pieces, offsets within 32 bits.
-bool in_place(const void *p, int64_t stride, int hidden)
-{
-    return hidden % kStep == 0 && stride % 8 == 0 && ((uintptr_t)p & 15) == 0 && stride <= (1 << 22);
-}
 
 template <typename S, typename T, int P>
 struct Head {

@@ -33,14 +33,21 @@
 // 32-bit operands come as three 16-bit arrays whose sum they are (8 bits of the significand in
 // each); the six products of those arrays that matter at 24 bits are summed one after the other, step by step (loss
 // and gradients of 2 x 91134 x 305 334 us, 40 x 30000 x 512 176; all steps of one product before the next 357 and 191).
+//
+// The feed-forward block's products are the same kernel with epilogues of their own (block_epilogue.h).  kGate has two
+// operands A, whose rows alternate sixteen at a time, so that a lane holds both projections of an element; kInput adds two
+// products, one's steps behind the other's; kOuter has the elements of both operands' m and n next to each other.
 #pragma once
+#include "block_epilogue.h"
 #include "ends_shapes.h"
 
 namespace deft {
 
 constexpr int kStepBytes = kStep * 2;
 
-enum Epilogue { kSoftmax = 0, kDerivative = 1, kSums = 2, kGradient = 3 };
+// kGate: both projections and the hidden activations; kGateGrad: the derivatives by both projections; kOut: y; kInput: x's
+// gradient; kOuter: a matrix's gradient
+enum Epilogue { kSoftmax = 0, kDerivative = 1, kSums = 2, kGradient = 3, kGate = 4, kGateGrad = 5, kOut = 6, kInput = 7, kOuter = 8 };
 
 struct ProductArgs {
     const void *a, *b;               // kSums, kGradient: b is the derivative, as below
@@ -49,7 +56,7 @@ struct ProductArgs {
     int m, n;                        // rows of a and of b
     const int *n_dev;                // rows of b that count, where the device knows it, or NULL
     int k;                           // a multiple of kStep
-    int a_rows;                      // kSums: the k that a has rows of
+    int a_rows, b_rows;              // the k that a has rows of where its m elements are next to each other; kOuter: that b has
     const int *k_dev;                // or the rows of another operand, rounded up to kStep
     int splits;                      // of k
     float scale;
@@ -73,6 +80,7 @@ struct ProductArgs {
     const float *out_scale;          // beside `scale`
     void *out;
     int64_t out_ld;
+    FfnArgs ffn;                     // the feed-forward block's
 };
 
 template <typename T> struct Mfma;
@@ -90,29 +98,6 @@ template <> struct Mfma<bf16> {
         asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
     }
 };
-
-// A float as a sum of three bf16: the first two cut off (so that they are exact and cannot
-// overflow), the last rounded.  What is not finite stays in the first.
-__device__ __forceinline__ void split3(float x, bf16 (&p)[3])
-{
-    const auto cut = [](float f) { return __uint_as_float(__float_as_uint(f) & 0xffff0000u); };
-    const bool finite = (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u;
-    const float first = finite ? cut(x) : x;
-    const float rest = finite ? x - first : 0.0f;
-    const float second = cut(rest);
-    p[0] = (bf16)first;
-    p[1] = (bf16)second;
-    p[2] = (bf16)(rest - second);
-}
-
-__device__ __forceinline__ unsigned pack2(f16 a, f16 b)
-{
-    return (unsigned)__builtin_bit_cast(unsigned short, a) | (unsigned)__builtin_bit_cast(unsigned short, b) << 16;
-}
-__device__ __forceinline__ unsigned pack2(bf16 a, bf16 b)
-{
-    return (unsigned)__builtin_bit_cast(unsigned short, a) | (unsigned)__builtin_bit_cast(unsigned short, b) << 16;
-}
 
 constexpr int kStagesA = 3, kStagesB = 2;
 // The rows that a tile's loads bring: every thread loads 16 bytes, an eighth of a row, at a time.
@@ -165,18 +150,21 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
     constexpr int kABytes = kARows * kStepBytes, kBBytes = kBRows * kStepBytes, kBAt = kStagesA * kABytes;
     constexpr int kALoads = kARows * 8 / kThreads, kBLoads = kBRows * 8 / kThreads;
     constexpr int kFetches = MT + NT, kProducts = MT * NT;
-    constexpr bool kTurned = E == kGradient;   // B's n elements are next to each other
-    constexpr bool kTurnedA = E == kSums;      // A's m elements are
-    constexpr bool kPanels = E == kSums || E == kGradient;
+    constexpr bool kTurned = E == kGradient || E == kOuter;   // B's n elements are next to each other
+    constexpr bool kTurnedA = E == kSums || E == kGateGrad || E == kInput || E == kOuter;   // A's m elements are
+    constexpr bool kPanels = E == kSums || E == kGradient || E == kOut || E == kInput;
+    constexpr bool kAimed = kPanels || kTurned || kTurnedA;   // a step's place is not the last one's and 64 elements more
     constexpr int kPanelSteps = 256 / kStep;
+    constexpr int kColumns = E == kGate ? TM / 2 : TM;   // of C that a tile has
     constexpr int kPieces = TN / 8, kPiecesA = TM / 8;   // 16-byte pieces of a row of TN, of TM
     static_assert(!kTurned || kBRows == TN, "whole rows of k");
     typedef typename Mfma<T>::operand Operand;
+    static_assert(E < kGate || WM * WN * epilogue_floats(MT) * 4 <= product_lds(TM, TN, kThreads));
     extern __shared__ __align__(16) char lds[];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / WN, wn = wave % WN;
     const int n_rows = p.n_dev ? *p.n_dev : p.n;
-    const int tiles_m = (p.m + TM - 1) / TM, tiles_n = (n_rows + TN - 1) / TN;
+    const int tiles_m = (p.m + kColumns - 1) / kColumns, tiles_n = (n_rows + TN - 1) / TN;
     // workgroup b runs on XCD b % 8; each XCD has an equal share of the parts' tiles, in groups four wide
     const int tiles = tiles_m * tiles_n, items = tiles * p.splits, xcd = blockIdx.x & 7, share = items >> 3, more = items & 7;
     if ((int)(blockIdx.x >> 3) >= share + (xcd < more ? 1 : 0)) return;
@@ -185,36 +173,59 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
     const int group = tile / (tiles_m * 4), in_group = tile - group * tiles_m * 4;
     const int wide = min(tiles_n - group * 4, 4);
     const int tm = in_group / wide, tn = group * 4 + in_group - tm * wide;
-    const int m0 = tm * TM, n0 = tn * TN;
+    const int m0 = tm * kColumns, n0 = tn * TN;
 
-    const int steps_all = (p.k_dev ? *p.k_dev + kStep - 1 : p.k) / kStep;
+    const int steps_one = (p.k_dev ? *p.k_dev + kStep - 1 : p.k) / kStep, steps_all = E == kInput ? 2 * steps_one : steps_one;
     const int from = (int)((int64_t)steps_all * split / p.splits), to = (int)((int64_t)steps_all * (split + 1) / p.splits);
-    const int steps = to - from, total = SPLIT ? steps * 6 : kTurned ? steps * p.d_arrays : steps;
+    const int steps = to - from, total = SPLIT ? steps * 6 : E == kGradient ? steps * p.d_arrays : steps;
 
     // where this thread's 16-byte pieces come from (rows past the operand's last one read that one)
-    const char *a_base = static_cast<const char *>(p.a) + (kTurnedA ? (int64_t)m0 : (int64_t)m0 * p.a_ld + (int64_t)from * kStep) * 2;
+    const bool second = E == kGate && ((wave >> 1) & 1);   // this wavefront loads rows of the other projection
+    const int64_t a_ld = second ? p.ffn.a2_ld : p.a_ld, a_plane = second ? p.ffn.a2_plane : p.a_plane;
+    const char *a_base = static_cast<const char *>(second ? p.ffn.a2 : p.a);
+    if (E == kOuter) a_base += ((m0 >> 8) * p.ffn.a_panel + (m0 & 255)) * 2;
+    else a_base += (kTurnedA ? (int64_t)m0 : (int64_t)m0 * a_ld + (int64_t)from * kStep) * 2;
     const char *b_base = static_cast<const char *>(p.b);
     if (kTurned) b_base += ((n0 >> 8) * p.d_panel + (n0 & 255)) * 2;
     else if (kPanels) b_base += (int64_t)n0 * p.b_ld * 2;
     else b_base += ((int64_t)n0 * p.b_ld + (int64_t)from * kStep) * 2;
     unsigned a_off[kALoads], b_off[kBLoads];
+    int at_step = 0, at_product = 0;   // the next tiles to load
     const auto turned_a = [&](int rows) {   // of a step that a has `rows` rows for; and columns past its last piece read that one
 #pragma unroll
         for (int i = 0; i < kALoads; ++i) {
             const int c = tid + i * kThreads, row = c / kPiecesA, piece = c % kPiecesA;
             const int at = (piece >> 1 ^ turn_of(TM, row)) * 2 + (piece & 1);
-            a_off[i] = (unsigned)min(row, rows - 1) * (unsigned)(p.a_ld * 2) + (min(at, ((p.m + 7) >> 3) - 1 - (m0 >> 3)) << 4);
+            if constexpr (E == kOuter) {   // (a tile of 192 or 160 columns may lie in two panels)
+                const int col = (m0 & 255) + min(at, ((p.m + 7) >> 3) - 1 - (m0 >> 3)) * 8;
+                a_off[i] = (unsigned)min(row, rows - 1) * (unsigned)(p.a_ld * 2) +
+                           ((unsigned)(col >> 8) * (unsigned)p.ffn.a_panel + (col & 255) - (m0 & 255)) * 2;
+            } else {
+                const int64_t ld = E == kInput && from + at_step >= steps_one ? p.ffn.a2_ld : p.a_ld;
+                a_off[i] = (unsigned)min(row, rows - 1) * (unsigned)(ld * 2) + (min(at, ((p.m + 7) >> 3) - 1 - (m0 >> 3)) << 4);
+            }
+        }
+    };
+    const auto turned_b = [&](int rows) {   // the same of a b whose rows end where they end (kOuter)
+#pragma unroll
+        for (int i = 0; i < kBLoads; ++i) {
+            const int c = tid + i * kThreads, row = c / kPieces, piece = c % kPieces;
+            const int at = (piece >> 1 ^ turn_of(TN, row)) * 2 + (piece & 1);
+            b_off[i] = (unsigned)min(row, rows - 1) * (unsigned)(p.b_ld * 2) + (min(at, ((p.n + 7) >> 3) - 1 - (n0 >> 3)) << 4);
         }
     };
 #pragma unroll
     for (int i = 0; i < kALoads; ++i) {
         const int c = tid + i * kThreads, row = c >> 3;
-        if (!kTurnedA) a_off[i] = (unsigned)min(row, p.m - 1 - m0) * (unsigned)(p.a_ld * 2) + (((c & 7) ^ ((row >> 1) & 7)) << 4);
+        const int in_a = E == kGate ? (row >> 5) * 16 + (row & 15) : row;
+        if (!kTurnedA) a_off[i] = (unsigned)min(in_a, p.m - 1 - m0) * (unsigned)(a_ld * 2) + (((c & 7) ^ ((row >> 1) & 7)) << 4);
     }
 #pragma unroll
     for (int i = 0; i < kBLoads; ++i) {
         const int c = tid + i * kThreads;
-        if constexpr (kTurned) {   // (a panel has whole tiles of 64 rows)
+        if constexpr (E == kOuter) {
+            b_off[i] = 0;
+        } else if constexpr (kTurned) {   // (a panel has whole tiles of 64 rows)
             const int row = c / kPieces, piece = c % kPieces, turn = turn_of(TN, row);
             b_off[i] = (unsigned)row * (unsigned)(p.b_ld * 2) + (((piece >> 1 ^ turn) * 2 + (piece & 1)) << 4);
         } else {
@@ -222,27 +233,40 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
             b_off[i] = (unsigned)min(row, p.n - 1 - n0) * (unsigned)(p.b_ld * 2) + (((c & 7) ^ ((row >> 1) & 7)) << 4);
         }
     }
-    // The next tiles to load.  Where operands are three arrays: the six products of them that are kept, the smallest first.
-    int at_step = 0, at_product = 0;
+    // Where operands are three arrays: the six products of them that are kept, the smallest first.
     i32x4 a_from, b_from;   // buffer descriptors
     const auto descriptor = [](const char *base) {
         const uint64_t at = (uint64_t)base;
         return i32x4{__builtin_amdgcn_readfirstlane((int)(uint32_t)at),
                      __builtin_amdgcn_readfirstlane((int)(uint32_t)(at >> 32) & 0xffff), -1, 0x00020000};
     };
+    const int64_t a_to_a2 = E == kInput ? (int64_t)((uintptr_t)p.ffn.a2 - (uintptr_t)p.a) : 0;
     const auto aim = [&]() {
         int64_t a_at = 0, b_at = 0;
-        if (kTurned) b_at = (int64_t)(from + at_step) * kStep * 512;
+        if (E == kOuter) b_at = (int64_t)(from + at_step) * kStep * p.b_ld * 2;
+        else if (kTurned) b_at = (int64_t)(from + at_step) * kStep * 512;
         else if (kPanels) b_at = ((from + at_step) / kPanelSteps * p.d_panel + (from + at_step) % kPanelSteps * kStep) * 2;
-        if (kTurnedA) {
+        if constexpr (E == kInput) {   // (steps of the second product: its own weights, and the other half of b)
+            const int step = from + at_step, step_of = step >= steps_one ? step - steps_one : step, k = step_of * kStep;
+            b_at = (step_of / kPanelSteps * p.d_panel + step_of % kPanelSteps * kStep) * 2;
+            if (step >= steps_one) {
+                a_at = (int64_t)k * p.ffn.a2_ld * 2 + a_to_a2;
+                b_at += p.ffn.d_half * 2;
+            } else {
+                a_at = (int64_t)k * p.a_ld * 2;
+            }
+            if ((at_step == 0 || step_of == 0 || k + kStep > p.a_rows) && at_product == 0) turned_a(min(p.a_rows - k, kStep));
+        } else if (kTurnedA) {
             const int k = (from + at_step) * kStep;
             a_at = (int64_t)k * p.a_ld * 2;
+            if (E == kOuter && ((at_step == 0 && at_product == 0) || k + kStep > p.b_rows)) turned_b(min(p.b_rows - k, kStep));
             if ((at_step == 0 && at_product == 0) || k + kStep > p.a_rows) turned_a(min(p.a_rows - k, kStep));
         }
         if (SPLIT) {
-            a_at += ((0x021010 >> (4 * (5 - at_product))) & 15) * p.a_plane * 2;
+            a_at += ((0x021010 >> (4 * (5 - at_product))) & 15) *
+                    (E == kInput && from + at_step >= steps_one ? p.ffn.a2_plane : a_plane) * 2;
             b_at += ((0x201100 >> (4 * (5 - at_product))) & 15) * p.b_plane * 2;
-        } else if (kTurned) {
+        } else if (E == kGradient) {
             b_at += at_product * p.d_plane * 2;
         }
         a_from = descriptor(a_base + a_at);
@@ -258,11 +282,11 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
             return;
         }
         ++at_step;
-        if (kTurned && at_step == steps) {
+        if (E == kGradient && at_step == steps) {
             at_step = 0;
             ++at_product;
             aim();
-        } else if (kPanels) {   // (beyond an offset's 32 bits)
+        } else if (kAimed) {   // (beyond an offset's 32 bits)
             aim();
         }
     };
@@ -271,7 +295,7 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
         load_to_lds(a_from, a_off[i], kTurnedA ? 0 : at_step * kStepBytes, lds_at + stage + i * kThreads * 16);
     };
     const auto load_b = [&](int stage, int i) {
-        load_to_lds(b_from, b_off[i], kPanels ? 0 : at_step * kStepBytes, lds_at + kBAt + stage + i * kThreads * 16);
+        load_to_lds(b_from, b_off[i], kPanels || kTurned ? 0 : at_step * kStepBytes, lds_at + kBAt + stage + i * kThreads * 16);
     };
 
     f32x4 acc[MT][NT];
@@ -504,6 +528,15 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
                 *to_sum = p.add ? *to_sum + acc[i][j] : acc[i][j];
             }
         }
+    } else if constexpr (E >= kGate) {
+        __syncthreads();
+        float *own = reinterpret_cast<float *>(lds) + wave * epilogue_floats(MT);
+        const int m_wave = m0 + wm * MT * (E == kGate ? 8 : 16), n_wave = n0 + wn * NT * 16;
+        if constexpr (E == kGate) gate_epilogue<T, O, MT, NT, SPLIT>(p.ffn, acc, own, lane, m_wave, n_wave, n_rows, p.m);
+        else if constexpr (E == kGateGrad) gate_grad_epilogue<T, O, MT, NT, SPLIT>(p.ffn, acc, own, lane, m_wave, n_wave, n_rows, p.m);
+        else
+            out_epilogue<O, MT, NT>(p.ffn, acc, own, lane, m_wave, n_wave, n_rows, p.m, p.add, p.splits > 1 ? p.sums + split * p.sums_split : nullptr,
+                                    p.sums_ld);
     } else {
         const float alpha = p.scale * *p.out_scale;
         typedef O O4 __attribute__((ext_vector_type(4), aligned(sizeof(O))));

@@ -39,29 +39,30 @@ inline double cost_of(Shape shape, int64_t m, int64_t n, int64_t steps, int64_t 
            (rest > 0 && rest <= units ? kAloneStep * each + kAloneFixed : 0.0);
 }
 
-inline Shape shape_of(int64_t m, int64_t n, int64_t steps, int64_t splits, int64_t units)
+// `without`: shapes (their bits) that a product has no kernel for.
+inline Shape shape_of(int64_t m, int64_t n, int64_t steps, int64_t splits, int64_t units, unsigned without = 0)
 {
     if (n <= kFew) return kNarrow;
     Shape best = kLarge;
     for (int s = 1; s < kNarrow; ++s)
-        if (cost_of((Shape)s, m, n, steps, splits, units) < cost_of(best, m, n, steps, splits, units)) best = (Shape)s;
+        if (!(without >> s & 1) && cost_of((Shape)s, m, n, steps, splits, units) < cost_of(best, m, n, steps, splits, units)) best = (Shape)s;
     return best;
 }
 
-inline double least_cost(int64_t m, int64_t n, int64_t steps, int64_t splits, int64_t units)
+inline double least_cost(int64_t m, int64_t n, int64_t steps, int64_t splits, int64_t units, unsigned without = 0)
 {
-    return cost_of(shape_of(m, n, steps, splits, units), m, n, steps, splits, units);
+    return cost_of(shape_of(m, n, steps, splits, units, without), m, n, steps, splits, units);
 }
 
 // Parts that a sum over k is cut into, where its tiles leave compute units idle: each part's sums go to memory and are
 // joined later, so there are no more of them than shorten the whole by a twentieth.
-inline int splits_of(int64_t m, int64_t n, int64_t steps, int64_t units)
+inline int splits_of(int64_t m, int64_t n, int64_t steps, int64_t units, unsigned without = 0)
 {
     const int64_t tiles = up(m, 256) / 256 * (n <= kFew ? 1 : up(n, 256) / 256);
     int best = 1;
     double least = 1e30;
     for (int s = 1; s <= kMaxSplits && (s == 1 || (tiles * s <= 2 * units && steps >= s * 8)); s *= 2) {
-        const double t = least_cost(m, n, steps, s, units);
+        const double t = least_cost(m, n, steps, s, units, without);
         if (t < 0.95 * least) {
             least = t;
             best = s;

@@ -99,14 +99,64 @@ def _on_stream(method):
             raise ValueError(f"stream: one of {self.device} is wanted, got one of device {stream.device_index}")
         with torch.cuda.stream(stream):
             out = method(self, *args, **kwargs)
-        for t in (*args, *kwargs.values()):
-            if isinstance(t, torch.Tensor):
-                t.record_stream(stream)
+        _record((*args, *kwargs.values()), stream)
         return out
     return call
 
 
-class DeftEnds:
+def _record(values, stream):
+    for t in values:
+        if isinstance(t, torch.Tensor):
+            t.record_stream(stream)
+        elif isinstance(t, tuple):
+            _record(t, stream)
+
+
+class Marshalling:
+    """What the owners of handles share: `with`, calls and their errors, checks of tensors."""
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    def _call(self, name: str, arg) -> None:
+        if not self._h:
+            raise ValueError("the handle is closed")
+        rc = getattr(self._lib, name)(self._h, arg)
+        if rc != DEFT_OK:
+            raise DeftError(name, rc)
+
+    def _rows(self, name, t, rows, width):
+        """Checks a matrix of the handle's type whose rows lie apart as they like; gives its shape."""
+        return self._matrix(name, t, self.dtype, rows, width)
+
+    def _matrix(self, name, t, dtype, rows, width):
+        if not isinstance(t, torch.Tensor) or t.dim() != 2 or t.dtype != dtype or t.get_device() != self._index:
+            raise ValueError(f"{name}: a matrix of {dtype} on {self.device} is wanted")
+        n, w = t.shape
+        if n > _MOST or w > _MOST:
+            raise ValueError(f"{name}: sizes of 32 bits are wanted, got {(n, w)}")
+        if (rows is not None and n != rows) or (width is not None and w != width):
+            raise ValueError(f"{name}: shape {(n, w)} does not fit {(rows, width)}")
+        if not t.is_contiguous() and ((w > 1 and t.stride(1) != 1) or (n > 1 and t.stride(0) < w)):
+            raise ValueError(f"{name}: a row's elements have to be next to each other, rows apart")
+        return n, w
+
+    def _words(self, name, t, dtype, shape):
+        if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.get_device() != self._index or not t.is_contiguous():
+            raise ValueError(f"{name}: a contiguous tensor of {dtype} on {self.device} is wanted")
+        got = t.shape
+        if len(got) != len(shape) or any(g > _MOST or (s is not None and s != g) for s, g in zip(shape, got)):
+            raise ValueError(f"{name}: shape {tuple(got)} does not fit {shape}")
+        return got
+
+    def _stream(self) -> int:
+        return torch._C._cuda_getCurrentRawStream(self._index)
+
+
+class DeftEnds(Marshalling):
     """Owner of one deft_ends_t handle.
 
     `operators` names what the handle serves (keys of OPERATORS): it holds no scratch memory for
@@ -149,12 +199,6 @@ class DeftEnds:
             self._h = None   # (at the interpreter's end the module's names are gone)
 
     __del__ = close
-
-    def __enter__(self):
-        return self
-
-    def __exit__(self, *exc):
-        self.close()
 
     def info(self) -> deft_ends_info_t:
         info = deft_ends_info_t()
@@ -275,39 +319,6 @@ class DeftEnds:
             n, vocab, top_k, temperature, _p(logits), _ld(logits), _p(teacher_index), _p(teacher_logit),
             _p(row_grad), _p(loss), _p(grad_logits), _ld(grad_logits), _p(status), self._stream())))
         return loss, grad_logits
-
-    # ---- marshalling ------------------------------------------------------------------------
-
-    def _call(self, name: str, arg) -> None:
-        if not self._h:
-            raise ValueError("the handle is closed")
-        rc = getattr(self._lib, name)(self._h, arg)
-        if rc != DEFT_OK:
-            raise DeftError(name, rc)
-
-    def _rows(self, name, t, rows, width):
-        """Checks a matrix of the handle's type whose rows lie apart as they like; gives its shape."""
-        if not isinstance(t, torch.Tensor) or t.dim() != 2 or t.dtype != self.dtype or t.get_device() != self._index:
-            raise ValueError(f"{name}: a matrix of {self.dtype} on {self.device} is wanted")
-        n, w = t.shape
-        if n > _MOST or w > _MOST:
-            raise ValueError(f"{name}: sizes of 32 bits are wanted, got {(n, w)}")
-        if (rows is not None and n != rows) or (width is not None and w != width):
-            raise ValueError(f"{name}: shape {(n, w)} does not fit {(rows, width)}")
-        if not t.is_contiguous() and ((w > 1 and t.stride(1) != 1) or (n > 1 and t.stride(0) < w)):
-            raise ValueError(f"{name}: a row's elements have to be next to each other, rows apart")
-        return n, w
-
-    def _words(self, name, t, dtype, shape):
-        if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.get_device() != self._index or not t.is_contiguous():
-            raise ValueError(f"{name}: a contiguous tensor of {dtype} on {self.device} is wanted")
-        got = t.shape
-        if len(got) != len(shape) or any(g > _MOST or (s is not None and s != g) for s, g in zip(shape, got)):
-            raise ValueError(f"{name}: shape {tuple(got)} does not fit {shape}")
-        return got
-
-    def _stream(self) -> int:
-        return torch._C._cuda_getCurrentRawStream(self._index)
 
 
 def _p(t):
