@@ -50,12 +50,6 @@ __device__ __forceinline__ int checkpoint_code(float x, float s, float inverse)
     return is_finite(x) ? code + more - less : -128;
 }
 
-// The same up to the half of a step that x itself, a sum in 32 bits, is unsure of.
-__device__ __forceinline__ int checkpoint_code_of_sum(float x, float inverse, float most)
-{
-    return is_finite(x) ? (int)__builtin_rintf(fminf(fmaxf(x * inverse, -most), most)) : -(int)most - 1;
-}
-
 // What a code stands for, up to `most`, the largest number of its type: the nearest multiple of s may lie beyond.
 __device__ __forceinline__ float checkpoint_value(int code, float s, int none, float most)
 {

@@ -3,152 +3,204 @@
 //
 // All pass their sums through LDS, sixteen rows of a wavefront's tile at a time, so that a lane has eight
 // neighbouring columns of one row, what it loads and stores is 16 bytes, a row's lanes are next to each other, and a
-// checkpoint's group of 32 is four lanes'.
+// checkpoint's group of 32 is four lanes'.  What the derivatives' epilogue reads of the rows ahead is on its way meanwhile.
+//
+// Bound by vector instructions where tiles lie inside the matrix: about 30 an element for the derivatives.
 #pragma once
+#include <type_traits>
+
 #include "block.h"
 
 namespace deft {
 
 constexpr int kEight = 8;   // columns of a lane
 
-// What eight elements do: act(a), or act(a) and its derivative.  kExact: 32-bit outputs; otherwise exponentials and
-// reciprocals are the hardware's (off by 1 or 2 units of the last 24 bits, and |a| of them in the exponential), far below the
-// rounding to 16 bits that follows.
-template <bool kExact, bool kSlope>
-__device__ __forceinline__ void act_of(const float (&a)[kEight], int kind, float (&y)[kEight], float (&slope)[kEight])
+// An activation of the gate and its derivative.  kExact: 32-bit outputs; otherwise exponentials and reciprocals are the
+// hardware's (off by 1 or 2 units of the last 24 bits, and |a| of them in the exponential), far below the rounding to 16
+// bits that follows.
+template <int KIND, bool kExact>
+__device__ __forceinline__ void act_of(float a, float &y, float &slope)
 {
-    const auto exp_of = [](float x) { return kExact ? expf(x) : __expf(x); };
+    constexpr float kLog2e = 1.44269504f;
+    const auto exp_of = [](float x) { return kExact ? expf(x) : __builtin_amdgcn_exp2f(x * kLog2e); };
     const auto inverse = [](float x) { return kExact ? 1.0f / x : __builtin_amdgcn_rcpf(x); };
-    if (kind == DEFT_SILU) {
-#pragma unroll
-        for (int i = 0; i < kEight; ++i) {
-            const float p = inverse(1.0f + exp_of(-a[i]));
-            y[i] = a[i] * p;
-            if (kSlope) slope[i] = p * (1.0f + a[i] * (1.0f - p));
+    if constexpr (KIND == DEFT_SILU) {
+        const float p = inverse(1.0f + exp_of(-a));
+        y = a * p;
+        slope = fmaf(y, 1.0f - p, p);
+    } else if constexpr (KIND == DEFT_GELU) {
+        const float e = exp_of(-0.5f * a * a);
+        float p;   // the normal distribution's share below a
+        if constexpr (kExact) {
+            p = 0.5f * erfcf(-0.707106781f * a);
+        } else {
+            // Of the share beyond |a|: exp(-a^2 / 2) times a polynomial in 1 / (1 + 0.3 |a|), fitted to erfcx(|a| / sqrt 2) / 2 for
+            // |a| <= 14 (where 16-bit outputs are 0 beyond) with the least relative error, 8.5e-6 in 32 bits.
+            const float t = inverse(fmaf(0.3f, fabsf(a), 1.0f));
+            float q = -0.0770978130f;
+            q = fmaf(q, t, 0.216038091f);
+            q = fmaf(q, t, -0.0169490538f);
+            q = fmaf(q, t, 0.144196782f);
+            q = fmaf(q, t, 0.113741861f);
+            q = fmaf(q, t, 0.120074235f) * t * e;
+            p = a < 0.0f ? q : 1.0f - q;
         }
-    } else if (kind == DEFT_GELU) {
-#pragma unroll
-        for (int i = 0; i < kEight; ++i) {
-            const float p = 0.5f * erfcf(-0.707106781f * a[i]);
-            y[i] = a[i] * p;
-            if (kSlope) slope[i] = p + a[i] * (0.398942280f * exp_of(-0.5f * a[i] * a[i]));
-        }
-    } else if (kind == DEFT_GELU_TANH) {   // (1 + tanh(u / 2)) / 2 = 1 / (1 + exp(-u))
-#pragma unroll
-        for (int i = 0; i < kEight; ++i) {
-            const float square = a[i] * a[i], u = 1.595769122f * a[i] * (1.0f + 0.044715f * square), p = inverse(1.0f + exp_of(-u));
-            const float rest = p * (1.0f - p);   // (0 where the square may be infinite)
-            y[i] = a[i] * p;
-            if (kSlope) slope[i] = p + (rest == 0.0f ? 0.0f : rest * 1.595769122f * a[i] * (1.0f + 0.134145f * square));
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < kEight; ++i) {   // (NaN stays)
-            y[i] = a[i] < 0.0f ? 0.0f : a[i];
-            if (kSlope) slope[i] = a[i] > 0.0f ? 1.0f : 0.0f;
-        }
+        y = a * p;
+        slope = fmaf(a, 0.398942280f * e, p);
+    } else if constexpr (KIND == DEFT_GELU_TANH) {   // (1 + tanh(u / 2)) / 2 = 1 / (1 + exp(-u))
+        const float square = a * a, u = 1.595769122f * a * fmaf(0.044715f, square, 1.0f), p = inverse(1.0f + exp_of(-u));
+        const float rest = p - p * p;   // (0 where the square may be infinite)
+        y = a * p;
+        slope = p + (rest == 0.0f ? 0.0f : rest * 1.595769122f * a * fmaf(0.134145f, square, 1.0f));
+    } else {   // (NaN stays)
+        y = a < 0.0f ? 0.0f : a;
+        slope = a > 0.0f ? 1.0f : 0.0f;
     }
 }
+
+template <typename O> struct Eight {
+    typedef O type __attribute__((ext_vector_type(8), aligned(sizeof(O))));
+};
 
 // Eight elements of a row from column `at` on, where `cols` is the first that the row does not have (0: none of it is there).
-template <typename O>
-__device__ __forceinline__ void store_eight(O *row, int at, int cols, const float (&x)[kEight])
+// kInside: it has them all.
+template <bool kInside, typename O>
+__device__ __forceinline__ void store_eight(O *to, int at, int cols, const typename Eight<O>::type &y)
 {
-    typedef O O8 __attribute__((ext_vector_type(8), aligned(sizeof(O))));
-    if (at + kEight <= cols) {
-        O8 y;
-#pragma unroll
-        for (int r = 0; r < kEight; ++r) y[r] = (O)x[r];
-        *reinterpret_cast<O8 *>(row + at) = y;
+    if (kInside || at + kEight <= cols) {
+        *reinterpret_cast<typename Eight<O>::type *>(to) = y;
     } else {
 #pragma unroll
         for (int r = 0; r < kEight; ++r)
-            if (at + r < cols) row[at + r] = (O)x[r];
+            if (at + r < cols) to[r] = y[r];
     }
 }
 
-template <typename O>
-__device__ __forceinline__ void load_eight(const O *row, int at, int cols, float (&x)[kEight])
+template <bool kInside, typename O>
+__device__ __forceinline__ typename Eight<O>::type load_eight(const O *from, int at, int cols)
 {
-    typedef O O8 __attribute__((ext_vector_type(8), aligned(sizeof(O))));
-    if (at + kEight <= cols) {
-        const O8 y = *reinterpret_cast<const O8 *>(row + at);
-#pragma unroll
-        for (int r = 0; r < kEight; ++r) x[r] = (float)y[r];
-    } else {
-#pragma unroll
-        for (int r = 0; r < kEight; ++r) x[r] = at + r < cols ? (float)row[at + r] : 0.0f;
-    }
-}
-
-// The same as codes C of a checkpoint, whose group this and three neighbouring lanes hold.
-template <typename C>
-__device__ __forceinline__ void store_codes(const deft_checkpoint_t &to, int n, int at, int cols, const float (&x)[kEight])
-{
-    typedef C C8 __attribute__((ext_vector_type(8), aligned(sizeof(C))));
-    constexpr float kMost = sizeof(C) == 1 ? kCodes8 : kCodes16;
-    float top = 0.0f;
-#pragma unroll
-    for (int r = 0; r < kEight; ++r) top = fmaxf(top, at + r < cols && is_finite(x[r]) ? fabsf(x[r]) : 0.0f);
-    top = fmaxf(top, __shfl_xor(top, 1));
-    top = fmaxf(top, __shfl_xor(top, 2));
-    const float s = checkpoint_scale(top, kMost), inverse = 1.0f / s;
-    C8 y;
-#pragma unroll
-    for (int r = 0; r < kEight; ++r) y[r] = (C)checkpoint_code_of_sum(x[r], inverse, kMost);
-    C *row = static_cast<C *>(to.codes) + n * to.codes_stride;
-    if (at + kEight <= cols) {
-        *reinterpret_cast<C8 *>(row + at) = y;
+    typename Eight<O>::type y = {};
+    if (kInside || at + kEight <= cols) {
+        y = *reinterpret_cast<const typename Eight<O>::type *>(from);
     } else {
 #pragma unroll
         for (int r = 0; r < kEight; ++r)
-            if (at + r < cols) row[at + r] = y[r];
+            if (at + r < cols) y[r] = from[r];
     }
-    if (at % kGroup == 0 && at < cols) static_cast<bf16 *>(to.scales)[n * to.scales_stride + at / kGroup] = (bf16)s;   // (exactly)
+    return y;
 }
 
-template <typename C>
-__device__ __forceinline__ void load_codes(const deft_checkpoint_t &from, int n, int at, int cols, float (&x)[kEight])
+template <typename O>
+__device__ __forceinline__ typename Eight<O>::type rounded(const float (&x)[kEight])
 {
-    typedef C C8 __attribute__((ext_vector_type(8), aligned(sizeof(C))));
-    const C *row = static_cast<const C *>(from.codes) + n * from.codes_stride;
-    C8 y = {};
-    if (at + kEight <= cols) {
-        y = *reinterpret_cast<const C8 *>(row + at);
+    typename Eight<O>::type y;
+#pragma unroll
+    for (int r = 0; r < kEight; ++r) y[r] = (O)x[r];
+    return y;
+}
+
+// The largest of four neighbouring lanes.
+__device__ __forceinline__ unsigned quad_max(unsigned x)
+{
+    x = max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0xb1, 0xf, 0xf, true));
+    return max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x4e, 0xf, 0xf, true));
+}
+
+// Sums as codes C of a checkpoint, whose group this and three neighbouring lanes hold.  A group with a sum that is not finite
+// gets NaN as its scale.  Codes are the low bits of x / s + 3 2^22, rounded once to a whole number.
+template <bool kInside, typename C>
+__device__ __forceinline__ void store_codes(deft_checkpoint_t to, int n, int at, int cols, const float (&x)[kEight])
+{
+    constexpr bool k8 = sizeof(C) == 1;
+    constexpr float kLargest = k8 ? kCodes8 : kCodes16, kOver = k8 ? 1.0f / 127.0f : 1.0f / 32767.0f;
+    unsigned top = 0;   // (as whole numbers infinity is above all finite magnitudes and NaN above infinity)
+#pragma unroll
+    for (int r = 0; r < kEight; ++r) top = max(top, kInside || at + r < cols ? __float_as_uint(x[r]) & 0x7fffffffu : 0u);
+    top = quad_max(top);
+    float s = __uint_as_float((__float_as_uint(fmaxf(__uint_as_float(top) * kOver, 1.17549435e-38f)) + 0xffffu) & 0xffff0000u);
+    if (fmaf(s, kLargest, -__uint_as_float(top)) < 0.0f) s = __uint_as_float(__float_as_uint(s) + 0x10000u);   // (as in checkpoint_scale)
+    const float inverse = __builtin_amdgcn_rcpf(s);
+    unsigned c[kEight];
+#pragma unroll
+    for (int r = 0; r < kEight; ++r) c[r] = __float_as_uint(fmaf(x[r], inverse, 12582912.0f));
+    typename Eight<C>::type y;
+    if constexpr (k8) {
+        uint2 all;
+        all.x = __builtin_amdgcn_perm(__builtin_amdgcn_perm(c[3], c[2], 0x0c0c0400), __builtin_amdgcn_perm(c[1], c[0], 0x0c0c0400), 0x05040100);
+        all.y = __builtin_amdgcn_perm(__builtin_amdgcn_perm(c[7], c[6], 0x0c0c0400), __builtin_amdgcn_perm(c[5], c[4], 0x0c0c0400), 0x05040100);
+        y = __builtin_bit_cast(typename Eight<C>::type, all);
+    } else {
+        uint4 all;
+        all.x = __builtin_amdgcn_perm(c[1], c[0], 0x05040100);
+        all.y = __builtin_amdgcn_perm(c[3], c[2], 0x05040100);
+        all.z = __builtin_amdgcn_perm(c[5], c[4], 0x05040100);
+        all.w = __builtin_amdgcn_perm(c[7], c[6], 0x05040100);
+        y = __builtin_bit_cast(typename Eight<C>::type, all);
+    }
+    store_eight<kInside>(static_cast<C *>(to.codes) + n * to.codes_stride + at, at, cols, y);
+    if ((at & (kGroup - 1)) == 0 && (kInside || at < cols))
+        static_cast<unsigned short *>(to.scales)[n * to.scales_stride + at / kGroup] = top < 0x7f800000u ? __float_as_uint(s) >> 16 : 0x7fc0;
+}
+
+// A projection as it is kept: in 8 bits, or in as many as O has.
+template <bool kInside, typename O>
+__device__ __forceinline__ void store_saved(int kind, deft_checkpoint_t to, int n, int at, int cols, const float (&x)[kEight])
+{
+    if (kind == DEFT_SAVE_PACKED) store_codes<kInside, int8_t>(to, n, at, cols, x);
+    else if constexpr (sizeof(O) == 4) store_eight<kInside>(static_cast<float *>(to.codes) + n * to.codes_stride + at, at, cols, rounded<float>(x));
+    else store_codes<kInside, int16_t>(to, n, at, cols, x);
+}
+
+// Eight elements of it as they come from memory: codes of 8 bits in the first two words, of 16 in four, or floats.
+template <typename O> struct Kept {
+    static constexpr bool kFloats = sizeof(O) == 4;
+    unsigned words[kFloats ? 8 : 4];
+    unsigned short scale;
+};
+
+template <bool kInside, typename C, typename O>
+__device__ __forceinline__ void load_words(const C *from, int at, int cols, Kept<O> &k)
+{
+    const typename Eight<C>::type y = load_eight<kInside>(from, at, cols);
+    unsigned words[2 * sizeof(C)];
+    static_assert(sizeof(words) == sizeof(y));
+    __builtin_memcpy(words, &y, sizeof(words));
+#pragma unroll
+    for (unsigned i = 0; i < 2 * sizeof(C); ++i) k.words[i] = words[i];
+}
+
+template <bool kInside, typename O>
+__device__ __forceinline__ void load_saved(int kind, deft_checkpoint_t from, int n, int at, int cols, Kept<O> &k)
+{
+    if (kind == DEFT_SAVE_PACKED) load_words<kInside>(static_cast<const int8_t *>(from.codes) + n * from.codes_stride + at, at, cols, k);
+    else if constexpr (Kept<O>::kFloats) load_words<kInside>(static_cast<const float *>(from.codes) + n * from.codes_stride + at, at, cols, k);
+    else load_words<kInside>(static_cast<const int16_t *>(from.codes) + n * from.codes_stride + at, at, cols, k);
+    k.scale = 0;
+    if ((kind == DEFT_SAVE_PACKED || !Kept<O>::kFloats) && (kInside || at < cols))
+        k.scale = static_cast<const unsigned short *>(from.scales)[n * from.scales_stride + at / kGroup];
+}
+
+template <typename O>
+__device__ __forceinline__ void use_saved(int kind, const Kept<O> &k, float (&x)[kEight])
+{
+    const float s = __uint_as_float((unsigned)k.scale << 16);
+    if (kind == DEFT_SAVE_PACKED) {
+#pragma unroll
+        for (int r = 0; r < kEight; ++r) x[r] = (float)(int8_t)(k.words[r / 4] >> (8 * (r % 4))) * s;
+    } else if constexpr (Kept<O>::kFloats) {
+#pragma unroll
+        for (int r = 0; r < kEight; ++r) x[r] = __uint_as_float(k.words[r]);
     } else {
 #pragma unroll
-        for (int r = 0; r < kEight; ++r)
-            if (at + r < cols) y[r] = row[at + r];
+        for (int r = 0; r < kEight; ++r) x[r] = (float)(int16_t)(k.words[r / 2] >> (16 * (r % 2))) * s;
     }
-    const float s = at < cols ? (float)static_cast<const bf16 *>(from.scales)[n * from.scales_stride + at / kGroup] : 0.0f;
-#pragma unroll
-    for (int r = 0; r < kEight; ++r) x[r] = checkpoint_value(y[r], s, sizeof(C) == 1 ? -128 : -32768, 3.402823466e38f);
-}
-
-// The same of a projection as it is kept: in 8 bits, or in as many as O has.
-template <typename O>
-__device__ __forceinline__ void store_saved(int kind, const deft_checkpoint_t &to, int n, int at, int cols, const float (&x)[kEight])
-{
-    if (kind == DEFT_SAVE_PACKED) store_codes<int8_t>(to, n, at, cols, x);
-    else if constexpr (sizeof(O) == 4) store_eight(static_cast<float *>(to.codes) + n * to.codes_stride, at, cols, x);
-    else store_codes<int16_t>(to, n, at, cols, x);
-}
-
-template <typename O>
-__device__ __forceinline__ void load_saved(int kind, const deft_checkpoint_t &from, int n, int at, int cols, float (&x)[kEight])
-{
-    if (kind == DEFT_SAVE_PACKED) load_codes<int8_t>(from, n, at, cols, x);
-    else if constexpr (sizeof(O) == 4) load_eight(static_cast<const float *>(from.codes) + n * from.codes_stride, at, cols, x);
-    else load_codes<int16_t>(from, n, at, cols, x);
 }
 
 // Eight elements of an operand in panels: one array of T, or three of bf16 whose sum they are.
 template <typename T, bool SPLIT>
-__device__ __forceinline__ void store_operand(void *panels, int64_t panel, int64_t plane, int n, int at, int cols_up, const float (&x)[kEight])
+__device__ __forceinline__ void store_operand(T *to, int64_t plane, const float (&x)[kEight])
 {
     typedef T T8 __attribute__((ext_vector_type(8)));
-    if (at >= cols_up) return;
-    T *to = static_cast<T *>(panels) + (at >> 8) * panel + (int64_t)n * 256 + (at & 255);
     if constexpr (SPLIT) {
         T8 y[3];
 #pragma unroll
@@ -171,28 +223,69 @@ __device__ __forceinline__ void store_operand(void *panels, int64_t panel, int64
 constexpr __host__ __device__ int epilogue_pitch(int mt) { return mt * 16 + 4; }   // of a row of sums in LDS
 constexpr __host__ __device__ int epilogue_floats(int mt) { return 16 * epilogue_pitch(mt); }   // of a wavefront
 
-// Goes through a wavefront's tile sixteen rows at a time: its sums go to `lds` (the wavefront's own part), and `use` is called with a
-// row's number in the tile and where its sums lie, for every lane and kLanes lanes a row; kEach columns of sums belong to a
-// lane's eight elements.  acc[i][j][r] is row row16 + 16 j, column part * 4 + 16 i + r.
-template <int MT, int NT, int kEach, typename F>
-__device__ __forceinline__ void by_rows(const f32x4 (&acc)[MT][NT], float *lds, int lane, F use)
+template <int MT, int NT>
+__device__ __forceinline__ void to_lds(const f32x4 (&acc)[MT][NT], int j, float *to)
 {
-    constexpr int kPitch = epilogue_pitch(MT), kLanes = MT * 16 / kEach;
+#pragma unroll
+    for (int i = 0; i < MT; ++i) *reinterpret_cast<f32x4 *>(to + i * 16) = acc[i][j];
+}
+
+// Goes through a wavefront's tile sixteen rows at a time: its sums go to `lds` (the wavefront's own part), and `use(row, sums, ahead)` is
+// called with a row's number in the tile, where its sums lie, and what `fetch(row, ahead)` brought; the next sixteen rows' are fetched
+// meanwhile.  kLanes lanes have a row, each the same columns of all its rows.  acc[i][j][r] is row row16 + 16 j, column
+// part * 4 + 16 i + r.
+template <typename Ahead, int kLanes, int MT, int NT, typename Fetch, typename Use>
+__device__ __forceinline__ void by_rows(const f32x4 (&acc)[MT][NT], float *lds, int lane, Fetch fetch, Use use)
+{
+    static_assert(kLanes <= 16 && kWave % kLanes == 0);
+    constexpr int kPitch = epilogue_pitch(MT), kRows = kWave / kLanes, kTimes = 16 / kRows;
+    const int row16 = lane & 15, part = lane >> 4, own = lane / kLanes;
+    Ahead ahead[kTimes];
+#pragma unroll
+    for (int t = 0; t < kTimes; ++t) fetch(t * kRows + own, ahead[t]);
+#pragma clang loop unroll(disable)
+    for (int j = 0; j < NT; ++j) {
+#pragma unroll
+        for (int which = 0; which < NT; ++which)
+            if (j == which) {
+                to_lds(acc, which, lds + row16 * kPitch + part * 4);
+                asm volatile("; sixteen rows, number %0" ::"s"(which));   // (alike, the branches would become one that indexes registers in memory)
+            }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // (a wavefront's LDS accesses are done in order)
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int t = 0; t < kTimes; ++t) {
+            const int row = t * kRows + own;
+            const Ahead now = ahead[t];
+            if (j + 1 < NT) fetch((j + 1) * 16 + row, ahead[t]);
+            use(j * 16 + row, lds + row * kPitch, now);
+            __builtin_amdgcn_sched_barrier(0);   // (several rows' work at once would not fit the registers)
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// The same piece by piece of eight columns, rows of any number of pieces, nothing fetched.
+template <int kEach, int MT, int NT, typename Use>
+__device__ __forceinline__ void by_pieces(const f32x4 (&acc)[MT][NT], float *lds, int lane, Use use)
+{
+    constexpr int kPitch = epilogue_pitch(MT), kLanes = MT * 16 / kEach;   // kEach columns of sums make eight
     const int row16 = lane & 15, part = lane >> 4;
 #pragma clang loop unroll(disable)
     for (int j = 0; j < NT; ++j) {
 #pragma unroll
         for (int which = 0; which < NT; ++which)
             if (j == which) {
-#pragma unroll
-                for (int i = 0; i < MT; ++i) *reinterpret_cast<f32x4 *>(lds + row16 * kPitch + i * 16 + part * 4) = acc[i][which];
+                to_lds(acc, which, lds + row16 * kPitch + part * 4);
+                asm volatile("; sixteen rows, number %0" ::"s"(which));   // (alike, the branches would become one that indexes registers in memory)
             }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // (a wavefront's LDS accesses are done in order)
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
 #pragma clang loop unroll(disable)
         for (int at = lane; at < 16 * kLanes; at += kWave) {
             const int row = at / kLanes;
-            use(j * 16 + row, (at - row * kLanes) * 8, lds + row * kPitch);
+            use(j * 16 + row, (at - row * kLanes) * kEight, lds + row * kPitch);
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
@@ -209,59 +302,146 @@ __device__ __forceinline__ void read_eight(const float *from, float (&x)[kEight]
     }
 }
 
-// Sixteens of columns are gate and up in turn.  The wavefront's tile begins at row n_wave and, of either, column m_wave.  Rows
-// behind the last one and columns behind `cols` are zeros in h.
-template <typename T, typename O, int MT, int NT, bool SPLIT>
-__device__ __forceinline__ void gate_epilogue(const FfnArgs &f, const f32x4 (&acc)[MT][NT], float *lds, int lane, int m_wave, int n_wave, int n_rows, int cols)
+struct Nothing {};
+
+// All eight, whatever the activation is.
+template <bool kExact>
+__device__ __forceinline__ void act_of(int kind, const float (&a)[kEight], float (&y)[kEight], float (&slope)[kEight])
 {
-    static_assert(MT % 4 == 0);   // whole groups of 32
-    by_rows<MT, NT, 16>(acc, lds, lane, [&](int row, int col, const float *sums) {
-        const int n = n_wave + row, at = m_wave + col, own_cols = n < n_rows ? cols : 0;
-        float gate[kEight], up[kEight], h[kEight], none[kEight];
-        read_eight(sums + (col >> 4) * 32 + (col & 15), gate);
-        read_eight(sums + (col >> 4) * 32 + 16 + (col & 15), up);
-        if (f.saved.kind != DEFT_SAVE_NONE) {
-            store_saved<O>(f.saved.kind, f.saved.gate, n, at, own_cols, gate);
-            store_saved<O>(f.saved.kind, f.saved.up, n, at, own_cols, up);
-        }
-        if (!f.h) return;
-        act_of<SPLIT, false>(gate, f.activation, h, none);
 #pragma unroll
-        for (int r = 0; r < kEight; ++r) h[r] = at + r < own_cols ? h[r] * up[r] : 0.0f;
-        store_operand<T, SPLIT>(f.h, f.panel, f.h_plane, n, at, f.cols_up, h);
+    for (int r = 0; r < kEight; ++r) {
+        if (kind == DEFT_SILU) act_of<DEFT_SILU, kExact>(a[r], y[r], slope[r]);
+        else if (kind == DEFT_GELU) act_of<DEFT_GELU, kExact>(a[r], y[r], slope[r]);
+        else if (kind == DEFT_GELU_TANH) act_of<DEFT_GELU_TANH, kExact>(a[r], y[r], slope[r]);
+        else act_of<DEFT_RELU, kExact>(a[r], y[r], slope[r]);
+    }
+}
+
+// What a wavefront's tile is to the epilogues below.
+struct Tile {
+    float *lds;
+    int lane, m, n;      // its first column (of either projection) and row
+    int n_rows, cols;    // that the matrix has
+};
+
+// Eight elements of the first product's: `at` their column, own_cols the columns that their row has (0: no such row, zeros in h).
+template <bool kInside, typename T, typename O, bool SPLIT, typename Act>
+__device__ __forceinline__ void use_gate(const FfnArgs &f, const Tile &t, int row, int col, const float *sums, T *h_at, Act act)
+{
+    const int n = t.n + row, at = t.m + col, own_cols = kInside || n < t.n_rows ? t.cols : 0;
+    float gate[kEight], up[kEight], y[kEight], slope[kEight];
+    read_eight(sums + (col >> 4) * 32 + (col & 15), gate);   // (sixteens of columns are gate and up in turn)
+    read_eight(sums + (col >> 4) * 32 + 16 + (col & 15), up);
+    if (f.saved.kind != DEFT_SAVE_NONE) {
+        store_saved<kInside, O>(f.saved.kind, f.saved.gate, n, at, own_cols, gate);
+        store_saved<kInside, O>(f.saved.kind, f.saved.up, n, at, own_cols, up);
+    }
+    if (!f.h || (!kInside && at >= f.cols_up)) return;
+    act(gate, y, slope);
+#pragma unroll
+    for (int r = 0; r < kEight; ++r) y[r] = kInside || at + r < own_cols ? y[r] * up[r] : 0.0f;
+    store_operand<T, SPLIT>(h_at + (int64_t)n * 256, f.h_plane, y);
+}
+
+template <typename O> struct Ahead {
+    Kept<O> gate, up;
+};
+
+// And of the derivative's by h.
+template <bool kInside, typename T, typename O, bool SPLIT, typename Act>
+__device__ __forceinline__ void use_gate_grad(const FfnArgs &f, const Tile &t, int row, int col, const float *sums, const Ahead<O> &a, float factor, T *h_at,
+                                              T *d_at, Act act)
+{
+    const int n = t.n + row, at = t.m + col, own_cols = kInside || n < t.n_rows ? t.cols : 0;
+    if (!kInside && at >= f.cols_up) return;
+    float by_h[kEight], gate[kEight], up[kEight], y[kEight], slope[kEight], h[kEight];
+    read_eight(sums + col, by_h);
+    use_saved(f.saved.kind, a.gate, gate);
+    use_saved(f.saved.kind, a.up, up);
+    act(gate, y, slope);
+#pragma unroll
+    for (int r = 0; r < kEight; ++r) {
+        const bool here = kInside || at + r < own_cols;
+        const float d = __is_same(T, f16) ? by_h[r] * factor : by_h[r];
+        h[r] = here ? y[r] * up[r] : 0.0f;
+        gate[r] = here ? d * up[r] * slope[r] : 0.0f;
+        up[r] = here ? d * y[r] : 0.0f;
+    }
+    const int64_t from = (int64_t)n * 256;
+    if (f.h) store_operand<T, SPLIT>(h_at + from, f.h_plane, h);
+    if (f.d) {
+        store_operand<T, SPLIT>(d_at + from, f.d_plane, gate);
+        store_operand<T, SPLIT>(d_at + (f.cols_up >> 8) * f.panel + from, f.d_plane, up);
+    }
+}
+
+template <bool kInside, typename O>
+__device__ __forceinline__ void load_ahead(const FfnArgs &f, const Tile &t, int row, int col, Ahead<O> &a)
+{
+    const int n = t.n + row, at = t.m + col, own_cols = kInside || n < t.n_rows ? t.cols : 0;
+    load_saved<kInside>(f.saved.kind, f.saved.gate, n, at, own_cols, a.gate);
+    load_saved<kInside>(f.saved.kind, f.saved.up, n, at, own_cols, a.up);
+}
+
+// A tile that lies inside the matrix.
+template <bool kGrad, int KIND, typename T, typename O, int MT, int NT>
+__device__ __forceinline__ void act_inside(const FfnArgs &f, const f32x4 (&acc)[MT][NT], const Tile &t)
+{
+    constexpr int kLanes = kGrad ? MT * 2 : MT;
+    const int col = (t.lane % kLanes) * kEight, at = t.m + col;
+    const int64_t place = (at >> 8) * f.panel + (at & 255);
+    T *const h_at = static_cast<T *>(f.h) + place;
+    const auto act = [](const float (&a)[kEight], float (&y)[kEight], float (&slope)[kEight]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int r = 0; r < kEight; ++r) act_of<KIND, false>(a[r], y[r], slope[r]);
+    };
+    if constexpr (kGrad) {
+        T *const d_at = static_cast<T *>(f.d) + place;
+        const float factor = __is_same(T, f16) && f.factor ? f.factor[0] : 1.0f;
+        by_rows<Ahead<O>, kLanes>(
+            acc, t.lds, t.lane, [&](int row, Ahead<O> &a) __attribute__((always_inline)) { load_ahead<true>(f, t, row, col, a); },
+            [&](int row, const float *sums, const Ahead<O> &a) __attribute__((always_inline)) {
+                use_gate_grad<true, T, O, false>(f, t, row, col, sums, a, factor, h_at, d_at, act);
+            });
+    } else {
+        by_rows<Nothing, kLanes>(
+            acc, t.lds, t.lane, [](int, Nothing &) {},
+            [&](int row, const float *sums, const Nothing &) __attribute__((always_inline)) { use_gate<true, T, O, false>(f, t, row, col, sums, h_at, act); });
+    }
+}
+
+// One that ends beyond it.
+template <bool kGrad, typename T, typename O, int MT, int NT, bool SPLIT>
+__device__ __forceinline__ void act_edge(const FfnArgs &f, const f32x4 (&acc)[MT][NT], const Tile &t)
+{
+    const float factor = kGrad && __is_same(T, f16) && f.factor ? f.factor[0] : 1.0f;
+    const auto act = [&](const float (&a)[kEight], float (&y)[kEight], float (&slope)[kEight])
+        __attribute__((always_inline)) { act_of<SPLIT>(f.activation, a, y, slope); };
+    by_pieces<kGrad ? 8 : 16>(acc, t.lds, t.lane, [&](int row, int col, const float *sums) __attribute__((always_inline)) {
+        const int at = t.m + col;
+        const int64_t place = (at >> 8) * f.panel + (at & 255);
+        if constexpr (kGrad) {
+            Ahead<O> a = {};
+            load_ahead<false>(f, t, row, col, a);
+            use_gate_grad<false, T, O, SPLIT>(f, t, row, col, sums, a, factor, static_cast<T *>(f.h) + place, static_cast<T *>(f.d) + place, act);
+        } else {
+            use_gate<false, T, O, SPLIT>(f, t, row, col, sums, static_cast<T *>(f.h) + place, act);
+        }
     });
 }
 
-// The sums are the derivative by h.
-template <typename T, typename O, int MT, int NT, bool SPLIT>
-__device__ __forceinline__ void gate_grad_epilogue(const FfnArgs &f, const f32x4 (&acc)[MT][NT], float *lds, int lane, int m_wave, int n_wave, int n_rows,
-                                                   int cols)
+template <bool kGrad, typename T, typename O, int MT, int NT, bool SPLIT>
+__device__ __forceinline__ void act_epilogue(const FfnArgs &f, const f32x4 (&acc)[MT][NT], const Tile &t)
 {
-    static_assert(MT % 2 == 0);   // whole groups of 32
-    const float factor = f.factor ? f.factor[0] : 1.0f;
-    const int64_t behind = (int64_t)(f.cols_up >> 8) * f.panel;   // up's derivatives
-    by_rows<MT, NT, 8>(acc, lds, lane, [&](int row, int col, const float *sums) {
-        const int n = n_wave + row, at = m_wave + col, own_cols = n < n_rows ? cols : 0;
-        float gate[kEight], up[kEight], by_h[kEight], y[kEight], slope[kEight];
-        load_saved<O>(f.saved.kind, f.saved.gate, n, at, own_cols, gate);
-        load_saved<O>(f.saved.kind, f.saved.up, n, at, own_cols, up);
-        read_eight(sums + col, by_h);
-        act_of<SPLIT, true>(gate, f.activation, y, slope);
-        float h[kEight];
-#pragma unroll
-        for (int r = 0; r < kEight; ++r) {
-            const bool here = at + r < own_cols;
-            const float d = by_h[r] * factor;
-            h[r] = here ? y[r] * up[r] : 0.0f;
-            slope[r] = here ? d * up[r] * slope[r] : 0.0f;
-            y[r] = here ? d * y[r] : 0.0f;
-        }
-        if (f.h) store_operand<T, SPLIT>(f.h, f.panel, f.h_plane, n, at, f.cols_up, h);
-        if (f.d) {
-            store_operand<T, SPLIT>(f.d, f.panel, f.d_plane, n, at, f.cols_up, slope);
-            store_operand<T, SPLIT>(static_cast<T *>(f.d) + behind, f.panel, f.d_plane, n, at, f.cols_up, y);
-        }
-    });
+    static_assert(MT % 4 == 0);   // whole groups of 32
+    // (32-bit operands are multiplied six times over: theirs take a fiftieth of it either way)
+    if (SPLIT || t.n + NT * 16 > t.n_rows || t.m + MT * (kGrad ? 16 : 8) > t.cols) return act_edge<kGrad, T, O, MT, NT, SPLIT>(f, acc, t);
+    if constexpr (!SPLIT) {
+        if (f.activation == DEFT_SILU) act_inside<kGrad, DEFT_SILU, T, O, MT, NT>(f, acc, t);
+        else if (f.activation == DEFT_GELU) act_inside<kGrad, DEFT_GELU, T, O, MT, NT>(f, acc, t);
+        else if (f.activation == DEFT_GELU_TANH) act_inside<kGrad, DEFT_GELU_TANH, T, O, MT, NT>(f, acc, t);
+        else act_inside<kGrad, DEFT_RELU, T, O, MT, NT>(f, acc, t);
+    }
 }
 
 // Where row n of a product's result goes, or NULL.
@@ -274,14 +454,18 @@ __device__ __forceinline__ O *out_row(const FfnArgs &f, int n)
 }
 
 // A lane's columns of a row: out = x / factor, or that and what is there, rounded once.
-template <typename O>
+template <bool kInside, typename O>
 __device__ __forceinline__ void store_out(O *row, int at, int cols, const float (&x)[kEight], float alpha, int add)
 {
     float y[kEight] = {};
-    if (add) load_eight(row, at, cols, y);
+    if (add) {
+        const auto there = load_eight<kInside>(row + at, at, cols);
+#pragma unroll
+        for (int r = 0; r < kEight; ++r) y[r] = (float)there[r];
+    }
 #pragma unroll
     for (int r = 0; r < kEight; ++r) y[r] += alpha * x[r];
-    store_eight(row, at, cols, y);
+    store_eight<kInside>(row + at, at, cols, rounded<O>(y));
 }
 
 // The sums are the result, or a part of it (`sums`: rows of sums_ld elements, a multiple of 8).
@@ -290,17 +474,15 @@ __device__ __forceinline__ void out_epilogue(const FfnArgs &f, const f32x4 (&acc
                                              int add, float *sums, int64_t sums_ld)
 {
     const float alpha = f.factor ? f.factor[1] : 1.0f;
-    by_rows<MT, NT, 8>(acc, lds, lane, [&](int row, int col, const float *from) {
+    const auto use = [&](int row, int col, const float *from) __attribute__((always_inline)) {
         const int n = n_wave + row, at = m_wave + col;
         if (n >= n_rows || at >= cols) return;
         float x[kEight];
         read_eight(from + col, x);
-        if (sums) {
-            store_eight(sums + n * sums_ld, at, INT32_MAX, x);
-        } else if (O *to = out_row<O>(f, n)) {
-            store_out(to, at, cols, x, alpha, add);
-        }
-    });
+        if (sums) store_eight<true>(sums + n * sums_ld + at, at, cols, rounded<float>(x));
+        else if (O *to = out_row<O>(f, n)) store_out<false>(to, at, cols, x, alpha, add);
+    };
+    by_pieces<8>(acc, lds, lane, use);
 }
 
 }  // namespace deft

@@ -22,7 +22,7 @@
 namespace deft {
 namespace {
 
-constexpr unsigned kNoGate = 1u << kMiddle | 1u << kLow, kNoOther = 1u << kLow;   // shapes without a kernel
+constexpr unsigned kNoAct = 1u << kMiddle | 1u << kLow, kNoOther = 1u << kLow;   // shapes without a kernel
 
 struct JoinArgs {
     FfnArgs ffn;
@@ -44,21 +44,20 @@ __global__ void __launch_bounds__(256) join_out_kernel(JoinArgs a)
     float x[kEight] = {};
     int s = 0;
     for (; s + 4 <= a.splits; s += 4) {   // (eight loads under way)
-        float y[4][kEight];
+        Eight<float>::type y[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) load_eight(sums + (s + i) * a.sums_split, 0, kEight, y[i]);
+        for (int i = 0; i < 4; ++i) y[i] = load_eight<true>(sums + (s + i) * a.sums_split, 0, kEight);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int r = 0; r < kEight; ++r) x[r] += y[i][r];
     }
     for (; s < a.splits; ++s) {
-        float y[kEight];
-        load_eight(sums + s * a.sums_split, 0, kEight, y);
+        const Eight<float>::type y = load_eight<true>(sums + s * a.sums_split, 0, kEight);
 #pragma unroll
         for (int r = 0; r < kEight; ++r) x[r] += y[r];
     }
-    store_out(row, m, a.m, x, a.ffn.factor ? a.ffn.factor[1] : 1.0f, a.add);
+    store_out<false>(row, m, a.m, x, a.ffn.factor ? a.ffn.factor[1] : 1.0f, a.add);
 }
 
 // One call's view of the scratch memory.
@@ -97,7 +96,7 @@ struct Ffn {
     {
         switch (shape) {
         case kMiddle:
-            if constexpr (E != kGate) return product_shape<T, S, E, 2, 4, 6, 4, kSplit>(p, st);
+            if constexpr (E != kGate && E != kGateGrad) return product_shape<T, S, E, 2, 4, 6, 4, kSplit>(p, st);
             return hipErrorInvalidValue;
         case kHalf: return product_shape<T, S, E, 4, 2, 4, 4, kSplit>(p, st);
         case kSmall: return product_shape<T, S, E, 2, 2, 4, 4, kSplit>(p, st);
@@ -111,7 +110,7 @@ struct Ffn {
     static hipError_t allow()
     {
         hipError_t e = allow_shape<T, S, E, 2, 4, 8, 4, kSplit>();
-        if constexpr (E != kGate)
+        if constexpr (E != kGate && E != kGateGrad)
             if (e == hipSuccess) e = allow_shape<T, S, E, 2, 4, 6, 4, kSplit>();
         if (e == hipSuccess) e = allow_shape<T, S, E, 4, 2, 4, 4, kSplit>();
         if (e == hipSuccess) e = allow_shape<T, S, E, 2, 2, 4, 4, kSplit>();
@@ -197,7 +196,7 @@ struct Ffn {
         p.ffn.a2 = w_up.p;
         p.ffn.a2_ld = w_up.ld;
         p.ffn.a2_plane = w_up.plane;
-        return product<kGate>(p, shape_of(2 * (int64_t)inner, n, (int64_t)(p.k / kStep) * (kSplit ? 6 : 1), 1, compute_units, kNoGate), st);
+        return product<kGate>(p, shape_of(2 * (int64_t)inner, n, (int64_t)(p.k / kStep) * (kSplit ? 6 : 1), 1, compute_units, kNoAct), st);
     }
 
     // A product whose sums are the result: cut into parts where that is quicker.
@@ -303,7 +302,7 @@ struct Ffn {
                 p.ffn = f;
                 p.ffn.h = a.grad_down ? s.h : nullptr;
                 p.ffn.d = by_projections ? s.d : nullptr;
-                e = product<kGateGrad>(p, shape_of(a.inner, n, (int64_t)(p.k / kStep) * (kSplit ? 6 : 1), 1, compute_units, kNoOther), st);
+                e = product<kGateGrad>(p, shape_of(a.inner, n, (int64_t)(p.k / kStep) * (kSplit ? 6 : 1), 1, compute_units, kNoAct), st);
             }
         }
         const bool weights = n > 0 || !a.accumulate;

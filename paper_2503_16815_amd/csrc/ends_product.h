@@ -532,8 +532,8 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
         __syncthreads();
         float *own = reinterpret_cast<float *>(lds) + wave * epilogue_floats(MT);
         const int m_wave = m0 + wm * MT * (E == kGate ? 8 : 16), n_wave = n0 + wn * NT * 16;
-        if constexpr (E == kGate) gate_epilogue<T, O, MT, NT, SPLIT>(p.ffn, acc, own, lane, m_wave, n_wave, n_rows, p.m);
-        else if constexpr (E == kGateGrad) gate_grad_epilogue<T, O, MT, NT, SPLIT>(p.ffn, acc, own, lane, m_wave, n_wave, n_rows, p.m);
+        if constexpr (E == kGate || E == kGateGrad)
+            act_epilogue<E == kGateGrad, T, O, MT, NT, SPLIT>(p.ffn, acc, Tile{own, lane, m_wave, n_wave, n_rows, p.m});
         else
             out_epilogue<O, MT, NT>(p.ffn, acc, own, lane, m_wave, n_wave, n_rows, p.m, p.add, p.splits > 1 ? p.sums + split * p.sums_split : nullptr,
                                     p.sums_ld);
