@@ -27,33 +27,44 @@ struct FfnArgs {
 
 constexpr int kGroup = DEFT_CHECKPOINT_GROUP;
 
+// How a workgroup of 256 threads goes through rows' pieces of eight elements: whole rows, at least 256 pieces.
+struct RowPieces {
+    int pieces, first, count;    // of a row; its first row; pieces in all
+    float one_by;
+    static __host__ __device__ int pieces_of(int cols) { return (cols + 7) / 8; }
+    static __host__ __device__ int rows_each(int cols) { return (256 + pieces_of(cols) - 1) / pieces_of(cols); }
+    static unsigned blocks(int64_t rows, int cols) { return (unsigned)((rows + rows_each(cols) - 1) / rows_each(cols)); }
+    __device__ RowPieces(unsigned block, int rows, int cols) : pieces(pieces_of(cols)), first((int)block * rows_each(cols))
+    {
+        count = min(rows - first, rows_each(cols)) * pieces;
+        one_by = 1.0f / (float)pieces;
+    }
+    // (a whole number less than 2^15 and a half, divided: never within the error of a whole number)
+    __device__ int in_block(int i) const { return (int)(((float)i + 0.5f) * one_by); }
+    __device__ int row(int i) const { return first + in_block(i); }
+    __device__ int piece(int i) const { return i - in_block(i) * pieces; }
+};
+
 constexpr float kCodes8 = 127.0f, kCodes16 = 32767.0f;   // the largest codes
+constexpr float kShift = 12582912.0f;   // 3 2^22: a sum with it is a whole number, in the low bits
 
 // The scale of a group: the smallest number of 8 significant bits, at least 2^-126, `most` times which reaches `top`.
-__device__ __forceinline__ float checkpoint_scale(float top, float most)
+// (`one_by`: 1 / most.  The product's rounding, and the divisor's, may end a step of 8 bits beside it: both neighbours are tried.)
+__device__ __forceinline__ float checkpoint_scale(float top, float most, float one_by)
 {
-    const auto up8 = [](float x) { return __uint_as_float((__float_as_uint(x) + 0xffffu) & 0xffff0000u); };
-    const float s = up8(fmaxf(top / most, 1.17549435e-38f));
-    // (where the quotient's rounding went down to a number of 8 bits)
-    return fmaf(s, most, -top) < 0.0f ? __uint_as_float(__float_as_uint(s) + 0x10000u) : s;
+    constexpr float kLeast = 1.17549435e-38f;
+    const unsigned up8 = (__float_as_uint(fmaxf(top * one_by, kLeast)) + 0xffffu) & 0xffff0000u;
+    const float s = __uint_as_float(up8), below = __uint_as_float(up8 - 0x10000u), above = __uint_as_float(up8 + 0x10000u);
+    if (fmaf(s, most, -top) < 0.0f) return above;
+    return below >= kLeast && fmaf(below, most, -top) >= 0.0f ? below : s;
 }
 
 __device__ __forceinline__ bool is_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
 
-// The whole number nearest to x / s, ties to the even one, given 1 / s: x - q s is exact, and tells where the quotient's
-// rounding brought x / s onto a half or away from one.
-__device__ __forceinline__ int checkpoint_code(float x, float s, float inverse)
-{
-    const float q = __builtin_rintf(x * inverse), twice = 2.0f * fmaf(-q, s, x);
-    const int code = (int)q, odd = code & 1;
-    const int more = twice > s || (odd && twice == s), less = twice < -s || (odd && twice == -s);
-    return is_finite(x) ? code + more - less : -128;
-}
-
 // What a code stands for, up to `most`, the largest number of its type: the nearest multiple of s may lie beyond.
-__device__ __forceinline__ float checkpoint_value(int code, float s, int none, float most)
+__device__ __forceinline__ float checkpoint_value(int code, float s, float most)
 {
-    return code == none ? __builtin_nanf("") : fminf(fmaxf((float)code * s, -most), most);
+    return code == -128 ? __builtin_nanf("") : fminf(fmaxf((float)code * s, -most), most);
 }
 
 // ---- launches (each returns hipGetLastError() of its launches) ------------------------------

@@ -6,7 +6,7 @@
 // One scale for 32 elements: an element that is many times as large as its neighbours costs 31 others their bits.  Scales of
 // 8 significant bits: powers of two alone (half a byte less for 32 elements) would make the step larger by 1.47 in the
 // root mean square.  Bound by memory, read and written once: four neighbouring lanes hold a group, 8 elements each.
-#include "block.h"
+#include "block_epilogue.h"
 
 namespace deft {
 namespace {
@@ -18,47 +18,54 @@ struct StoreArgs {
     deft_checkpoint_t out;
 };
 
-typedef int8_t codes8 __attribute__((ext_vector_type(8), aligned(1)));
-
 template <typename S>
 __global__ void __launch_bounds__(256) store_kernel(StoreArgs a)
 {
-    typedef S S8 __attribute__((ext_vector_type(8), aligned(sizeof(S))));
-    const unsigned pieces = (unsigned)((a.width + kGroup - 1) / kGroup) * 4;   // of 8 elements, of a row's groups
-    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t row = at / pieces;
-    const int piece = (int)(at - row * pieces), col = piece * 8;
-    if (row >= a.rows) return;   // (whole groups of four lanes)
-    const S *from = static_cast<const S *>(a.x) + row * a.x_stride + col;
-    float x[8] = {};
-    const bool whole = col + 8 <= a.width;
-    if (whole) {
-        const S8 v = *reinterpret_cast<const S8 *>(from);
+    // (whole groups of four lanes)
+    const RowPieces by(blockIdx.x, a.rows, (a.width + kGroup - 1) / kGroup * kGroup);
+    for (int i = threadIdx.x; i < by.count; i += 256) {
+        const int64_t row = by.row(i);
+        const int at = by.piece(i) * kEight;
+        const typename Eight<S>::type v = load_eight<false>(static_cast<const S *>(a.x) + row * a.x_stride + at, at, a.width);
+        float x[kEight];
+        unsigned own = 0;   // (as whole numbers infinity is above all finite magnitudes and NaN above infinity)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = (float)v[i];
-    } else {
+        for (int r = 0; r < kEight; ++r) {
+            x[r] = (float)v[r];
+            own = max(own, __float_as_uint(x[r]) & 0x7fffffffu);
+        }
+        unsigned top = quad_max(own);
+        const bool all_finite = top < 0x7f800000u;
+        if (!all_finite) {   // the others' largest
+            own = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (col + i < a.width) x[i] = (float)from[i];
+            for (int r = 0; r < kEight; ++r) own = max(own, is_finite(x[r]) ? __float_as_uint(x[r]) & 0x7fffffffu : 0u);
+            top = quad_max(own);
+        }
+        const float s = checkpoint_scale(__uint_as_float(top), kCodes8, 1.0f / kCodes8), inverse = __builtin_amdgcn_rcpf(s), half = 0.5f * s;
+        // x / s rounded by way of 1 / s; what is left of x, which is exact, tells whether that ended on a half or beyond
+        unsigned code[kEight];
+        bool nearest = all_finite;
+#pragma unroll
+        for (int r = 0; r < kEight; ++r) {
+            const float shifted = fmaf(x[r], inverse, kShift), left = fmaf(kShift - shifted, s, x[r]);
+            code[r] = __float_as_uint(shifted);
+            nearest = nearest && fabsf(left) < half;
+        }
+        if (!nearest) {
+#pragma unroll
+            for (int r = 0; r < kEight; ++r) {
+                const float left = fmaf(kShift - __uint_as_float(code[r]), s, x[r]);
+                const bool odd = code[r] & 1;
+                const int more = left > half || (odd && left == half), less = left < -half || (odd && left == -half);
+                code[r] = is_finite(x[r]) ? code[r] + (unsigned)(more - less) : 0x80u;
+            }
+        }
+        const uint2 all = make_uint2(pack_bytes(code[0], code[1], code[2], code[3]), pack_bytes(code[4], code[5], code[6], code[7]));
+        store_eight<false>(static_cast<int8_t *>(a.out.codes) + row * a.out.codes_stride + at, at, a.width,
+                           __builtin_bit_cast(Eight<int8_t>::type, all));
+        if ((at & (kGroup - 1)) == 0) static_cast<unsigned short *>(a.out.scales)[row * a.out.scales_stride + at / kGroup] = __float_as_uint(s) >> 16;
     }
-    float top = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) top = fmaxf(top, is_finite(x[i]) ? fabsf(x[i]) : 0.0f);
-    top = fmaxf(top, __shfl_xor(top, 1));
-    top = fmaxf(top, __shfl_xor(top, 2));
-    const float s = checkpoint_scale(top, kCodes8), inverse = 1.0f / s;
-    int8_t *to = static_cast<int8_t *>(a.out.codes) + row * a.out.codes_stride + col;
-    codes8 y;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = (int8_t)checkpoint_code(x[i], s, inverse);
-    if (whole) {
-        *reinterpret_cast<codes8 *>(to) = y;
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (col + i < a.width) to[i] = y[i];
-    }
-    if ((piece & 3) == 0) static_cast<bf16 *>(a.out.scales)[row * a.out.scales_stride + (piece >> 2)] = (bf16)s;   // (exactly)
 }
 
 template <typename S> constexpr float kMost = 3.402823466e38f;
@@ -69,57 +76,38 @@ template <> constexpr float kMost<bf16> = 3.38953139e38f;
 template <typename S, typename T, int P>
 __global__ void __launch_bounds__(256) restore_kernel(RestoreArgs a)
 {
-    typedef T T8 __attribute__((ext_vector_type(8), aligned(sizeof(T))));
-    const unsigned pieces = (unsigned)((a.cols_to + 7) >> 3);
-    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t row = at / pieces;
-    const int col = (int)(at - row * pieces) * 8;
-    if (row >= a.rows_to) return;
-    float x[8] = {};
-    if (row < a.rows && col < a.cols) {
-        const int8_t *from = static_cast<const int8_t *>(a.from.codes) + row * a.from.codes_stride + col;
-        const float s = (float)static_cast<const bf16 *>(a.from.scales)[row * a.from.scales_stride + col / kGroup];
-        if (col + 8 <= a.cols) {
-            const codes8 v = *reinterpret_cast<const codes8 *>(from);
+    const RowPieces by(blockIdx.x, a.rows_to, a.cols_to);
+    for (int i = threadIdx.x; i < by.count; i += 256) {
+        const int64_t row = by.row(i);
+        const int at = by.piece(i) * kEight;
+        float x[kEight] = {};
+        if (row < a.rows && at < a.cols) {
+            const float s = (float)static_cast<const bf16 *>(a.from.scales)[row * a.from.scales_stride + at / kGroup];
+            const Eight<int8_t>::type v = load_eight<false>(static_cast<const int8_t *>(a.from.codes) + row * a.from.codes_stride + at, at, a.cols);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = checkpoint_value(v[i], s, -128, kMost<S>);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (col + i < a.cols) x[i] = checkpoint_value(from[i], s, -128, kMost<S>);
+            for (int r = 0; r < kEight; ++r) x[r] = checkpoint_value(v[r], s, kMost<S>);
         }
-    }
-    T8 y[P];
+        typename Eight<T>::type y[P];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        if constexpr (P == 3) {
-            bf16 p[3];
-            split3((float)(S)x[i], p);
+        for (int r = 0; r < kEight; ++r) {
+            if constexpr (P == 3) {
+                bf16 p[3];
+                split3(x[r], p);
 #pragma unroll
-            for (int k = 0; k < 3; ++k) y[k][i] = p[k];
-        } else {
-            y[0][i] = (T)x[i];
+                for (int k = 0; k < 3; ++k) y[k][r] = p[k];
+            } else {
+                y[0][r] = (T)x[r];
+            }
         }
-    }
 #pragma unroll
-    for (int k = 0; k < P; ++k) {
-        T *to = static_cast<T *>(a.out) + k * a.out_plane + row * a.out_ld + col;
-        if (col + 8 <= a.cols_to) {
-            *reinterpret_cast<T8 *>(to) = y[k];
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (col + i < a.cols_to) to[i] = y[k][i];
-        }
+        for (int k = 0; k < P; ++k) store_eight<false>(static_cast<T *>(a.out) + k * a.out_plane + row * a.out_ld + at, at, a.cols_to, y[k]);
     }
 }
-
-unsigned blocks_of(int64_t rows, int64_t pieces) { return (unsigned)((rows * pieces + 255) / 256); }
 
 template <typename S, typename T, int P>
 hipError_t restore(const RestoreArgs &a, hipStream_t st)
 {
-    restore_kernel<S, T, P><<<blocks_of(a.rows_to, (a.cols_to + 7) >> 3), 256, 0, st>>>(a);
+    restore_kernel<S, T, P><<<RowPieces::blocks(a.rows_to, a.cols_to), 256, 0, st>>>(a);
     return hipGetLastError();
 }
 
@@ -128,7 +116,7 @@ hipError_t restore(const RestoreArgs &a, hipStream_t st)
 hipError_t checkpoint_launch(int dtype, const deft_checkpoint_call_t &c, hipStream_t st)
 {
     const StoreArgs a = {c.n_rows, c.width, c.x, c.x_stride, c.out};
-    const unsigned blocks = blocks_of(a.rows, (int64_t)(a.width + kGroup - 1) / kGroup * 4);
+    const unsigned blocks = RowPieces::blocks(a.rows, (a.width + kGroup - 1) / kGroup * kGroup);
     if (dtype == DEFT_F32) store_kernel<float><<<blocks, 256, 0, st>>>(a);
     else if (dtype == DEFT_F16) store_kernel<f16><<<blocks, 256, 0, st>>>(a);
     else store_kernel<bf16><<<blocks, 256, 0, st>>>(a);

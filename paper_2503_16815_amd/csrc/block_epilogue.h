@@ -106,28 +106,33 @@ __device__ __forceinline__ unsigned quad_max(unsigned x)
     return max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x4e, 0xf, 0xf, true));
 }
 
+// The low bytes of four numbers.
+__device__ __forceinline__ unsigned pack_bytes(unsigned a, unsigned b, unsigned c, unsigned d)
+{
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400), __builtin_amdgcn_perm(b, a, 0x0c0c0400), 0x05040100);
+}
+
 // Sums as codes C of a checkpoint, whose group this and three neighbouring lanes hold.  A group with a sum that is not finite
-// gets NaN as its scale.  Codes are the low bits of x / s + 3 2^22, rounded once to a whole number.
+// gets NaN as its scale.  Codes are the low bits of x / s + 3 2^22, rounded once (a sum in 32 bits is itself unsure of a half).
 template <bool kInside, typename C>
 __device__ __forceinline__ void store_codes(deft_checkpoint_t to, int n, int at, int cols, const float (&x)[kEight])
 {
     constexpr bool k8 = sizeof(C) == 1;
-    constexpr float kLargest = k8 ? kCodes8 : kCodes16, kOver = k8 ? 1.0f / 127.0f : 1.0f / 32767.0f;
+    constexpr float kLargest = k8 ? kCodes8 : kCodes16;
     unsigned top = 0;   // (as whole numbers infinity is above all finite magnitudes and NaN above infinity)
 #pragma unroll
     for (int r = 0; r < kEight; ++r) top = max(top, kInside || at + r < cols ? __float_as_uint(x[r]) & 0x7fffffffu : 0u);
     top = quad_max(top);
-    float s = __uint_as_float((__float_as_uint(fmaxf(__uint_as_float(top) * kOver, 1.17549435e-38f)) + 0xffffu) & 0xffff0000u);
-    if (fmaf(s, kLargest, -__uint_as_float(top)) < 0.0f) s = __uint_as_float(__float_as_uint(s) + 0x10000u);   // (as in checkpoint_scale)
+    const float s = checkpoint_scale(__uint_as_float(top), kLargest, 1.0f / kLargest);
     const float inverse = __builtin_amdgcn_rcpf(s);
     unsigned c[kEight];
 #pragma unroll
-    for (int r = 0; r < kEight; ++r) c[r] = __float_as_uint(fmaf(x[r], inverse, 12582912.0f));
+    for (int r = 0; r < kEight; ++r) c[r] = __float_as_uint(fmaf(x[r], inverse, kShift));
     typename Eight<C>::type y;
     if constexpr (k8) {
         uint2 all;
-        all.x = __builtin_amdgcn_perm(__builtin_amdgcn_perm(c[3], c[2], 0x0c0c0400), __builtin_amdgcn_perm(c[1], c[0], 0x0c0c0400), 0x05040100);
-        all.y = __builtin_amdgcn_perm(__builtin_amdgcn_perm(c[7], c[6], 0x0c0c0400), __builtin_amdgcn_perm(c[5], c[4], 0x0c0c0400), 0x05040100);
+        all.x = pack_bytes(c[0], c[1], c[2], c[3]);
+        all.y = pack_bytes(c[4], c[5], c[6], c[7]);
         y = __builtin_bit_cast(typename Eight<C>::type, all);
     } else {
         uint4 all;

@@ -16,7 +16,7 @@
 // 16-bit floats hold d_gate and d_up times a power of two that brings the largest of dy to 1 .. 2: the gradient of a mean over many
 // tokens is far below 1, and so out of their range's reach of 2^-14.
 #pragma once
-#include "block.h"
+#include "block_few.h"
 #include "ends_operands.h"
 
 namespace deft {
@@ -34,30 +34,30 @@ struct JoinArgs {
 template <typename O>
 __global__ void __launch_bounds__(256) join_out_kernel(JoinArgs a)
 {
-    const int64_t pieces = (a.m + kEight - 1) / kEight, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t n = at / pieces;
-    if (n >= a.n) return;
-    O *row = out_row<O>(a.ffn, (int)n);
-    if (!row) return;
-    const int m = (int)(at - n * pieces) * kEight;
-    const float *sums = a.sums + n * a.sums_ld + m;
-    float x[kEight] = {};
-    int s = 0;
-    for (; s + 4 <= a.splits; s += 4) {   // (eight loads under way)
-        Eight<float>::type y[4];
+    const RowPieces by(blockIdx.x, a.n, a.m);
+    for (int i = threadIdx.x; i < by.count; i += 256) {
+        const int n = by.row(i), m = by.piece(i) * kEight;
+        O *row = out_row<O>(a.ffn, n);
+        if (!row) continue;
+        const float *sums = a.sums + n * a.sums_ld + m;
+        float x[kEight] = {};
+        int s = 0;
+        for (; s + 4 <= a.splits; s += 4) {   // (eight loads under way)
+            Eight<float>::type y[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) y[i] = load_eight<true>(sums + (s + i) * a.sums_split, 0, kEight);
+            for (int k = 0; k < 4; ++k) y[k] = load_eight<true>(sums + (s + k) * a.sums_split, 0, kEight);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+            for (int k = 0; k < 4; ++k)
 #pragma unroll
-            for (int r = 0; r < kEight; ++r) x[r] += y[i][r];
+                for (int r = 0; r < kEight; ++r) x[r] += y[k][r];
+        }
+        for (; s < a.splits; ++s) {
+            const Eight<float>::type y = load_eight<true>(sums + s * a.sums_split, 0, kEight);
+#pragma unroll
+            for (int r = 0; r < kEight; ++r) x[r] += y[r];
+        }
+        store_out<false>(row, m, a.m, x, a.ffn.factor ? a.ffn.factor[1] : 1.0f, a.add);
     }
-    for (; s < a.splits; ++s) {
-        const Eight<float>::type y = load_eight<true>(sums + s * a.sums_split, 0, kEight);
-#pragma unroll
-        for (int r = 0; r < kEight; ++r) x[r] += y[r];
-    }
-    store_out<false>(row, m, a.m, x, a.ffn.factor ? a.ffn.factor[1] : 1.0f, a.add);
 }
 
 // One call's view of the scratch memory.
@@ -128,26 +128,37 @@ struct Ffn {
         return e;
     }
 
-    // Rows as the products read them: where they are, or packed.  `along`: a product has their elements as its k, beside those
-    // that have them as m or n (whole pieces of 16 bytes are enough for these).
-    static hipError_t operand(const void *p, int64_t stride, int rows, int cols, bool along, void *packed, Operand *out, hipStream_t st)
-    {
-        if (!kSplit && in_place(p, stride, cols, along ? kStep : 8)) {
-            *out = {p, stride, 0};
-            return hipSuccess;
+    // Rows as the products read them: where they are, or packed, by one launch for all that a call needs so.  `along`: a product
+    // has their elements as its k, beside those that have them as m or n (whole pieces of 16 bytes are enough for these).
+    struct Packing {
+        PackMany many{};
+        int count = 0;
+        unsigned blocks = 0;
+
+        static bool as_is(const void *p, int64_t stride, int cols, bool along) { return !kSplit && in_place(p, stride, cols, along ? kStep : 8); }
+
+        Operand operand(const void *p, int64_t stride, int rows, int cols, bool along, void *packed)
+        {
+            if (as_is(p, stride, cols, along)) return {p, stride, 0};
+            PackArgs &a = many.of[count];
+            a.src = p;
+            a.src_stride = stride;
+            a.rows = rows;
+            a.cols = cols;
+            a.out = packed;
+            a.out_ld = up(cols, kStep);
+            a.out_plane = up(rows, kTile) * a.out_ld;
+            blocks += many.blocks[count++] = pack_blocks(up(rows, kTile), a.out_ld);
+            return {packed, a.out_ld, a.out_plane};
         }
-        PackArgs a{};
-        a.src = p;
-        a.src_stride = stride;
-        a.rows = rows;
-        a.cols = cols;
-        a.out = packed;
-        a.out_ld = up(cols, kStep);
-        a.out_plane = up(rows, kTile) * a.out_ld;
-        *out = {packed, a.out_ld, a.out_plane};
-        pack_rows_kernel<S, T, P><<<(unsigned)(up(a.out_plane >> 3, 1024) / 1024), 256, 0, st>>>(a);
-        return hipGetLastError();
-    }
+
+        hipError_t launch(hipStream_t st) const
+        {
+            if (blocks == 0) return hipSuccess;
+            pack_many_kernel<S, T, P><<<blocks, 256, 0, st>>>(many);
+            return hipGetLastError();
+        }
+    };
 
     static hipError_t restored(const deft_checkpoint_t &from, int rows, int cols, int dtype, void *packed, Operand *out, hipStream_t st)
     {
@@ -219,17 +230,49 @@ struct Ffn {
         j.sums = p.sums;
         j.sums_ld = p.sums_ld;
         j.sums_split = p.sums_split;
-        join_out_kernel<S><<<(unsigned)(up((int64_t)p.n * ((p.m + kEight - 1) / kEight), 256) / 256), 256, 0, st>>>(j);
+        join_out_kernel<S><<<RowPieces::blocks(p.n, p.m), 256, 0, st>>>(j);
         return hipGetLastError();
+    }
+
+    static hipError_t few(const deft_ffn_t &a, const FfnScratch &s, int compute_units, hipStream_t st)
+    {
+        FewArgs f{};
+        f.n = a.n_rows;
+        f.hidden = a.hidden;
+        f.inner = a.inner;
+        f.activation = a.activation;
+        f.x = a.x;
+        f.x_stride = a.x_stride;
+        f.w_gate = a.w_gate;
+        f.w_gate_stride = a.w_gate_stride;
+        f.w_up = a.w_up;
+        f.w_up_stride = a.w_up_stride;
+        f.w_down = a.w_down;
+        f.w_down_stride = a.w_down_stride;
+        f.h = s.h;
+        f.h_stride = up(a.inner, 8);
+        f.h_array = kFew * f.h_stride;   // (within the room for a tile's rows)
+        f.saved = a.save;
+        f.y = a.y;
+        f.y_stride = a.y_stride;
+        if (f.n <= 16) return few_tokens<S, 1>(f, compute_units, st);
+        if (f.n <= 32) return few_tokens<S, 2>(f, compute_units, st);
+        return few_tokens<S, 4>(f, compute_units, st);
     }
 
     static hipError_t forward(const FfnPlan &, const deft_ffn_t &a, const FfnScratch &s, int compute_units, hipStream_t st)
     {
-        Operand x, w_gate, w_up, w_down;
-        hipError_t e = operand(a.x, a.x_stride, a.n_rows, a.hidden, true, s.x, &x, st);
-        if (e == hipSuccess) e = operand(a.w_gate, a.w_gate_stride, a.inner, a.hidden, true, s.w_gate, &w_gate, st);
-        if (e == hipSuccess) e = operand(a.w_up, a.w_up_stride, a.inner, a.hidden, true, s.w_up, &w_up, st);
-        if (e == hipSuccess) e = operand(a.w_down, a.w_down_stride, a.hidden, a.inner, true, s.w_down, &w_down, st);
+        // Up to 16 tokens; up to 64 where the matrices would have to be packed.  16 of 4096 x 12288 bf16: 78 us for 86 by the products
+        // below, 24: 99 for 86; 48 of 1021 x 2731 f16 41 for 44; 64 of 1024 x 4096 f32 62 for 96.
+        const bool whole = Packing::as_is(a.x, a.x_stride, a.hidden, true) && Packing::as_is(a.w_gate, a.w_gate_stride, a.hidden, true) &&
+                           Packing::as_is(a.w_up, a.w_up_stride, a.hidden, true) && Packing::as_is(a.w_down, a.w_down_stride, a.inner, true);
+        if (a.n_rows <= (whole ? 16 : kFew)) return few(a, s, compute_units, st);
+        Packing pack;
+        const Operand x = pack.operand(a.x, a.x_stride, a.n_rows, a.hidden, true, s.x);
+        const Operand w_gate = pack.operand(a.w_gate, a.w_gate_stride, a.inner, a.hidden, true, s.w_gate);
+        const Operand w_up = pack.operand(a.w_up, a.w_up_stride, a.inner, a.hidden, true, s.w_up);
+        const Operand w_down = pack.operand(a.w_down, a.w_down_stride, a.hidden, a.inner, true, s.w_down);
+        hipError_t e = pack.launch(st);
         if (e != hipSuccess) return e;
         FfnArgs f = panels(s, a.n_rows, a.inner, a.activation);
         f.saved = a.save;
@@ -261,13 +304,17 @@ struct Ffn {
         hipError_t e = hipSuccess;
         if (n > 0) {
             const bool again = a.saved.kind == DEFT_SAVE_NONE;
-            e = operand(a.grad_y, a.grad_y_stride, n, a.hidden, true, s.grad_y, &grad_y, st);
-            if (e == hipSuccess && (again || of_gate))
-                e = a.x ? operand(a.x, a.x_stride, n, a.hidden, again, s.x, &x, st)
-                        : restored(a.packed_x, n, a.hidden, kSplit ? DEFT_F32 : kHalf16 ? DEFT_F16 : DEFT_BF16, s.x, &x, st);
-            if (e == hipSuccess && (again || a.grad_x)) e = operand(a.w_gate, a.w_gate_stride, a.inner, a.hidden, again, s.w_gate, &w_gate, st);
-            if (e == hipSuccess && (again || a.grad_x)) e = operand(a.w_up, a.w_up_stride, a.inner, a.hidden, again, s.w_up, &w_up, st);
-            if (e == hipSuccess && by_projections) e = operand(a.w_down, a.w_down_stride, a.hidden, a.inner, false, s.w_down, &w_down, st);
+            Packing pack;
+            grad_y = pack.operand(a.grad_y, a.grad_y_stride, n, a.hidden, true, s.grad_y);
+            if ((again || of_gate) && a.x) x = pack.operand(a.x, a.x_stride, n, a.hidden, again, s.x);
+            if (again || a.grad_x) {
+                w_gate = pack.operand(a.w_gate, a.w_gate_stride, a.inner, a.hidden, again, s.w_gate);
+                w_up = pack.operand(a.w_up, a.w_up_stride, a.inner, a.hidden, again, s.w_up);
+            }
+            if (by_projections) w_down = pack.operand(a.w_down, a.w_down_stride, a.hidden, a.inner, false, s.w_down);
+            e = pack.launch(st);
+            if (e == hipSuccess && (again || of_gate) && !a.x)
+                e = restored(a.packed_x, n, a.hidden, kSplit ? DEFT_F32 : kHalf16 ? DEFT_F16 : DEFT_BF16, s.x, &x, st);
             if (e != hipSuccess) return e;
             if (again) {
                 const int64_t ld = up(a.inner, kStep);

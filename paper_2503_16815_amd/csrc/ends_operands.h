@@ -22,11 +22,11 @@ struct PackArgs {
 // 16 bytes a thread, four at a time, one row's after the other.  Bound by memory (30011
 // rows of 1021 16-bit elements, 1026 apart: 24.5 us, 5.0 TB/s read and written; in tiles of 64 x 64 33 us).
 template <typename S, typename T, int P>
-__global__ void __launch_bounds__(256) pack_rows_kernel(PackArgs a)
+__device__ __forceinline__ void pack_rows(const PackArgs &a, unsigned block)
 {
     typedef S S8 __attribute__((ext_vector_type(8), aligned(sizeof(S))));
     typedef T T8 __attribute__((ext_vector_type(8)));
-    const unsigned pieces = (unsigned)(a.out_ld >> 3), first = blockIdx.x * 1024 + threadIdx.x;
+    const unsigned pieces = (unsigned)(a.out_ld >> 3), first = block * 1024 + threadIdx.x;
     const int rows = a.rows_dev ? *a.rows_dev : a.rows, rows_up = (rows + kTile - 1) / kTile * kTile;
     S x[4][8] = {};
     unsigned row[4], col[4];
@@ -66,6 +66,29 @@ __global__ void __launch_bounds__(256) pack_rows_kernel(PackArgs a)
             *reinterpret_cast<T8 *>(static_cast<T *>(a.out) + p * a.out_plane + (int64_t)row[q] * a.out_ld + col[q]) = y[p];
     }
 }
+
+template <typename S, typename T, int P>
+__global__ void __launch_bounds__(256) pack_rows_kernel(PackArgs a) { pack_rows<S, T, P>(a, blockIdx.x); }
+
+// Several matrices' rows in one launch (a launch alone is 5 us, as long as a small matrix takes).
+constexpr int kPackMost = 5;
+struct PackMany {
+    PackArgs of[kPackMost];
+    unsigned blocks[kPackMost];   // that each takes, none behind the last one
+};
+
+template <typename S, typename T, int P>
+__global__ void __launch_bounds__(256) pack_many_kernel(PackMany a)
+{
+    unsigned block = blockIdx.x;
+#pragma unroll
+    for (int i = 0; i < kPackMost; ++i) {
+        if (block < a.blocks[i]) return pack_rows<S, T, P>(a.of[i], block);
+        block -= a.blocks[i];
+    }
+}
+
+inline unsigned pack_blocks(int64_t rows, int64_t out_ld) { return (unsigned)(up(rows * (out_ld >> 3), 1024) / 1024); }
 
 // Whether a product can read rows where they are: whole steps where their elements are its k (the next row's elements, or
 // what lies between rows, must not come in), 16-byte pieces, offsets within 32 bits.
