@@ -18,7 +18,7 @@ struct FfnArgs {
     void *h, *d;                     // panels: hidden activations; derivatives by gate, and behind them by up; or NULL
     int64_t panel, h_plane, d_plane; // elements between panels, between arrays
     deft_saved_t saved;              // the projections
-    const float *factor;             // a power of two that d is held times, and its reciprocal; or NULL
+    const float *largest;            // 16-bit floats: [kFactorParts], which tell the power of two that d is held times; or NULL
     // kOut, kInput, kOuter: rows n < half go to the first, the others, less `half`, to the second
     void *out[2];                    // or NULL
     int64_t out_ld[2];
@@ -26,14 +26,15 @@ struct FfnArgs {
 };
 
 constexpr int kGroup = DEFT_CHECKPOINT_GROUP;
+constexpr int kFactorParts = 256;
 
-// How a workgroup of 256 threads goes through rows' pieces of eight elements: whole rows, at least 256 pieces.
+// How a workgroup of 256 threads goes through rows' pieces of eight elements: as many whole rows as it has threads for, or one.
 struct RowPieces {
     int pieces, first, count;    // of a row; its first row; pieces in all
     float one_by;
     static __host__ __device__ int pieces_of(int cols) { return (cols + 7) / 8; }
-    static __host__ __device__ int rows_each(int cols) { return (256 + pieces_of(cols) - 1) / pieces_of(cols); }
-    static unsigned blocks(int64_t rows, int cols) { return (unsigned)((rows + rows_each(cols) - 1) / rows_each(cols)); }
+    static __host__ __device__ int rows_each(int cols) { return pieces_of(cols) < 256 ? 256 / pieces_of(cols) : 1; }
+    static __host__ __device__ unsigned blocks(int64_t rows, int cols) { return (unsigned)((rows + rows_each(cols) - 1) / rows_each(cols)); }
     __device__ RowPieces(unsigned block, int rows, int cols) : pieces(pieces_of(cols)), first((int)block * rows_each(cols))
     {
         count = min(rows - first, rows_each(cols)) * pieces;
@@ -81,16 +82,14 @@ hipError_t checkpoint_launch(int dtype, const deft_checkpoint_call_t &a, hipStre
 hipError_t restore_launch(int dtype, const deft_restore_call_t &a, hipStream_t st);
 hipError_t restore_operand_launch(int dtype, const RestoreArgs &a, hipStream_t st);
 
-// 16-bit floats: the power of two that brings the largest finite magnitude of x to 1 .. 2, and its reciprocal.
-struct FactorArgs {
+// 16-bit floats: the largest finite magnitudes of the rows' parts.
+struct LargestArgs {
     int rows, cols;
     const f16 *x;
     int64_t x_stride;
-    float *parts;    // [kFactorParts]
-    float *factor;   // [2]
+    float *largest;    // [kFactorParts]
 };
-constexpr int kFactorParts = 256;
-hipError_t ffn_factor_launch(const FactorArgs &a, hipStream_t st);
+hipError_t ffn_largest_launch(const LargestArgs &a, hipStream_t st);
 
 struct FfnPlan {
     int64_t scratch_bytes = 0;
@@ -98,7 +97,7 @@ struct FfnPlan {
     int planes = 1;                  // 16-bit arrays that an operand is held in: 1, or 3 for 32-bit types
     bool grad = false;
     // offsets into the scratch memory
-    int64_t floats, x, grad_y, w_gate, w_up, w_down, h, d, gate, up, sums;
+    int64_t largest, x, grad_y, w_gate, w_up, w_down, h, d, gate, up, sums;
 };
 void ffn_plan(int dtype, int max_rows, int max_hidden, int max_inner, bool grad, int compute_units, FfnPlan *plan);
 hipError_t ffn_prepare();            // kernel attributes, on the current device

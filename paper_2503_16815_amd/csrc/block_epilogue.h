@@ -16,14 +16,23 @@ namespace deft {
 constexpr int kEight = 8;   // columns of a lane
 
 // An activation of the gate and its derivative.  kExact: 32-bit outputs; otherwise exponentials and reciprocals are the
-// hardware's (off by 1 or 2 units of the last 24 bits, and |a| of them in the exponential), far below the rounding to 16
-// bits that follows.
+// hardware's as they come (off by 1 or 2 units of the last 24 bits, and |a| of them in the exponential), far below the rounding
+// to 16 bits that follows.
 template <int KIND, bool kExact>
 __device__ __forceinline__ void act_of(float a, float &y, float &slope)
 {
-    constexpr float kLog2e = 1.44269504f;
-    const auto exp_of = [](float x) { return kExact ? expf(x) : __builtin_amdgcn_exp2f(x * kLog2e); };
-    const auto inverse = [](float x) { return kExact ? 1.0f / x : __builtin_amdgcn_rcpf(x); };
+    constexpr float kLog2e = 1.44269504f, kLog2eRest = 1.92596303e-8f;
+    const auto exp_of = [](float x) {
+        if constexpr (!kExact) return __builtin_amdgcn_exp2f(x * kLog2e);
+        // (what x log2 e loses by its rounding, times ln 2; limits beyond which 1 + exp x is 1 or the gate's share of it 0)
+        const float within = fminf(fmaxf(x, -104.0f), 88.0f), power = within * kLog2e;
+        const float rest = fmaf(within, kLog2e, -power) + within * kLog2eRest, y = __builtin_amdgcn_exp2f(power);
+        return fmaf(y, 0.693147181f * rest, y);
+    };
+    const auto inverse = [](float x) {
+        const float y = __builtin_amdgcn_rcpf(x);
+        return kExact ? fmaf(fmaf(-x, y, 1.0f), y, y) : y;
+    };
     if constexpr (KIND == DEFT_SILU) {
         const float p = inverse(1.0f + exp_of(-a));
         y = a * p;
@@ -239,15 +248,16 @@ __device__ __forceinline__ void to_lds(const f32x4 (&acc)[MT][NT], int j, float 
 // called with a row's number in the tile, where its sums lie, and what `fetch(row, ahead)` brought; the next sixteen rows' are fetched
 // meanwhile.  kLanes lanes have a row, each the same columns of all its rows.  acc[i][j][r] is row row16 + 16 j, column
 // part * 4 + 16 i + r.
-template <typename Ahead, int kLanes, int MT, int NT, typename Fetch, typename Use>
+// kUnroll: the code of all rows that j has, sixteen rows ahead fetched; otherwise one row's, and the next one fetched.
+template <typename Ahead, int kLanes, bool kUnroll, int MT, int NT, typename Fetch, typename Use>
 __device__ __forceinline__ void by_rows(const f32x4 (&acc)[MT][NT], float *lds, int lane, Fetch fetch, Use use)
 {
     static_assert(kLanes <= 16 && kWave % kLanes == 0);
-    constexpr int kPitch = epilogue_pitch(MT), kRows = kWave / kLanes, kTimes = 16 / kRows;
+    constexpr int kPitch = epilogue_pitch(MT), kRows = kWave / kLanes, kTimes = 16 / kRows, kDepth = kUnroll ? kTimes : 1;
     const int row16 = lane & 15, part = lane >> 4, own = lane / kLanes;
-    Ahead ahead[kTimes];
+    Ahead ahead[kDepth];
 #pragma unroll
-    for (int t = 0; t < kTimes; ++t) fetch(t * kRows + own, ahead[t]);
+    for (int t = 0; t < kDepth; ++t) fetch(t * kRows + own, ahead[t]);
 #pragma clang loop unroll(disable)
     for (int j = 0; j < NT; ++j) {
 #pragma unroll
@@ -258,13 +268,19 @@ __device__ __forceinline__ void by_rows(const f32x4 (&acc)[MT][NT], float *lds, 
             }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // (a wavefront's LDS accesses are done in order)
         __builtin_amdgcn_wave_barrier();
-#pragma unroll
-        for (int t = 0; t < kTimes; ++t) {
+        const auto rows = [&](int t, Ahead &a) __attribute__((always_inline)) {
             const int row = t * kRows + own;
-            const Ahead now = ahead[t];
-            if (j + 1 < NT) fetch((j + 1) * 16 + row, ahead[t]);
+            const Ahead now = a;
+            if (kDepth < kTimes ? j * kTimes + t + 1 < NT * kTimes : j + 1 < NT) fetch(j * 16 + row + kDepth * kRows, a);
             use(j * 16 + row, lds + row * kPitch, now);
             __builtin_amdgcn_sched_barrier(0);   // (several rows' work at once would not fit the registers)
+        };
+        if constexpr (kUnroll) {
+#pragma unroll
+            for (int t = 0; t < kTimes; ++t) rows(t, ahead[t]);
+        } else {
+#pragma clang loop unroll(disable)
+            for (int t = 0; t < kTimes; ++t) rows(t, ahead[0]);
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
@@ -308,6 +324,15 @@ __device__ __forceinline__ void read_eight(const float *from, float (&x)[kEight]
 }
 
 struct Nothing {};
+
+// The power of two that brings the largest of kFactorParts magnitudes to 1 .. 2, and its reciprocal.
+__device__ __forceinline__ float2 factor_of(const float *largest, int lane)
+{
+    const f32x4 x = *reinterpret_cast<const f32x4 *>(largest + lane * 4);
+    const float top = wave_max(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])));
+    const unsigned power = __float_as_uint(top) & 0x7f800000u;   // (a 16-bit float's: none is below 2^-24)
+    return power ? make_float2(__uint_as_float(0x7f000000u - power), __uint_as_float(power)) : make_float2(1.0f, 1.0f);
+}
 
 // All eight, whatever the activation is.
 template <bool kExact>
@@ -388,64 +413,50 @@ __device__ __forceinline__ void load_ahead(const FfnArgs &f, const Tile &t, int 
     load_saved<kInside>(f.saved.kind, f.saved.up, n, at, own_cols, a.up);
 }
 
-// A tile that lies inside the matrix.
-template <bool kGrad, int KIND, typename T, typename O, int MT, int NT>
-__device__ __forceinline__ void act_inside(const FfnArgs &f, const f32x4 (&acc)[MT][NT], const Tile &t)
+// KIND: the activation; or -1, whichever the call has.
+template <bool kGrad, int KIND, bool kInside, typename T, typename O, int MT, int NT, bool SPLIT>
+__device__ __forceinline__ void act_rows(const FfnArgs &f, const f32x4 (&acc)[MT][NT], const Tile &t)
 {
     constexpr int kLanes = kGrad ? MT * 2 : MT;
     const int col = (t.lane % kLanes) * kEight, at = t.m + col;
     const int64_t place = (at >> 8) * f.panel + (at & 255);
     T *const h_at = static_cast<T *>(f.h) + place;
-    const auto act = [](const float (&a)[kEight], float (&y)[kEight], float (&slope)[kEight]) __attribute__((always_inline)) {
+    const auto act = [&](const float (&a)[kEight], float (&y)[kEight], float (&slope)[kEight]) __attribute__((always_inline)) {
+        if constexpr (KIND >= 0) {
 #pragma unroll
-        for (int r = 0; r < kEight; ++r) act_of<KIND, false>(a[r], y[r], slope[r]);
+            for (int r = 0; r < kEight; ++r) act_of<KIND, SPLIT>(a[r], y[r], slope[r]);
+        } else {
+            act_of<SPLIT>(f.activation, a, y, slope);
+        }
     };
     if constexpr (kGrad) {
         T *const d_at = static_cast<T *>(f.d) + place;
-        const float factor = __is_same(T, f16) && f.factor ? f.factor[0] : 1.0f;
-        by_rows<Ahead<O>, kLanes>(
-            acc, t.lds, t.lane, [&](int row, Ahead<O> &a) __attribute__((always_inline)) { load_ahead<true>(f, t, row, col, a); },
+        const float factor = __is_same(T, f16) && f.largest ? factor_of(f.largest, t.lane).x : 1.0f;
+        by_rows<Ahead<O>, kLanes, (KIND >= 0)>(
+            acc, t.lds, t.lane, [&](int row, Ahead<O> &a) __attribute__((always_inline)) { load_ahead<kInside>(f, t, row, col, a); },
             [&](int row, const float *sums, const Ahead<O> &a) __attribute__((always_inline)) {
-                use_gate_grad<true, T, O, false>(f, t, row, col, sums, a, factor, h_at, d_at, act);
+                use_gate_grad<kInside, T, O, SPLIT>(f, t, row, col, sums, a, factor, h_at, d_at, act);
             });
     } else {
-        by_rows<Nothing, kLanes>(
+        by_rows<Nothing, kLanes, (KIND >= 0)>(
             acc, t.lds, t.lane, [](int, Nothing &) {},
-            [&](int row, const float *sums, const Nothing &) __attribute__((always_inline)) { use_gate<true, T, O, false>(f, t, row, col, sums, h_at, act); });
+            [&](int row, const float *sums, const Nothing &) __attribute__((always_inline)) { use_gate<kInside, T, O, SPLIT>(f, t, row, col, sums, h_at, act); });
     }
-}
-
-// One that ends beyond it.
-template <bool kGrad, typename T, typename O, int MT, int NT, bool SPLIT>
-__device__ __forceinline__ void act_edge(const FfnArgs &f, const f32x4 (&acc)[MT][NT], const Tile &t)
-{
-    const float factor = kGrad && __is_same(T, f16) && f.factor ? f.factor[0] : 1.0f;
-    const auto act = [&](const float (&a)[kEight], float (&y)[kEight], float (&slope)[kEight])
-        __attribute__((always_inline)) { act_of<SPLIT>(f.activation, a, y, slope); };
-    by_pieces<kGrad ? 8 : 16>(acc, t.lds, t.lane, [&](int row, int col, const float *sums) __attribute__((always_inline)) {
-        const int at = t.m + col;
-        const int64_t place = (at >> 8) * f.panel + (at & 255);
-        if constexpr (kGrad) {
-            Ahead<O> a = {};
-            load_ahead<false>(f, t, row, col, a);
-            use_gate_grad<false, T, O, SPLIT>(f, t, row, col, sums, a, factor, static_cast<T *>(f.h) + place, static_cast<T *>(f.d) + place, act);
-        } else {
-            use_gate<false, T, O, SPLIT>(f, t, row, col, sums, static_cast<T *>(f.h) + place, act);
-        }
-    });
 }
 
 template <bool kGrad, typename T, typename O, int MT, int NT, bool SPLIT>
 __device__ __forceinline__ void act_epilogue(const FfnArgs &f, const f32x4 (&acc)[MT][NT], const Tile &t)
 {
     static_assert(MT % 4 == 0);   // whole groups of 32
-    // (32-bit operands are multiplied six times over: theirs take a fiftieth of it either way)
-    if (SPLIT || t.n + NT * 16 > t.n_rows || t.m + MT * (kGrad ? 16 : 8) > t.cols) return act_edge<kGrad, T, O, MT, NT, SPLIT>(f, acc, t);
-    if constexpr (!SPLIT) {
-        if (f.activation == DEFT_SILU) act_inside<kGrad, DEFT_SILU, T, O, MT, NT>(f, acc, t);
-        else if (f.activation == DEFT_GELU) act_inside<kGrad, DEFT_GELU, T, O, MT, NT>(f, acc, t);
-        else if (f.activation == DEFT_GELU_TANH) act_inside<kGrad, DEFT_GELU_TANH, T, O, MT, NT>(f, acc, t);
-        else act_inside<kGrad, DEFT_RELU, T, O, MT, NT>(f, acc, t);
+    const bool inside = t.n + NT * 16 <= t.n_rows && t.m + MT * (kGrad ? 16 : 8) <= t.cols;
+    if (!inside) return act_rows<kGrad, -1, false, T, O, MT, NT, SPLIT>(f, acc, t);
+    if constexpr (SPLIT) {   // (32-bit operands are multiplied six times over: less of the whole, and twice the registers)
+        act_rows<kGrad, -1, true, T, O, MT, NT, SPLIT>(f, acc, t);
+    } else {
+        if (f.activation == DEFT_SILU) act_rows<kGrad, DEFT_SILU, true, T, O, MT, NT, SPLIT>(f, acc, t);
+        else if (f.activation == DEFT_GELU) act_rows<kGrad, DEFT_GELU, true, T, O, MT, NT, SPLIT>(f, acc, t);
+        else if (f.activation == DEFT_GELU_TANH) act_rows<kGrad, DEFT_GELU_TANH, true, T, O, MT, NT, SPLIT>(f, acc, t);
+        else act_rows<kGrad, DEFT_RELU, true, T, O, MT, NT, SPLIT>(f, acc, t);
     }
 }
 
@@ -458,7 +469,7 @@ __device__ __forceinline__ O *out_row(const FfnArgs &f, int n)
     return out && row < f.rows ? out + row * (which ? f.out_ld[1] : f.out_ld[0]) : nullptr;
 }
 
-// A lane's columns of a row: out = x / factor, or that and what is there, rounded once.
+// A lane's columns of a row: out = alpha x, or that and what is there, rounded once.
 template <bool kInside, typename O>
 __device__ __forceinline__ void store_out(O *row, int at, int cols, const float (&x)[kEight], float alpha, int add)
 {
@@ -478,7 +489,7 @@ template <typename O, int MT, int NT>
 __device__ __forceinline__ void out_epilogue(const FfnArgs &f, const f32x4 (&acc)[MT][NT], float *lds, int lane, int m_wave, int n_wave, int n_rows, int cols,
                                              int add, float *sums, int64_t sums_ld)
 {
-    const float alpha = f.factor ? f.factor[1] : 1.0f;
+    const float alpha = __is_same(O, f16) && f.largest ? factor_of(f.largest, lane).y : 1.0f;
     const auto use = [&](int row, int col, const float *from) __attribute__((always_inline)) {
         const int n = n_wave + row, at = m_wave + col;
         if (n >= n_rows || at >= cols) return;

@@ -35,6 +35,7 @@ template <typename O>
 __global__ void __launch_bounds__(256) join_out_kernel(JoinArgs a)
 {
     const RowPieces by(blockIdx.x, a.n, a.m);
+    const float alpha = __is_same(O, f16) && a.ffn.largest ? factor_of(a.ffn.largest, threadIdx.x & 63).y : 1.0f;
     for (int i = threadIdx.x; i < by.count; i += 256) {
         const int n = by.row(i), m = by.piece(i) * kEight;
         O *row = out_row<O>(a.ffn, n);
@@ -56,19 +57,18 @@ __global__ void __launch_bounds__(256) join_out_kernel(JoinArgs a)
 #pragma unroll
             for (int r = 0; r < kEight; ++r) x[r] += y[r];
         }
-        store_out<false>(row, m, a.m, x, a.ffn.factor ? a.ffn.factor[1] : 1.0f, a.add);
+        store_out<false>(row, m, a.m, x, alpha, a.add);
     }
 }
 
 // One call's view of the scratch memory.
 struct FfnScratch {
-    float *factor, *parts, *sums;
+    float *largest, *sums;
     char *x, *grad_y, *w_gate, *w_up, *w_down, *h, *d, *gate, *up;
     FfnScratch(const FfnPlan &plan, void *scratch)
     {
         char *s = static_cast<char *>(scratch);
-        factor = reinterpret_cast<float *>(s + plan.floats);
-        parts = factor + 64;
+        largest = reinterpret_cast<float *>(s + plan.largest);
         x = s + plan.x;
         grad_y = s + plan.grad_y;
         w_gate = s + plan.w_gate;
@@ -101,6 +101,7 @@ struct Ffn {
         case kHalf: return product_shape<T, S, E, 4, 2, 4, 4, kSplit>(p, st);
         case kSmall: return product_shape<T, S, E, 2, 2, 4, 4, kSplit>(p, st);
         case kNarrow: return product_shape<T, S, E, 4, 2, 4, 2, kSplit>(p, st);
+        case kTiny: return product_shape<T, S, E, 2, 2, 4, 2, kSplit>(p, st);
         case kLarge: return product_shape<T, S, E, 2, 4, 8, 4, kSplit>(p, st);
         default: return hipErrorInvalidValue;
         }
@@ -115,6 +116,7 @@ struct Ffn {
         if (e == hipSuccess) e = allow_shape<T, S, E, 4, 2, 4, 4, kSplit>();
         if (e == hipSuccess) e = allow_shape<T, S, E, 2, 2, 4, 4, kSplit>();
         if (e == hipSuccess) e = allow_shape<T, S, E, 4, 2, 4, 2, kSplit>();
+        if (e == hipSuccess) e = allow_shape<T, S, E, 2, 2, 4, 2, kSplit>();
         return e;
     }
 
@@ -210,12 +212,29 @@ struct Ffn {
         return product<kGate>(p, shape_of(2 * (int64_t)inner, n, (int64_t)(p.k / kStep) * (kSplit ? 6 : 1), 1, compute_units, kNoAct), st);
     }
 
+    // Parts of a sum, as splits_of has them, with the time that it takes to write and join them: a launch and 8 bytes an element
+    // at 5 TB/s, in the time of a large tile's step.
+    static int parts_of(int64_t m, int64_t n, int64_t steps, int64_t units)
+    {
+        const int64_t tiles = up(m, kTile) / kTile * (n <= kFew ? 1 : up(n, kTile) / kTile);
+        int best = 1;
+        double least = 1e300;
+        for (int s = 1; s <= kMaxSplits && (s == 1 || (tiles * s <= 2 * units && steps >= s * 8)); s *= 2) {
+            const double t = least_cost(m, n, steps, s, units, kNoOther) + (s > 1 ? 2.0 + 1e-6 * (double)(m * n) * s : 0.0);
+            if (t < least) {
+                least = t;
+                best = s;
+            }
+        }
+        return best;
+    }
+
     // A product whose sums are the result: cut into parts where that is quicker.
     template <int E>
     static hipError_t summed(ProductArgs &p, const FfnScratch &s, int compute_units, hipStream_t st)
     {
         const int64_t steps = (int64_t)(p.k / kStep) * (kSplit ? 6 : 1) * (E == kInput ? 2 : 1);
-        p.splits = splits_of(p.m, p.n, steps, compute_units, kNoOther);
+        p.splits = parts_of(p.m, p.n, steps, compute_units);
         p.sums = s.sums;
         p.sums_ld = up(p.m, kEight);
         p.sums_split = p.n * p.sums_ld;
@@ -329,8 +348,8 @@ struct Ffn {
             }
             if constexpr (kHalf16) {
                 if (e == hipSuccess && by_projections) {
-                    e = ffn_factor_launch({n, a.hidden, static_cast<const f16 *>(a.grad_y), a.grad_y_stride, s.parts, s.factor}, st);
-                    f.factor = s.factor;
+                    e = ffn_largest_launch({n, a.hidden, static_cast<const f16 *>(a.grad_y), a.grad_y_stride, s.largest}, st);
+                    f.largest = s.largest;
                 }
             }
             if (e == hipSuccess && (by_projections || !again)) {   // (else the product above has left h)
@@ -373,7 +392,7 @@ struct Ffn {
             p.n = a.hidden;
             p.ffn.out[0] = a.grad_down;
             p.ffn.out_ld[0] = a.grad_down_stride;
-            p.ffn.factor = nullptr;
+            p.ffn.largest = nullptr;
             e = summed<kOuter>(p, s, compute_units, st);
         }
         if (e == hipSuccess && a.events) e = hipEventRecord(static_cast<hipEvent_t>(a.events[0]), st);

@@ -1,46 +1,36 @@
 // The feed-forward block's scratch memory, and its calls by type (each type's kernels are a file of their own).
-#include "block.h"
+#include "block_epilogue.h"
 #include "ends_shapes.h"
 
 namespace deft {
 namespace {
 
-// The largest finite magnitude of the rows that a workgroup has.
-__global__ void __launch_bounds__(256) largest_kernel(FactorArgs a)
+// The largest finite magnitude of the pieces of eight that a workgroup has.
+__global__ void __launch_bounds__(256) largest_kernel(LargestArgs a)
 {
     __shared__ float of_wave[4];
     float top = 0.0f;
-    for (int row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        const f16 *x = a.x + (int64_t)row * a.x_stride;
-        for (int c = threadIdx.x; c < a.cols; c += 256) {
-            const float v = fabsf((float)x[c]);
-            top = fmaxf(top, is_finite(v) ? v : 0.0f);
+    for (unsigned block = blockIdx.x;; block += kFactorParts) {
+        if (block >= RowPieces::blocks(a.rows, a.cols)) break;
+        const RowPieces by(block, a.rows, a.cols);
+        for (int i = threadIdx.x; i < by.count; i += 256) {
+            const int at = by.piece(i) * kEight;
+            const Eight<f16>::type x = load_eight<false>(a.x + by.row(i) * a.x_stride + at, at, a.cols);
+#pragma unroll
+            for (int r = 0; r < kEight; ++r) top = fmaxf(top, is_finite((float)x[r]) ? fabsf((float)x[r]) : 0.0f);
         }
     }
     top = wave_max(top);
     if ((threadIdx.x & 63) == 0) of_wave[threadIdx.x >> 6] = top;
     __syncthreads();
-    if (threadIdx.x == 0) a.parts[blockIdx.x] = fmaxf(fmaxf(of_wave[0], of_wave[1]), fmaxf(of_wave[2], of_wave[3]));
-}
-
-__global__ void __launch_bounds__(64) factor_kernel(FactorArgs a)
-{
-    float top = 0.0f;
-    for (int i = threadIdx.x; i < kFactorParts; i += 64) top = fmaxf(top, a.parts[i]);
-    top = wave_max(top);
-    if (threadIdx.x == 0) {
-        const int e = top > 0.0f ? ilogbf(top) : 0;
-        a.factor[0] = ldexpf(1.0f, -e);
-        a.factor[1] = ldexpf(1.0f, e);
-    }
+    if (threadIdx.x == 0) a.largest[blockIdx.x] = fmaxf(fmaxf(of_wave[0], of_wave[1]), fmaxf(of_wave[2], of_wave[3]));
 }
 
 }  // namespace
 
-hipError_t ffn_factor_launch(const FactorArgs &a, hipStream_t st)
+hipError_t ffn_largest_launch(const LargestArgs &a, hipStream_t st)
 {
     largest_kernel<<<kFactorParts, 256, 0, st>>>(a);
-    factor_kernel<<<1, 64, 0, st>>>(a);
     return hipGetLastError();
 }
 
@@ -67,7 +57,7 @@ void ffn_plan(int dtype, int max_rows, int max_hidden, int max_inner, bool grad,
         return here;
     };
     const int64_t element = 2 * plan->planes, own = dtype == DEFT_F32 ? 4 : 2;
-    plan->floats = take((64 + kFactorParts) * 4);
+    plan->largest = take(kFactorParts * 4);
     // (whether a call's rows can be read in place is known when it is made)
     plan->x = take(n * up(max_hidden, kStep) * element);
     plan->w_gate = take(inner * up(max_hidden, kStep) * element);
