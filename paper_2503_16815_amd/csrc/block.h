@@ -28,22 +28,30 @@ struct FfnArgs {
 constexpr int kGroup = DEFT_CHECKPOINT_GROUP;
 constexpr int kFactorParts = 256;
 
-// How a workgroup of 256 threads goes through rows' pieces of eight elements: as many whole rows as it has threads for, or one.
+// How workgroups of 256 threads go through rows' pieces of eight elements, a piece each: as many whole rows as a workgroup has
+// threads for, or a part of one.
 struct RowPieces {
-    int pieces, first, count;    // of a row; its first row; pieces in all
+    int pieces, first, from, count;    // of a row; its first row, and piece of that; pieces in all
     float one_by;
     static __host__ __device__ int pieces_of(int cols) { return (cols + 7) / 8; }
     static __host__ __device__ int rows_each(int cols) { return pieces_of(cols) < 256 ? 256 / pieces_of(cols) : 1; }
-    static __host__ __device__ unsigned blocks(int64_t rows, int cols) { return (unsigned)((rows + rows_each(cols) - 1) / rows_each(cols)); }
-    __device__ RowPieces(unsigned block, int rows, int cols) : pieces(pieces_of(cols)), first((int)block * rows_each(cols))
+    static __host__ __device__ int parts(int cols) { return (pieces_of(cols) + 255) / 256; }   // of a row
+    static __host__ __device__ unsigned blocks(int64_t rows, int cols)
     {
-        count = min(rows - first, rows_each(cols)) * pieces;
+        return (unsigned)((rows + rows_each(cols) - 1) / rows_each(cols) * parts(cols));
+    }
+    __device__ RowPieces(unsigned block, int rows, int cols) : pieces(pieces_of(cols))
+    {
+        const int of = parts(cols);
+        first = (int)(block / of) * rows_each(cols);
+        from = (int)(block % of) * 256;
+        count = of > 1 ? min(pieces - from, 256) : min(rows - first, rows_each(cols)) * pieces;
         one_by = 1.0f / (float)pieces;
     }
-    // (a whole number less than 2^15 and a half, divided: never within the error of a whole number)
-    __device__ int in_block(int i) const { return (int)(((float)i + 0.5f) * one_by); }
+    // (a whole number less than 256 and a half, divided: never within the error of a whole number)
+    __device__ int in_block(int i) const { return from > 0 ? 0 : (int)(((float)i + 0.5f) * one_by); }
     __device__ int row(int i) const { return first + in_block(i); }
-    __device__ int piece(int i) const { return i - in_block(i) * pieces; }
+    __device__ int piece(int i) const { return from + i - in_block(i) * pieces; }
 };
 
 constexpr float kCodes8 = 127.0f, kCodes16 = 32767.0f;   // the largest codes

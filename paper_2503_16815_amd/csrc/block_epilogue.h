@@ -168,42 +168,43 @@ __device__ __forceinline__ void store_saved(int kind, deft_checkpoint_t to, int 
 // Eight elements of it as they come from memory: codes of 8 bits in the first two words, of 16 in four, or floats.
 template <typename O> struct Kept {
     static constexpr bool kFloats = sizeof(O) == 4;
-    unsigned words[kFloats ? 8 : 4];
-    unsigned short scale;
+    i32x4 words, more;
+    unsigned scale;
 };
-
-template <bool kInside, typename C, typename O>
-__device__ __forceinline__ void load_words(const C *from, int at, int cols, Kept<O> &k)
-{
-    const typename Eight<C>::type y = load_eight<kInside>(from, at, cols);
-    unsigned words[2 * sizeof(C)];
-    static_assert(sizeof(words) == sizeof(y));
-    __builtin_memcpy(words, &y, sizeof(words));
-#pragma unroll
-    for (unsigned i = 0; i < 2 * sizeof(C); ++i) k.words[i] = words[i];
-}
 
 template <bool kInside, typename O>
 __device__ __forceinline__ void load_saved(int kind, deft_checkpoint_t from, int n, int at, int cols, Kept<O> &k)
 {
-    if (kind == DEFT_SAVE_PACKED) load_words<kInside>(static_cast<const int8_t *>(from.codes) + n * from.codes_stride + at, at, cols, k);
-    else if constexpr (Kept<O>::kFloats) load_words<kInside>(static_cast<const float *>(from.codes) + n * from.codes_stride + at, at, cols, k);
-    else load_words<kInside>(static_cast<const int16_t *>(from.codes) + n * from.codes_stride + at, at, cols, k);
+    k.words = k.more = i32x4{0, 0, 0, 0};
     k.scale = 0;
-    if ((kind == DEFT_SAVE_PACKED || !Kept<O>::kFloats) && (kInside || at < cols))
-        k.scale = static_cast<const unsigned short *>(from.scales)[n * from.scales_stride + at / kGroup];
+    if (kind == DEFT_SAVE_PACKED) {
+        const uint2 y = __builtin_bit_cast(uint2, load_eight<kInside>(static_cast<const int8_t *>(from.codes) + n * from.codes_stride + at, at, cols));
+        k.words[0] = (int)y.x;
+        k.words[1] = (int)y.y;
+    } else if constexpr (Kept<O>::kFloats) {
+        const Eight<float>::type y = load_eight<kInside>(static_cast<const float *>(from.codes) + n * from.codes_stride + at, at, cols);
+        k.words = __builtin_bit_cast(i32x4, __builtin_shufflevector(y, y, 0, 1, 2, 3));
+        k.more = __builtin_bit_cast(i32x4, __builtin_shufflevector(y, y, 4, 5, 6, 7));
+        return;
+    } else {
+        k.words = __builtin_bit_cast(i32x4, load_eight<kInside>(static_cast<const int16_t *>(from.codes) + n * from.codes_stride + at, at, cols));
+    }
+    if (kInside || at < cols) k.scale = static_cast<const unsigned short *>(from.scales)[n * from.scales_stride + at / kGroup];
 }
 
 template <typename O>
 __device__ __forceinline__ void use_saved(int kind, const Kept<O> &k, float (&x)[kEight])
 {
-    const float s = __uint_as_float((unsigned)k.scale << 16);
+    const float s = __uint_as_float(k.scale << 16);
     if (kind == DEFT_SAVE_PACKED) {
 #pragma unroll
         for (int r = 0; r < kEight; ++r) x[r] = (float)(int8_t)(k.words[r / 4] >> (8 * (r % 4))) * s;
     } else if constexpr (Kept<O>::kFloats) {
 #pragma unroll
-        for (int r = 0; r < kEight; ++r) x[r] = __uint_as_float(k.words[r]);
+        for (int r = 0; r < 4; ++r) {
+            x[r] = __int_as_float(k.words[r]);
+            x[r + 4] = __int_as_float(k.more[r]);
+        }
     } else {
 #pragma unroll
         for (int r = 0; r < kEight; ++r) x[r] = (float)(int16_t)(k.words[r / 2] >> (16 * (r % 2))) * s;
@@ -334,17 +335,21 @@ __device__ __forceinline__ float2 factor_of(const float *largest, int lane)
     return power ? make_float2(__uint_as_float(0x7f000000u - power), __uint_as_float(power)) : make_float2(1.0f, 1.0f);
 }
 
-// All eight, whatever the activation is.
+template <int KIND, bool kExact>
+__device__ __forceinline__ void act_of(const float (&a)[kEight], float (&y)[kEight], float (&slope)[kEight])
+{
+#pragma unroll
+    for (int r = 0; r < kEight; ++r) act_of<KIND, kExact>(a[r], y[r], slope[r]);
+}
+
+// Whatever the activation is.
 template <bool kExact>
 __device__ __forceinline__ void act_of(int kind, const float (&a)[kEight], float (&y)[kEight], float (&slope)[kEight])
 {
-#pragma unroll
-    for (int r = 0; r < kEight; ++r) {
-        if (kind == DEFT_SILU) act_of<DEFT_SILU, kExact>(a[r], y[r], slope[r]);
-        else if (kind == DEFT_GELU) act_of<DEFT_GELU, kExact>(a[r], y[r], slope[r]);
-        else if (kind == DEFT_GELU_TANH) act_of<DEFT_GELU_TANH, kExact>(a[r], y[r], slope[r]);
-        else act_of<DEFT_RELU, kExact>(a[r], y[r], slope[r]);
-    }
+    if (kind == DEFT_SILU) act_of<DEFT_SILU, kExact>(a, y, slope);
+    else if (kind == DEFT_GELU) act_of<DEFT_GELU, kExact>(a, y, slope);
+    else if (kind == DEFT_GELU_TANH) act_of<DEFT_GELU_TANH, kExact>(a, y, slope);
+    else act_of<DEFT_RELU, kExact>(a, y, slope);
 }
 
 // What a wavefront's tile is to the epilogues below.
@@ -354,14 +359,12 @@ struct Tile {
     int n_rows, cols;    // that the matrix has
 };
 
-// Eight elements of the first product's: `at` their column, own_cols the columns that their row has (0: no such row, zeros in h).
+// Eight elements of both projections, of row n and from column `at` on; own_cols: the columns that the row has (0: no such row, zeros
+// in h).  h_at: where h has the column.
 template <bool kInside, typename T, typename O, bool SPLIT, typename Act>
-__device__ __forceinline__ void use_gate(const FfnArgs &f, const Tile &t, int row, int col, const float *sums, T *h_at, Act act)
+__device__ __forceinline__ void use_gate(const FfnArgs &f, int n, int at, int own_cols, const float (&gate)[kEight], const float (&up)[kEight], T *h_at, Act act)
 {
-    const int n = t.n + row, at = t.m + col, own_cols = kInside || n < t.n_rows ? t.cols : 0;
-    float gate[kEight], up[kEight], y[kEight], slope[kEight];
-    read_eight(sums + (col >> 4) * 32 + (col & 15), gate);   // (sixteens of columns are gate and up in turn)
-    read_eight(sums + (col >> 4) * 32 + 16 + (col & 15), up);
+    float y[kEight], slope[kEight];
     if (f.saved.kind != DEFT_SAVE_NONE) {
         store_saved<kInside, O>(f.saved.kind, f.saved.gate, n, at, own_cols, gate);
         store_saved<kInside, O>(f.saved.kind, f.saved.up, n, at, own_cols, up);
@@ -377,15 +380,13 @@ template <typename O> struct Ahead {
     Kept<O> gate, up;
 };
 
-// And of the derivative's by h.
+// And of the derivative by h.
 template <bool kInside, typename T, typename O, bool SPLIT, typename Act>
-__device__ __forceinline__ void use_gate_grad(const FfnArgs &f, const Tile &t, int row, int col, const float *sums, const Ahead<O> &a, float factor, T *h_at,
-                                              T *d_at, Act act)
+__device__ __forceinline__ void use_gate_grad(const FfnArgs &f, int n, int at, int own_cols, const float (&by_h)[kEight], const Ahead<O> &a, float factor,
+                                              T *h_at, T *d_at, Act act)
 {
-    const int n = t.n + row, at = t.m + col, own_cols = kInside || n < t.n_rows ? t.cols : 0;
     if (!kInside && at >= f.cols_up) return;
-    float by_h[kEight], gate[kEight], up[kEight], y[kEight], slope[kEight], h[kEight];
-    read_eight(sums + col, by_h);
+    float gate[kEight], up[kEight], y[kEight], slope[kEight], h[kEight];
     use_saved(f.saved.kind, a.gate, gate);
     use_saved(f.saved.kind, a.up, up);
     act(gate, y, slope);
@@ -406,9 +407,8 @@ __device__ __forceinline__ void use_gate_grad(const FfnArgs &f, const Tile &t, i
 }
 
 template <bool kInside, typename O>
-__device__ __forceinline__ void load_ahead(const FfnArgs &f, const Tile &t, int row, int col, Ahead<O> &a)
+__device__ __forceinline__ void load_ahead(const FfnArgs &f, int n, int at, int own_cols, Ahead<O> &a)
 {
-    const int n = t.n + row, at = t.m + col, own_cols = kInside || n < t.n_rows ? t.cols : 0;
     load_saved<kInside>(f.saved.kind, f.saved.gate, n, at, own_cols, a.gate);
     load_saved<kInside>(f.saved.kind, f.saved.up, n, at, own_cols, a.up);
 }
@@ -422,25 +422,30 @@ __device__ __forceinline__ void act_rows(const FfnArgs &f, const f32x4 (&acc)[MT
     const int64_t place = (at >> 8) * f.panel + (at & 255);
     T *const h_at = static_cast<T *>(f.h) + place;
     const auto act = [&](const float (&a)[kEight], float (&y)[kEight], float (&slope)[kEight]) __attribute__((always_inline)) {
-        if constexpr (KIND >= 0) {
-#pragma unroll
-            for (int r = 0; r < kEight; ++r) act_of<KIND, SPLIT>(a[r], y[r], slope[r]);
-        } else {
-            act_of<SPLIT>(f.activation, a, y, slope);
-        }
+        if constexpr (KIND >= 0) act_of<KIND, SPLIT>(a, y, slope);
+        else act_of<SPLIT>(f.activation, a, y, slope);
     };
+    const auto cols_of = [&](int n) __attribute__((always_inline)) { return kInside || n < t.n_rows ? t.cols : 0; };
     if constexpr (kGrad) {
         T *const d_at = static_cast<T *>(f.d) + place;
         const float factor = __is_same(T, f16) && f.largest ? factor_of(f.largest, t.lane).x : 1.0f;
         by_rows<Ahead<O>, kLanes, (KIND >= 0)>(
-            acc, t.lds, t.lane, [&](int row, Ahead<O> &a) __attribute__((always_inline)) { load_ahead<kInside>(f, t, row, col, a); },
+            acc, t.lds, t.lane,
+            [&](int row, Ahead<O> &a) __attribute__((always_inline)) { load_ahead<kInside>(f, t.n + row, at, cols_of(t.n + row), a); },
             [&](int row, const float *sums, const Ahead<O> &a) __attribute__((always_inline)) {
-                use_gate_grad<kInside, T, O, SPLIT>(f, t, row, col, sums, a, factor, h_at, d_at, act);
+                float by_h[kEight];
+                read_eight(sums + col, by_h);
+                use_gate_grad<kInside, T, O, SPLIT>(f, t.n + row, at, cols_of(t.n + row), by_h, a, factor, h_at, d_at, act);
             });
     } else {
         by_rows<Nothing, kLanes, (KIND >= 0)>(
             acc, t.lds, t.lane, [](int, Nothing &) {},
-            [&](int row, const float *sums, const Nothing &) __attribute__((always_inline)) { use_gate<kInside, T, O, SPLIT>(f, t, row, col, sums, h_at, act); });
+            [&](int row, const float *sums, const Nothing &) __attribute__((always_inline)) {
+                float gate[kEight], up[kEight];
+                read_eight(sums + (col >> 4) * 32 + (col & 15), gate);   // (sixteens of columns are gate and up in turn)
+                read_eight(sums + (col >> 4) * 32 + 16 + (col & 15), up);
+                use_gate<kInside, T, O, SPLIT>(f, t.n + row, at, cols_of(t.n + row), gate, up, h_at, act);
+            });
     }
 }
 
@@ -484,21 +489,31 @@ __device__ __forceinline__ void store_out(O *row, int at, int cols, const float 
     store_eight<kInside>(row + at, at, cols, rounded<O>(y));
 }
 
-// The sums are the result, or a part of it (`sums`: rows of sums_ld elements, a multiple of 8).
-template <typename O, int MT, int NT>
-__device__ __forceinline__ void out_epilogue(const FfnArgs &f, const f32x4 (&acc)[MT][NT], float *lds, int lane, int m_wave, int n_wave, int n_rows, int cols,
-                                             int add, float *sums, int64_t sums_ld)
+// A part of the sums: rows of `ld` elements, a multiple of 8.
+template <int MT, int NT>
+__device__ __forceinline__ void sums_epilogue(float *sums, int64_t ld, const f32x4 (&acc)[MT][NT], const Tile &t)
 {
-    const float alpha = __is_same(O, f16) && f.largest ? factor_of(f.largest, lane).y : 1.0f;
-    const auto use = [&](int row, int col, const float *from) __attribute__((always_inline)) {
-        const int n = n_wave + row, at = m_wave + col;
-        if (n >= n_rows || at >= cols) return;
+    by_pieces<8>(acc, t.lds, t.lane, [&](int row, int col, const float *from) __attribute__((always_inline)) {
+        const int n = t.n + row, at = t.m + col;
+        if (n >= t.n_rows || at >= t.cols) return;
         float x[kEight];
         read_eight(from + col, x);
-        if (sums) store_eight<true>(sums + n * sums_ld + at, at, cols, rounded<float>(x));
-        else if (O *to = out_row<O>(f, n)) store_out<false>(to, at, cols, x, alpha, add);
-    };
-    by_pieces<8>(acc, lds, lane, use);
+        store_eight<true>(sums + n * ld + at, at, t.cols, rounded<float>(x));
+    });
+}
+
+// The sums are the result.
+template <typename O, int MT, int NT>
+__device__ __forceinline__ void out_epilogue(const FfnArgs &f, const f32x4 (&acc)[MT][NT], const Tile &t, int add)
+{
+    const float alpha = __is_same(O, f16) && f.largest ? factor_of(f.largest, t.lane).y : 1.0f;
+    by_pieces<8>(acc, t.lds, t.lane, [&](int row, int col, const float *from) __attribute__((always_inline)) {
+        const int n = t.n + row, at = t.m + col;
+        if (n >= t.n_rows || at >= t.cols) return;
+        float x[kEight];
+        read_eight(from + col, x);
+        if (O *to = out_row<O>(f, n)) store_out<false>(to, at, t.cols, x, alpha, add);
+    });
 }
 
 }  // namespace deft

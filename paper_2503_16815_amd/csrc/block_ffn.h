@@ -31,6 +31,28 @@ struct JoinArgs {
     int64_t sums_ld, sums_split;
 };
 
+// The sums of all parts, eight columns from `from` on.
+__device__ __forceinline__ void joined(const JoinArgs &a, const float *from, float (&x)[kEight])
+{
+#pragma unroll
+    for (int r = 0; r < kEight; ++r) x[r] = 0.0f;
+    int s = 0;
+    for (; s + 4 <= a.splits; s += 4) {   // (eight loads under way)
+        Eight<float>::type y[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) y[k] = load_eight<true>(from + (s + k) * a.sums_split, 0, kEight);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int r = 0; r < kEight; ++r) x[r] += y[k][r];
+    }
+    for (; s < a.splits; ++s) {
+        const Eight<float>::type y = load_eight<true>(from + s * a.sums_split, 0, kEight);
+#pragma unroll
+        for (int r = 0; r < kEight; ++r) x[r] += y[r];
+    }
+}
+
 template <typename O>
 __global__ void __launch_bounds__(256) join_out_kernel(JoinArgs a)
 {
@@ -40,24 +62,46 @@ __global__ void __launch_bounds__(256) join_out_kernel(JoinArgs a)
         const int n = by.row(i), m = by.piece(i) * kEight;
         O *row = out_row<O>(a.ffn, n);
         if (!row) continue;
-        const float *sums = a.sums + n * a.sums_ld + m;
-        float x[kEight] = {};
-        int s = 0;
-        for (; s + 4 <= a.splits; s += 4) {   // (eight loads under way)
-            Eight<float>::type y[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) y[k] = load_eight<true>(sums + (s + k) * a.sums_split, 0, kEight);
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-#pragma unroll
-                for (int r = 0; r < kEight; ++r) x[r] += y[k][r];
-        }
-        for (; s < a.splits; ++s) {
-            const Eight<float>::type y = load_eight<true>(sums + s * a.sums_split, 0, kEight);
-#pragma unroll
-            for (int r = 0; r < kEight; ++r) x[r] += y[r];
-        }
+        float x[kEight];
+        joined(a, a.sums + n * a.sums_ld + m, x);
         store_out<false>(row, m, a.m, x, alpha, a.add);
+    }
+}
+
+// What the products of the projections and of the derivative by h do with their sums, of sums that were cut into parts: m columns
+// of n rows, zeros in what the next products read beyond (four neighbouring lanes have a checkpoint's group).
+template <bool kGrad, typename T, typename O, bool SPLIT>
+__global__ void __launch_bounds__(256) join_act_kernel(JoinArgs a)
+{
+    const FfnArgs &f = a.ffn;
+    const float factor = kGrad && __is_same(T, f16) && f.largest ? factor_of(f.largest, threadIdx.x & 63).x : 1.0f;
+    const auto act = [&](const float (&x)[kEight], float (&y)[kEight], float (&slope)[kEight])
+        __attribute__((always_inline)) { act_of<SPLIT>(f.activation, x, y, slope); };
+    const auto eight = [&](auto inside, int n, int at) __attribute__((always_inline)) {
+        constexpr bool kInside = decltype(inside)::value;
+        const int own_cols = kInside || n < a.n ? a.m : 0;
+        const float *sums = a.sums + n * a.sums_ld;
+        const int64_t place = (at >> 8) * f.panel + (at & 255);
+        T *const h_at = static_cast<T *>(f.h) + place;
+        float x[kEight] = {}, up[kEight] = {};
+        if constexpr (kGrad) {
+            Ahead<O> ahead = {};
+            load_ahead<kInside>(f, n, at, own_cols, ahead);
+            if (kInside || at < own_cols) joined(a, sums + at, x);
+            use_gate_grad<kInside, T, O, SPLIT>(f, n, at, own_cols, x, ahead, factor, h_at, static_cast<T *>(f.d) + place, act);
+        } else {
+            if (kInside || at < own_cols) {
+                joined(a, sums + (at >> 4) * 32 + (at & 15), x);
+                joined(a, sums + (at >> 4) * 32 + 16 + (at & 15), up);
+            }
+            use_gate<kInside, T, O, SPLIT>(f, n, at, own_cols, x, up, h_at, act);
+        }
+    };
+    const RowPieces by(blockIdx.x, (a.n + kStep - 1) / kStep * kStep, (a.m + kStep - 1) / kStep * kStep);
+    for (int i = threadIdx.x; i < by.count; i += 256) {
+        const int n = by.row(i), at = by.piece(i) * kEight;
+        if (n < a.n && (at & -kGroup) + kGroup <= a.m) eight(std::true_type{}, n, at);   // (a group's four lanes go the same way)
+        else eight(std::false_type{}, n, at);
     }
 }
 
@@ -90,6 +134,7 @@ struct Operand {
 template <typename S, typename T, int P>
 struct Ffn {
     static constexpr bool kSplit = P == 3, kHalf16 = __is_same(T, f16);
+    static constexpr double kAlone = kSplit ? 1.6 : 1.0;   // (128 x 128 tiles 0.72 us a step for 0.46, 128 x 64 ones 0.45 for 0.28)
 
     template <int E>
     static hipError_t product(const ProductArgs &p, Shape shape, hipStream_t st)
@@ -191,8 +236,62 @@ struct Ffn {
         return f;
     }
 
-    static hipError_t gate(const FfnArgs &f, const Operand &x, const Operand &w_gate, const Operand &w_up, int n, int hidden, int inner, int compute_units,
-                           hipStream_t st)
+    // Parts of a sum, as splits_of has them, with the time that it takes to write and join them: a launch and 8 bytes an element
+    // at 5 TB/s, in the time of a large tile's step.
+    static int parts_of(int64_t m, int64_t n, int64_t steps, int64_t units, unsigned without)
+    {
+        const int64_t tiles = up(m, kTile) / kTile * (n <= kFew ? 1 : up(n, kTile) / kTile);
+        int best = 1;
+        double least = 1e300;
+        for (int s = 1; s <= kMaxSplits && (s == 1 || (tiles * s <= 2 * units && steps >= s * 4)); s *= 2) {
+            const double t = least_cost(m, n, steps, s, units, without, kAlone) + (s > 1 ? 2.0 + 1e-6 * (double)(m * n) * s : 0.0);
+            if (t < least) {
+                least = t;
+                best = s;
+            }
+        }
+        return best;
+    }
+
+    // A product of `rows` by `cols` sums, cut into parts where that is quicker.
+    template <int E>
+    static hipError_t parts(ProductArgs &p, int cols, const FfnScratch &s, int compute_units, hipStream_t st)
+    {
+        constexpr unsigned kWithout = E == kGate || E == kGateGrad ? kNoAct : kNoOther;
+        const int64_t steps = (int64_t)(p.k / kStep) * (kSplit ? 6 : 1) * (E == kInput ? 2 : 1);
+        p.splits = parts_of(cols, p.n, steps, compute_units, kWithout);
+        p.sums = s.sums;
+        p.sums_ld = up(cols, kEight);
+        p.sums_split = p.n * p.sums_ld;
+        return product<E>(p, shape_of(cols, p.n, steps, p.splits, compute_units, kWithout, kAlone), st);
+    }
+
+    static JoinArgs join(const ProductArgs &p)
+    {
+        JoinArgs j{};
+        j.ffn = p.ffn;
+        j.m = p.m;
+        j.n = p.n;
+        j.splits = p.splits;
+        j.add = p.add;
+        j.sums = p.sums;
+        j.sums_ld = p.sums_ld;
+        j.sums_split = p.sums_split;
+        return j;
+    }
+
+    // One whose sums go through the activation: both projections, or the derivative by h.
+    template <int E>
+    static hipError_t activated(ProductArgs &p, const FfnScratch &s, int compute_units, hipStream_t st)
+    {
+        const hipError_t e = parts<E>(p, E == kGate ? (int)up(p.m, 16) * 2 : p.m, s, compute_units, st);
+        if (e != hipSuccess || p.splits == 1) return e;
+        join_act_kernel<E == kGateGrad, T, S, kSplit><<<RowPieces::blocks(up(p.n, kStep), (int)up(p.m, kStep)), 256, 0, st>>>(join(p));
+        return hipGetLastError();
+    }
+
+    static hipError_t gate(const FfnArgs &f, const Operand &x, const Operand &w_gate, const Operand &w_up, int n, int hidden, int inner, const FfnScratch &s,
+                           int compute_units, hipStream_t st)
     {
         ProductArgs p{};
         p.a = w_gate.p;
@@ -204,52 +303,20 @@ struct Ffn {
         p.m = inner;
         p.n = n;
         p.k = (int)up(hidden, kStep);
-        p.splits = 1;
         p.ffn = f;
         p.ffn.a2 = w_up.p;
         p.ffn.a2_ld = w_up.ld;
         p.ffn.a2_plane = w_up.plane;
-        return product<kGate>(p, shape_of(2 * (int64_t)inner, n, (int64_t)(p.k / kStep) * (kSplit ? 6 : 1), 1, compute_units, kNoAct), st);
+        return activated<kGate>(p, s, compute_units, st);
     }
 
-    // Parts of a sum, as splits_of has them, with the time that it takes to write and join them: a launch and 8 bytes an element
-    // at 5 TB/s, in the time of a large tile's step.
-    static int parts_of(int64_t m, int64_t n, int64_t steps, int64_t units)
-    {
-        const int64_t tiles = up(m, kTile) / kTile * (n <= kFew ? 1 : up(n, kTile) / kTile);
-        int best = 1;
-        double least = 1e300;
-        for (int s = 1; s <= kMaxSplits && (s == 1 || (tiles * s <= 2 * units && steps >= s * 8)); s *= 2) {
-            const double t = least_cost(m, n, steps, s, units, kNoOther) + (s > 1 ? 2.0 + 1e-6 * (double)(m * n) * s : 0.0);
-            if (t < least) {
-                least = t;
-                best = s;
-            }
-        }
-        return best;
-    }
-
-    // A product whose sums are the result: cut into parts where that is quicker.
+    // One whose sums are the result.
     template <int E>
     static hipError_t summed(ProductArgs &p, const FfnScratch &s, int compute_units, hipStream_t st)
     {
-        const int64_t steps = (int64_t)(p.k / kStep) * (kSplit ? 6 : 1) * (E == kInput ? 2 : 1);
-        p.splits = parts_of(p.m, p.n, steps, compute_units);
-        p.sums = s.sums;
-        p.sums_ld = up(p.m, kEight);
-        p.sums_split = p.n * p.sums_ld;
-        const hipError_t e = product<E>(p, shape_of(p.m, p.n, steps, p.splits, compute_units, kNoOther), st);
+        const hipError_t e = parts<E>(p, p.m, s, compute_units, st);
         if (e != hipSuccess || p.splits == 1) return e;
-        JoinArgs j{};
-        j.ffn = p.ffn;
-        j.m = p.m;
-        j.n = p.n;
-        j.splits = p.splits;
-        j.add = p.add;
-        j.sums = p.sums;
-        j.sums_ld = p.sums_ld;
-        j.sums_split = p.sums_split;
-        join_out_kernel<S><<<RowPieces::blocks(p.n, p.m), 256, 0, st>>>(j);
+        join_out_kernel<S><<<RowPieces::blocks(p.n, p.m), 256, 0, st>>>(join(p));
         return hipGetLastError();
     }
 
@@ -295,7 +362,7 @@ struct Ffn {
         if (e != hipSuccess) return e;
         FfnArgs f = panels(s, a.n_rows, a.inner, a.activation);
         f.saved = a.save;
-        e = gate(f, x, w_gate, w_up, a.n_rows, a.hidden, a.inner, compute_units, st);
+        e = gate(f, x, w_gate, w_up, a.n_rows, a.hidden, a.inner, s, compute_units, st);
         if (e != hipSuccess) return e;
         ProductArgs p{};
         p.a = w_down.p;
@@ -342,7 +409,7 @@ struct Ffn {
                 f.saved.up = {s.up, ld, s.up + up(n, kTile) * ld * (int64_t)sizeof(S), ld / kGroup};
                 FfnArgs g = f;
                 if (by_projections) g.h = nullptr;
-                e = gate(g, x, w_gate, w_up, n, a.hidden, a.inner, compute_units, st);
+                e = gate(g, x, w_gate, w_up, n, a.hidden, a.inner, s, compute_units, st);
             } else {
                 f.saved = a.saved;
             }
@@ -364,11 +431,10 @@ struct Ffn {
                 p.m = a.inner;
                 p.n = n;
                 p.k = by_projections ? (int)up(a.hidden, kStep) : 0;
-                p.splits = 1;
                 p.ffn = f;
                 p.ffn.h = a.grad_down ? s.h : nullptr;
                 p.ffn.d = by_projections ? s.d : nullptr;
-                e = product<kGateGrad>(p, shape_of(a.inner, n, (int64_t)(p.k / kStep) * (kSplit ? 6 : 1), 1, compute_units, kNoAct), st);
+                e = activated<kGateGrad>(p, s, compute_units, st);
             }
         }
         const bool weights = n > 0 || !a.accumulate;

@@ -64,7 +64,7 @@ void ffn_plan(int dtype, int max_rows, int max_hidden, int max_inner, bool grad,
     plan->w_up = take(inner * up(max_hidden, kStep) * element);
     plan->w_down = take(hidden * up(max_inner, kStep) * element);
     plan->h = take(n * inner * element);
-    int64_t most = n * hidden;   // sums of one part
+    int64_t most = n * (2 * inner > hidden ? 2 * inner : hidden);   // sums of one part
     if (grad) {
         plan->grad_y = take(n * up(max_hidden, kStep) * element);
         plan->d = take(2 * n * inner * element);

@@ -530,13 +530,18 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
         }
     } else if constexpr (E >= kGate) {
         __syncthreads();
-        float *own = reinterpret_cast<float *>(lds) + wave * epilogue_floats(MT);
-        const int m_wave = m0 + wm * MT * (E == kGate ? 8 : 16), n_wave = n0 + wn * NT * 16;
-        if constexpr (E == kGate || E == kGateGrad)
-            act_epilogue<E == kGateGrad, T, O, MT, NT, SPLIT>(p.ffn, acc, Tile{own, lane, m_wave, n_wave, n_rows, p.m});
-        else
-            out_epilogue<O, MT, NT>(p.ffn, acc, own, lane, m_wave, n_wave, n_rows, p.m, p.add, p.splits > 1 ? p.sums + split * p.sums_split : nullptr,
-                                    p.sums_ld);
+        Tile t = {reinterpret_cast<float *>(lds) + wave * epilogue_floats(MT), lane, m0 + wm * MT * (E == kGate ? 8 : 16), n0 + wn * NT * 16, n_rows, p.m};
+        if (p.splits > 1) {
+            if (E == kGate) {   // (both projections as they lie in the tiles)
+                t.m = tm * TM + wm * MT * 16;
+                t.cols = (p.m + 15) / 16 * 32;
+            }
+            sums_epilogue(p.sums + split * p.sums_split, p.sums_ld, acc, t);
+        } else if constexpr (E == kGate || E == kGateGrad) {
+            act_epilogue<E == kGateGrad, T, O, MT, NT, SPLIT>(p.ffn, acc, t);
+        } else {
+            out_epilogue<O, MT, NT>(p.ffn, acc, t, p.add);
+        }
     } else {
         const float alpha = p.scale * *p.out_scale;
         typedef O O4 __attribute__((ext_vector_type(4), aligned(sizeof(O))));

@@ -29,7 +29,9 @@ constexpr ShapeCost kCosts[kShapes] = {{256, 256, 1.0, 6.0}, {192, 256, 0.745, 5
 constexpr double kAloneStep = 0.29, kAloneFixed = 5.0;   // of a 128 x 128 tile that has a compute unit to itself
 constexpr double kTinyStep = 0.18, kTinyFixed = 4.0;     // of a 128 x 64 one
 
-inline double cost_of(Shape shape, int64_t m, int64_t n, int64_t steps, int64_t splits, int64_t units)
+// `alone`: by what a step of a tile that has a compute unit to itself takes longer than in bf16 (which waits for memory, and where
+// operands are three arrays the card's caches give half as much again).
+inline double cost_of(Shape shape, int64_t m, int64_t n, int64_t steps, int64_t splits, int64_t units, double alone = 1.0)
 {
     const ShapeCost &c = kCosts[shape];
     const int64_t tiles = up(m, c.tm) / c.tm * (up(n, c.tn) / c.tn) * splits;
@@ -37,24 +39,26 @@ inline double cost_of(Shape shape, int64_t m, int64_t n, int64_t steps, int64_t 
     if (shape != kSmall && shape != kTiny) return (double)(up(tiles, units) / units) * (c.step * each + c.fixed);
     const int64_t pairs = tiles / (2 * units), rest = tiles % (2 * units);
     return (double)(pairs + (rest > units ? 1 : 0)) * (c.step * each + c.fixed) +
-           (rest > 0 && rest <= units ? (shape == kTiny ? kTinyStep * each + kTinyFixed : kAloneStep * each + kAloneFixed) : 0.0);
+           (rest > 0 && rest <= units ? (shape == kTiny ? kTinyStep * alone * each + kTinyFixed : kAloneStep * alone * each + kAloneFixed) : 0.0);
 }
 
 constexpr unsigned kHeadWithout = 1u << kTiny;
 
 // `without`: shapes (their bits) that a product has no kernel for.
-inline Shape shape_of(int64_t m, int64_t n, int64_t steps, int64_t splits, int64_t units, unsigned without = kHeadWithout)
+inline Shape shape_of(int64_t m, int64_t n, int64_t steps, int64_t splits, int64_t units, unsigned without = kHeadWithout, double alone = 1.0)
 {
     if (n <= kFew) return kNarrow;
     Shape best = kLarge;
     for (int s = 1; s < kShapes; ++s)
-        if (s != kNarrow && !(without >> s & 1) && cost_of((Shape)s, m, n, steps, splits, units) < cost_of(best, m, n, steps, splits, units)) best = (Shape)s;
+        if (s != kNarrow && !(without >> s & 1) &&
+            cost_of((Shape)s, m, n, steps, splits, units, alone) < cost_of(best, m, n, steps, splits, units, alone))
+            best = (Shape)s;
     return best;
 }
 
-inline double least_cost(int64_t m, int64_t n, int64_t steps, int64_t splits, int64_t units, unsigned without = kHeadWithout)
+inline double least_cost(int64_t m, int64_t n, int64_t steps, int64_t splits, int64_t units, unsigned without = kHeadWithout, double alone = 1.0)
 {
-    return cost_of(shape_of(m, n, steps, splits, units, without), m, n, steps, splits, units);
+    return cost_of(shape_of(m, n, steps, splits, units, without, alone), m, n, steps, splits, units, alone);
 }
 
 // Parts that a sum over k is cut into, where its tiles leave compute units idle: each part's sums go to memory and are
