@@ -429,14 +429,22 @@ __device__ __forceinline__ void act_rows(const FfnArgs &f, const f32x4 (&acc)[MT
     if constexpr (kGrad) {
         T *const d_at = static_cast<T *>(f.d) + place;
         const float factor = __is_same(T, f16) && f.largest ? factor_of(f.largest, t.lane).x : 1.0f;
-        by_rows<Ahead<O>, kLanes, (KIND >= 0)>(
-            acc, t.lds, t.lane,
-            [&](int row, Ahead<O> &a) __attribute__((always_inline)) { load_ahead<kInside>(f, t.n + row, at, cols_of(t.n + row), a); },
-            [&](int row, const float *sums, const Ahead<O> &a) __attribute__((always_inline)) {
-                float by_h[kEight];
-                read_eight(sums + col, by_h);
-                use_gate_grad<kInside, T, O, SPLIT>(f, t.n + row, at, cols_of(t.n + row), by_h, a, factor, h_at, d_at, act);
-            });
+        const auto use = [&](int row, const float *sums, const Ahead<O> &a) __attribute__((always_inline)) {
+            float by_h[kEight];
+            read_eight(sums + col, by_h);
+            use_gate_grad<kInside, T, O, SPLIT>(f, t.n + row, at, cols_of(t.n + row), by_h, a, factor, h_at, d_at, act);
+        };
+        const auto fetch = [&](int row, Ahead<O> &a) __attribute__((always_inline)) { load_ahead<kInside>(f, t.n + row, at, cols_of(t.n + row), a); };
+        if constexpr (SPLIT) {   // (nothing ahead: 16 more registers would push sums out of theirs)
+            by_rows<Nothing, kLanes, false>(acc, t.lds, t.lane, [](int, Nothing &) {},
+                                            [&](int row, const float *sums, const Nothing &) __attribute__((always_inline)) {
+                                                Ahead<O> a;
+                                                fetch(row, a);
+                                                use(row, sums, a);
+                                            });
+        } else {
+            by_rows<Ahead<O>, kLanes, (KIND >= 0)>(acc, t.lds, t.lane, fetch, use);
+        }
     } else {
         by_rows<Nothing, kLanes, (KIND >= 0)>(
             acc, t.lds, t.lane, [](int, Nothing &) {},

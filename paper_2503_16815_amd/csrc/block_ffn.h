@@ -408,7 +408,7 @@ struct Ffn {
                 f.saved.gate = {s.gate, ld, s.gate + up(n, kTile) * ld * (int64_t)sizeof(S), ld / kGroup};
                 f.saved.up = {s.up, ld, s.up + up(n, kTile) * ld * (int64_t)sizeof(S), ld / kGroup};
                 FfnArgs g = f;
-                if (by_projections) g.h = nullptr;
+                g.h = nullptr;
                 e = gate(g, x, w_gate, w_up, n, a.hidden, a.inner, s, compute_units, st);
             } else {
                 f.saved = a.saved;
@@ -419,7 +419,7 @@ struct Ffn {
                     f.largest = s.largest;
                 }
             }
-            if (e == hipSuccess && (by_projections || !again)) {   // (else the product above has left h)
+            if (e == hipSuccess) {   // (without the derivatives by the projections: h alone)
                 ProductArgs p{};
                 p.a = w_down.p;
                 p.a_ld = w_down.ld;
