@@ -1,6 +1,6 @@
 """One training step's two ends on this library's kernels, and the schedule of the gradient that they share.
 
-    python -m paper_2503_16815_amd.tied_ends [--rows 4096 --vocab 50257 --hidden 768 --k 2 --link-gbs 50]
+    python -m paper_2503_16815_amd.tied_ends [--rows 4096 --vocab 50257 --hidden 768 --k 2 --link-gbs 50 --layers 0]
 
 A language model that ties its head to its token table has one gradient that is far larger than the others:
 the table's.  The loss begins it (a piece of the vocabulary after the other), a teacher's top logits add to
@@ -10,20 +10,24 @@ measures the forward and the backward window, cuts the table's gradient into buc
 vocabulary, and lets the exact solver place them in the windows of k iterations (Sec. III.A, III.B
 of the paper).  No row of a shared table is final before the embedding's part has been added, so all buckets
 are ready at the end of the backward pass, and the windows are those that follow it; the events of the head's
-pieces tell when its part of them is written (of a head with a table of its own: when the bucket is ready).  Inputs
-are synthetic.
+pieces tell when its part of them is written (of a head with a table of its own: when the bucket is ready).
+
+With --layers that many gated feed-forward blocks follow the stand-in, each adding to the hidden states, on this library's
+kernels too.  What a layer keeps for its backward pass, its input and both projections, is kept in 8 bits; its three
+matrices' gradients are buckets beside the table's, with an event as each is final.  Inputs are synthetic.
 """
 from __future__ import annotations
 
 import argparse
 import json
 import sys
-from dataclasses import dataclass
+from dataclasses import dataclass, field
+from typing import Optional
 
 import numpy as np
 import torch
 
-from . import binding, ends as _ends, workloads as W
+from . import binding, block as _block, ends as _ends, workloads as W
 
 
 @dataclass
@@ -34,27 +38,46 @@ class Step:
     mix: torch.Tensor         # [hidden][hidden], the stand-in for the layers
     grad_table: torch.Tensor
     scale: float
+    block: Optional[_block.DeftBlock] = None
+    layers: list = field(default_factory=list)        # (w_gate, w_up, w_down) of each
+    grad_layers: list = field(default_factory=list)   # their gradients
+    save: Optional[str] = "packed"                    # what is kept of the projections; in 8 bits the layer's input too
+    kept: list = field(default_factory=list)          # of the last forward pass: the stand-in's result, and each layer's
 
     @classmethod
-    def create(cls, rows, vocab, hidden, dtype=torch.bfloat16, seed=1, top_k=32):
+    def create(cls, rows, vocab, hidden, dtype=torch.bfloat16, seed=1, top_k=32, layers=0, inner=0, save="packed"):
         g = torch.Generator(device="cuda")
         g.manual_seed(seed)
         table = (torch.randn((vocab, hidden), generator=g, device="cuda") * 0.5).to(dtype)
         mix = (torch.randn((hidden, hidden), generator=g, device="cuda") / hidden ** 0.5).to(dtype)
         ends = _ends.DeftEnds(_ends.OPERATORS, dtype, rows, vocab, hidden, top_k)
-        return cls(ends, table, mix, torch.empty_like(table), float(hidden) ** 0.5)
+        step = cls(ends, table, mix, torch.empty_like(table), float(hidden) ** 0.5, save=save)
+        if layers > 0:
+            step.block = _block.DeftBlock(_block.OPERATORS, dtype, rows, hidden, inner)
+            rand = lambda out, by: (torch.randn((out, by), generator=g, device="cuda") / by ** 0.5).to(dtype)  # noqa: E731
+            step.layers = [(rand(inner, hidden), rand(inner, hidden), rand(hidden, inner)) for _ in range(layers)]
+            step.grad_layers = [tuple(torch.empty_like(w) for w in layer) for layer in step.layers]
+        return step
 
     def forward(self, tokens, labels):
         x = self.ends.embed(tokens, self.table, scale=self.scale)
         hidden = torch.tanh(x @ self.mix)
+        self.kept = [hidden]
+        for layer in self.layers:
+            kept = self.block.checkpoint(hidden) if self.save == "packed" else hidden
+            y = self.block.ffn(hidden, *layer, save=self.save)
+            y, saved = y if self.save else (y, None)
+            self.kept.append((kept, saved))
+            hidden = hidden + y
         loss, lse = self.ends.head_loss(hidden, self.table, labels)
         return x, hidden, loss, lse
 
-    def backward(self, tokens, labels, x, hidden, lse, row_grad, distilled=None, merge=False, piece_events=None):
+    def backward(self, tokens, labels, x, hidden, lse, row_grad, distilled=None, merge=False, piece_events=None, layer_events=None):
         """Gradients of sum(row_grad * loss), and of the distilled positions' losses where `distilled` is (positions,
         teacher_index, teacher_logit, row_grad, temperature).  merge: the table's gradient of an earlier iteration,
         whose update is delayed, is added to.  piece_events: recorded as the head's part of each piece of the table's
-        gradient is written; the distilled positions' part and the embedding's are added to all pieces after that."""
+        gradient is written; the distilled positions' part and the embedding's are added to all pieces after that.
+        layer_events: two of each layer, recorded as its gradients are final (w_down's, then the others')."""
         grad_hidden, grad_table = self.ends.head_grad(hidden, self.table, labels, lse, row_grad, grad_weight=self.grad_table,
                                                       accumulate=merge, piece_events=piece_events)
         extra = None
@@ -65,23 +88,36 @@ class Step:
             extra, d = self.ends.distill_grad(logits, index, value, by, temperature, grad_logits=logits)
             grad_hidden.index_add_(0, at, d @ self.table)
             grad_table.addmm_(d.T, picked)
-        d = grad_hidden * (1 - hidden * hidden)
+        for i in reversed(range(len(self.layers))):
+            kept, saved = self.kept[1 + i]
+            gate, up, down = self.grad_layers[i]
+            grad_hidden = grad_hidden + self.block.ffn_grad(
+                grad_hidden, kept, *self.layers[i], saved=saved, grad_gate=gate, grad_up=up, grad_down=down, accumulate=merge,
+                events=layer_events[i] if layer_events else None)[0]
+        mixed = self.kept[0] if self.layers else hidden
+        d = grad_hidden * (1 - mixed * mixed)
         grad_mix = x.T @ d
         self.ends.embed_grad(tokens, d @ self.mix.T, grad_table=grad_table, scale=self.scale, accumulate=True)
         return grad_table, grad_mix, extra
 
 
 def schedule(step: Step, forward_us: float, backward_us: float, k: int, link_gbs: float):
-    """The table's gradient placed by the exact solver in the forward and backward windows of the k iterations after
+    """The table's gradient, and the layers' behind it, placed by the exact solver in the forward and backward windows of the k iterations after
     the one that computed it, at whose end it is ready; times in 10 us units, value = communication time (Sec. III.B,
-    Problem 1).  A piece of the vocabulary is a bucket, cut further where it would take more than a quarter of the
-    smaller window (Sec. III.D: a bucket has to fit)."""
+    Problem 1).  A piece of the vocabulary is a bucket, and so is a layer's matrix, cut further where it would take more than
+    a quarter of the smaller window (Sec. III.D: a bucket has to fit)."""
     vocab, hidden = step.table.shape
     unit = 10.0
     row_us = hidden * step.table.element_size() / (link_gbs * 1e3)
     piece = min(step.ends.info().vocab_piece, vocab, max(1, int(min(forward_us, backward_us) / 4 / row_us)))
     rows = [min(piece, vocab - at) for at in range(0, vocab, piece)]
-    item = np.array([[max(1, round(r * row_us / unit)) for r in rows]], np.int32)
+    times = [r * row_us for r in rows]
+    most_us = min(forward_us, backward_us) / 4
+    for w in (w for layer in step.layers for w in layer):
+        us = w.numel() * w.element_size() / (link_gbs * 1e3)
+        parts = max(1, int(np.ceil(us / most_us)))
+        times += [us / parts] * parts
+    item = np.array([[max(1, round(t / unit)) for t in times]], np.int32)
     caps = np.array([[max(1, int(t / unit)) for t in (forward_us, backward_us)] * k], np.int32)
     kb = W.KnapsackBatch("tied_ends", W.MODE_SEQUENTIAL, 1, item.shape[1], 2 * k, np.array([item.shape[1]], np.int32),
                          np.array([2 * k], np.int32), item, item.copy(), caps)
@@ -90,14 +126,15 @@ def schedule(step: Step, forward_us: float, backward_us: float, k: int, link_gbs
 
 def main(argv=None) -> int:
     ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
-    for name, value in (("rows", 4096), ("vocab", 50257), ("hidden", 768), ("k", 2), ("top-k", 32), ("steps", 5)):
+    for name, value in (("rows", 4096), ("vocab", 50257), ("hidden", 768), ("k", 2), ("top-k", 32), ("steps", 5), ("layers", 0),
+                        ("inner", 0)):
         ap.add_argument("--" + name, type=int, default=value)
     ap.add_argument("--link-gbs", type=float, default=50.0, help="rate of the link that the buckets take")
     a = ap.parse_args(argv)
     if not torch.cuda.is_available():
         print("tied_ends: no GPU visible", file=sys.stderr)
         return 1
-    step = Step.create(a.rows, a.vocab, a.hidden, top_k=a.top_k)
+    step = Step.create(a.rows, a.vocab, a.hidden, top_k=a.top_k, layers=a.layers, inner=a.inner or max(1, a.hidden * 8 // 3))
     g = torch.Generator(device="cuda")
     g.manual_seed(7)
     tokens = torch.randint(0, a.vocab, (a.rows,), generator=g, device="cuda", dtype=torch.int32)
@@ -111,20 +148,23 @@ def main(argv=None) -> int:
     for n in range(a.steps):
         marks = [torch.cuda.Event(enable_timing=True) for _ in range(3)]
         head_part = [torch.cuda.Event(enable_timing=True) for _ in range(pieces)]
+        of_layers = [[torch.cuda.Event(enable_timing=True) for _ in range(2)] for _ in range(a.layers)]
         marks[0].record()
         x, hidden, loss, lse = step.forward(tokens, labels)
         marks[1].record()
-        step.backward(tokens, labels, x, hidden, lse, row_grad, distilled, merge=n % a.k != 0, piece_events=head_part)
+        step.backward(tokens, labels, x, hidden, lse, row_grad, distilled, merge=n % a.k != 0, piece_events=head_part,
+                      layer_events=of_layers)
         marks[2].record()   # (every piece of the table's gradient is final)
     torch.cuda.synchronize()
     forward_us, backward_us = (1e3 * marks[i].elapsed_time(marks[i + 1]) for i in range(2))
     kb, out = schedule(step, forward_us, backward_us, a.k, a.link_gbs)
+    more = {"layers_ready_us": [[1e3 * marks[1].elapsed_time(e) for e in events] for events in of_layers]} if a.layers else {}
     print(json.dumps({
         "loss": float(loss.sum() / (a.rows - 1)), "forward_us": forward_us, "backward_us": backward_us,
         "head_part_us": [1e3 * marks[1].elapsed_time(e) for e in head_part], "pieces_ready_us": [backward_us] * pieces,
         "unit_us": 10,
         "bucket_times": kb.weights[0].tolist(), "windows": kb.capacities[0].tolist(),
-        "window_of_bucket": out.assignment[0].tolist(), "time_hidden": int(out.total_value[0])}))
+        "window_of_bucket": out.assignment[0].tolist(), "time_hidden": int(out.total_value[0]), **more}))
     return 0
 
 

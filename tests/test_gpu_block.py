@@ -113,7 +113,8 @@ def test_strides_and_addresses(block, n, pad, shift, dtype):
 
 # (tests/test_block_plans.py has which shape of tiles, and how many parts, each product takes here)
 SHAPES = [(4096, 1024, 2048), (8192, 1600, 640), (700, 640, 1728), (1003, 1021, 2731), (2048, 768, 2048), (100, 1500, 4500), (1024, 64, 8192),
-          (64, 512, 4096), (33, 2048, 512), (2304, 2304, 512), (1536, 1536, 6144)]
+          (64, 512, 4096), (33, 2048, 512), (2304, 2304, 512), (1536, 1536, 6144), (7372, 1088, 64), (8302, 416, 64), (5972, 2176, 64),
+          (322, 64, 5504), (8251, 64, 416), (7289, 64, 1056), (75, 320, 8224)]
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
