@@ -156,19 +156,22 @@ class DeftBlock(Marshalling):
         n, width = self._rows("x", x, None, None)
         if out is None:
             out = self._new_checkpoint(n, width)
+        else:
+            self._check("out", out, n, width)
         self._call("deft_checkpoint", ctypes.byref(deft_checkpoint_call_t(
-            n, width, _p(x), _ld(x), self._packed("out", out, n, width), self._stream())))
+            n, width, _p(x), _ld(x), _packed(out), self._stream())))
         return out
 
     @_on_stream
     def restore(self, kept: Checkpoint, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """What a checkpoint stands for, in the handle's type."""
-        n, width = self._matrix("codes", _codes("kept", kept), torch.int8, None, None)
-        packed = self._packed("kept", kept, n, width)
+        n, width = self._check("kept", kept, None, None)
         if out is None:
             out = torch.empty((n, width), dtype=self.dtype, device=self.device)
-        self._rows("out", out, n, width)
-        self._call("deft_restore", ctypes.byref(deft_restore_call_t(n, width, packed, _p(out), _ld(out), self._stream())))
+        else:
+            self._rows("out", out, n, width)
+        self._call("deft_restore", ctypes.byref(deft_restore_call_t(
+            n, width, _packed(kept), _p(out), _ld(out), self._stream())))
         return out
 
     @_on_stream
@@ -180,14 +183,15 @@ class DeftBlock(Marshalling):
         kind, saves = self._choice("activation", activation, ACTIVATIONS), self._choice("save", save, SAVES)
         if out is None:
             out = torch.empty((n, hidden), dtype=self.dtype, device=self.device)
-        self._rows("out", out, n, hidden)
+        else:
+            self._rows("out", out, n, hidden)
         saved = None
         if save is not None:
             codes = torch.int8 if save == "packed" else torch.float32 if self.dtype == torch.float32 else torch.int16
             saved = Saved(self._new_checkpoint(n, inner, codes), self._new_checkpoint(n, inner, codes))
         self._call("deft_ffn", ctypes.byref(deft_ffn_t(
             n, hidden, inner, kind, _p(x), _ld(x), _p(w_gate), _ld(w_gate), _p(w_up), _ld(w_up), _p(w_down), _ld(w_down),
-            _p(out), _ld(out), self._saved(saved, saves, n, inner), self._stream())))
+            _p(out), _ld(out), _kept(saved, saves), self._stream())))
         return out if save is None else (out, saved)
 
     @_on_stream
@@ -204,14 +208,19 @@ class DeftBlock(Marshalling):
         kind = self._choice("activation", activation, ACTIVATIONS)
         packed_x = deft_checkpoint_t()
         if isinstance(x, Checkpoint):
-            packed_x = self._packed("x", x, n, hidden)
+            self._check("x", x, n, hidden)
+            packed_x = _packed(x)
         else:
             self._rows("x", x, n, hidden)
         saves = 0
         if saved is not None:
             if not isinstance(saved, Saved):
                 raise ValueError("saved: what ffn gave is wanted")
-            saves = SAVES["packed" if _codes("saved.gate", saved.gate).dtype == torch.int8 else "full"]
+            wide = torch.float32 if self.dtype == torch.float32 else torch.int16
+            packed = isinstance(saved.gate, Checkpoint) and saved.gate.codes.dtype == torch.int8
+            self._check("saved.gate", saved.gate, n, inner, torch.int8 if packed else wide)
+            self._check("saved.up", saved.up, n, inner, torch.int8 if packed else wide)
+            saves = SAVES["packed" if packed else "full"]
         if accumulate and (not need_weights or grad_gate is None or grad_up is None or grad_down is None):
             raise ValueError("accumulate needs grad_gate, grad_up and grad_down")
         if not need_x and not need_weights:
@@ -238,7 +247,7 @@ class DeftBlock(Marshalling):
         of_x = (None, 0) if isinstance(x, Checkpoint) else (_p(x), _ld(x))
         self._call("deft_ffn_grad", ctypes.byref(deft_ffn_grad_t(
             n, hidden, inner, kind, int(accumulate), _p(grad_y), _ld(grad_y), *of_x, packed_x, _p(w_gate), _ld(w_gate),
-            _p(w_up), _ld(w_up), _p(w_down), _ld(w_down), self._saved(saved, saves, n, inner), _p(grad_x), _ld(grad_x),
+            _p(w_up), _ld(w_up), _p(w_down), _ld(w_down), _kept(saved, saves), _p(grad_x), _ld(grad_x),
             _p(grad_gate), _ld(grad_gate), _p(grad_up), _ld(grad_up), _p(grad_down), _ld(grad_down),
             ctypes.cast(handles, _vp) if handles else None, self._stream())))
         return grad_x, grad_gate, grad_up, grad_down
@@ -258,27 +267,23 @@ class DeftBlock(Marshalling):
         return inner
 
     def _new_checkpoint(self, n, width, dtype=torch.int8):   # (rows from 16-byte boundaries on)
-        codes = torch.empty((n, -(-width // 16) * 16), dtype=dtype, device=self.device)
-        groups = -(-width // GROUP)
-        scales = None if dtype == torch.float32 else torch.empty((n, groups), dtype=torch.bfloat16, device=self.device)
-        return Checkpoint(codes[:, :width], scales)
+        codes = torch.empty_strided((n, width), (-(-width // 16) * 16, 1), dtype=dtype, device=self.device)
+        if dtype == torch.float32:
+            return Checkpoint(codes, None)
+        return Checkpoint(codes, torch.empty((n, -(-width // GROUP)), dtype=torch.bfloat16, device=self.device))
 
-    def _packed(self, name, kept, n, width, dtype=torch.int8):
-        self._matrix(name + ".codes", _codes(name, kept), dtype, n, width)
+    def _check(self, name, kept, n, width, dtype=torch.int8):
+        if not isinstance(kept, Checkpoint):
+            raise ValueError(f"{name}: a Checkpoint is wanted")
+        n, width = self._matrix(name + ".codes", kept.codes, dtype, n, width)
         if dtype != torch.float32:
             self._matrix(name + ".scales", kept.scales, torch.bfloat16, n, -(-width // GROUP))
-        return deft_checkpoint_t(_p(kept.codes), _ld(kept.codes), *((None, 0) if dtype == torch.float32 else
-                                                                    (_p(kept.scales), _ld(kept.scales))))
-
-    def _saved(self, saved, kind, n, inner):
-        if saved is None:
-            return deft_saved_t()
-        codes = torch.int8 if kind == SAVES["packed"] else torch.float32 if self.dtype == torch.float32 else torch.int16
-        return deft_saved_t(kind, self._packed("saved.gate", saved.gate, n, inner, codes),
-                            self._packed("saved.up", saved.up, n, inner, codes))
+        return n, width
 
 
-def _codes(name, kept):
-    if not isinstance(kept, Checkpoint):
-        raise ValueError(f"{name}: a Checkpoint is wanted")
-    return kept.codes
+def _packed(kept):
+    return deft_checkpoint_t(_p(kept.codes), _ld(kept.codes), _p(kept.scales), _ld(kept.scales))
+
+
+def _kept(saved, kind):
+    return deft_saved_t(kind, _packed(saved.gate), _packed(saved.up)) if saved is not None else deft_saved_t()

@@ -135,14 +135,14 @@ class Marshalling:
     def _matrix(self, name, t, dtype, rows, width):
         if not isinstance(t, torch.Tensor) or t.dim() != 2 or t.dtype != dtype or t.get_device() != self._index:
             raise ValueError(f"{name}: a matrix of {dtype} on {self.device} is wanted")
-        n, w = t.shape
+        n, w = shape = t.shape
         if n > _MOST or w > _MOST:
             raise ValueError(f"{name}: sizes of 32 bits are wanted, got {(n, w)}")
         if (rows is not None and n != rows) or (width is not None and w != width):
             raise ValueError(f"{name}: shape {(n, w)} does not fit {(rows, width)}")
         if not t.is_contiguous() and ((w > 1 and t.stride(1) != 1) or (n > 1 and t.stride(0) < w)):
             raise ValueError(f"{name}: a row's elements have to be next to each other, rows apart")
-        return n, w
+        return shape
 
     def _words(self, name, t, dtype, shape):
         if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.get_device() != self._index or not t.is_contiguous():

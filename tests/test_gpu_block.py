@@ -289,7 +289,7 @@ def _one_gradient(block, b, gy, x, weights, saved, which, out):
                     (("grad_x", "grad_gate", "grad_up", "grad_down")[which], out)):
         setattr(a, name, t.data_ptr())
         setattr(a, name + "_stride", t.stride(0))
-    a.saved = b._saved(saved, 1 if saved else 0, a.n_rows, a.inner)
+    a.saved = block._kept(saved, 1)
     a.stream = b._stream()
     b._call("deft_ffn_grad", ctypes.byref(a))
     return out
