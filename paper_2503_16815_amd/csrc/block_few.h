@@ -5,8 +5,9 @@
 // inner product's terms may come in any order, as long as both operands' do in the same; a tile of 32-bit operands takes
 // four instructions, one for each element of a lane's 16 bytes).  The wavefronts' sums meet in LDS.
 //
-// The hidden activations go from the first launch to the second as two numbers of the type, the rounded one and what the rounding
-// took: the matrix instructions idle anyway, so y is rounded once.
+// Of up to 8 tokens the hidden activations go from the first launch to the second as two numbers of the type, the rounded one and
+// what the rounding took, which are the two halves of a tile's sixteen rows: so y is rounded once.  (Of more they would be a second
+// tile: 16 tokens of 1600 x 6400 bf16 30 us.)
 #pragma once
 #include "block_epilogue.h"
 #include "ends_shapes.h"
@@ -19,17 +20,17 @@ constexpr int kGateWaves = 8, kOutWaves = 16;   // that share a workgroup's rows
 template <typename S> struct FewTile;   // how a wavefront multiplies sixteen rows by sixteen
 template <> struct FewTile<bf16> {
     typedef bf16 operand __attribute__((ext_vector_type(8)));
-    static constexpr int kVec = 8, kArrays = 2;
+    static constexpr int kVec = 8;
     static __device__ __forceinline__ f32x4 run(operand a, operand b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 };
 template <> struct FewTile<f16> {
     typedef f16 operand __attribute__((ext_vector_type(8)));
-    static constexpr int kVec = 8, kArrays = 2;
+    static constexpr int kVec = 8;
     static __device__ __forceinline__ f32x4 run(operand a, operand b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 };
 template <> struct FewTile<float> {
     typedef float operand __attribute__((ext_vector_type(4)));
-    static constexpr int kVec = 4, kArrays = 1;
+    static constexpr int kVec = 4;
     static __device__ __forceinline__ f32x4 run(operand a, operand b, f32x4 c)
     {
 #pragma unroll
@@ -38,18 +39,18 @@ template <> struct FewTile<float> {
     }
 };
 
-// Sums of MT tiles of rows with NT tiles of (arrays of) rows over this wavefront's part of k.  All of a few steps' loads are on
+// Sums of MT tiles of rows with NT tiles of rows over this wavefront's part of k.  All of a few steps' loads are on
 // their way before the first is multiplied (in the order that the compiler would choose, few are).
-template <typename S, int WAVES, int MT, int NT, int ARRAYS>
-__device__ __forceinline__ void few_sums(const S *const (&rows_a)[MT], const S *const (&rows_b)[NT], int64_t b_array, int k_all, int wave, int lane,
+template <typename S, int WAVES, int MT, int NT>
+__device__ __forceinline__ void few_sums(const S *const (&rows_a)[MT], const S *const (&rows_b)[NT], int k_all, int wave, int lane,
                                          f32x4 (&acc)[MT][NT])
 {
     typedef typename FewTile<S>::operand Operand;
     typedef S Loaded __attribute__((ext_vector_type(FewTile<S>::kVec), aligned(sizeof(S))));
     constexpr int kVec = FewTile<S>::kVec, kFewStep = 8 * kVec;   // a lane has two pieces of 16 bytes: a row's are 128
-    constexpr int kEach = MT + NT * ARRAYS, kAhead = kEach > 7 ? 2 : 16 / kEach / 2 * 2;   // pieces at a time, about 64 registers of them
+    constexpr int kEach = MT + NT, kAhead = kEach > 7 ? 2 : 16 / kEach / 2 * 2;   // pieces at a time, about 64 registers of them
     struct Batch {
-        Operand x[kAhead][MT], y[kAhead][NT][ARRAYS];
+        Operand x[kAhead][MT], y[kAhead][NT];
     };
     const int steps = (k_all + kFewStep - 1) / kFewStep, last = steps * (wave + 1) / WAVES;
     const int part = (lane >> 4) * 2 * kVec;
@@ -65,9 +66,7 @@ __device__ __forceinline__ void few_sums(const S *const (&rows_a)[MT], const S *
 #pragma unroll
             for (int i = 0; i < MT; ++i) w.x[q][i] = *reinterpret_cast<const Loaded *>(a[i] + (q >> 1) * kFewStep + (q & 1) * kVec);
 #pragma unroll
-            for (int j = 0; j < NT; ++j)
-#pragma unroll
-                for (int s = 0; s < ARRAYS; ++s) w.y[q][j][s] = *reinterpret_cast<const Loaded *>(b[j] + s * b_array + (q >> 1) * kFewStep + (q & 1) * kVec);
+            for (int j = 0; j < NT; ++j) w.y[q][j] = *reinterpret_cast<const Loaded *>(b[j] + (q >> 1) * kFewStep + (q & 1) * kVec);
         }
 #pragma unroll
         for (int i = 0; i < MT; ++i) a[i] += kAhead / 2 * kFewStep;
@@ -81,9 +80,7 @@ __device__ __forceinline__ void few_sums(const S *const (&rows_a)[MT], const S *
 #pragma unroll
             for (int i = 0; i < MT; ++i)
 #pragma unroll
-                for (int j = 0; j < NT; ++j)
-#pragma unroll
-                    for (int s = 0; s < ARRAYS; ++s) acc[i][j] = FewTile<S>::run(w.x[q][i], w.y[q][j][s], acc[i][j]);
+                for (int j = 0; j < NT; ++j) acc[i][j] = FewTile<S>::run(w.x[q][i], w.y[q][j], acc[i][j]);
         __builtin_amdgcn_sched_barrier(0);
     };
     const int whole = min(last, k_all / kFewStep);   // steps that end within the rows
@@ -105,9 +102,7 @@ __device__ __forceinline__ void few_sums(const S *const (&rows_a)[MT], const S *
 #pragma unroll
             for (int i = 0; i < MT; ++i) rest.x[q][i] = *reinterpret_cast<const Loaded *>(a[i] + (q >> 1) * kFewStep + (q & 1) * kVec);
 #pragma unroll
-            for (int j = 0; j < NT; ++j)
-#pragma unroll
-                for (int s = 0; s < ARRAYS; ++s) rest.y[q][j][s] = *reinterpret_cast<const Loaded *>(b[j] + s * b_array + (q >> 1) * kFewStep + (q & 1) * kVec);
+            for (int j = 0; j < NT; ++j) rest.y[q][j] = *reinterpret_cast<const Loaded *>(b[j] + (q >> 1) * kFewStep + (q & 1) * kVec);
         } else {
 #pragma unroll
             for (int r = 0; r < kVec; ++r) {
@@ -115,9 +110,7 @@ __device__ __forceinline__ void few_sums(const S *const (&rows_a)[MT], const S *
 #pragma unroll
                 for (int i = 0; i < MT; ++i) rest.x[q][i][r] = a[i][(q >> 1) * kFewStep + (q & 1) * kVec + r];
 #pragma unroll
-                for (int j = 0; j < NT; ++j)
-#pragma unroll
-                    for (int s = 0; s < ARRAYS; ++s) rest.y[q][j][s][r] = b[j][s * b_array + (q >> 1) * kFewStep + (q & 1) * kVec + r];
+                for (int j = 0; j < NT; ++j) rest.y[q][j][r] = b[j][(q >> 1) * kFewStep + (q & 1) * kVec + r];
             }
         }
     }
@@ -130,6 +123,7 @@ struct FewArgs {
     int64_t x_stride, w_gate_stride, w_up_stride, w_down_stride;
     void *h;             // [arrays][n][h_stride]
     int64_t h_stride, h_array;
+    int h_arrays;
     deft_saved_t saved;
     void *y;
     int64_t y_stride;
@@ -201,7 +195,7 @@ __global__ void __launch_bounds__(kGateWaves *kWave, 4) few_gate_kernel(FewArgs 
 #pragma unroll
     for (int j = 0; j < NT; ++j) x[j] = static_cast<const S *>(a.x) + min(j * 16 + row16, a.n - 1) * a.x_stride;
     f32x4 acc[MT][NT] = {};
-    few_sums<S, kGateWaves, MT, NT, 1>(w, x, 0, a.hidden, wave, lane, acc);
+    few_sums<S, kGateWaves, MT, NT>(w, x, a.hidden, wave, lane, acc);
     const int token = tid / kCols, col = tid % kCols, at = first + col;
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
@@ -226,11 +220,8 @@ __global__ void __launch_bounds__(kGateWaves *kWave, 4) few_gate_kernel(FewArgs 
         else act_of<DEFT_RELU, kExact>(gate, y, slope);
         S *h = static_cast<S *>(a.h) + n * a.h_stride + at;
         float rest = y * up;
-#pragma unroll
-        for (int s = 0; s < FewTile<S>::kArrays; ++s) {
-            h[s * a.h_array] = (S)rest;
-            rest -= (float)(S)rest;
-        }
+        *h = (S)rest;
+        if (a.h_arrays == 2) h[a.h_array] = (S)(rest - (float)(S)rest);
     }
 }
 
@@ -247,7 +238,7 @@ __global__ void __launch_bounds__(kOutWaves *kWave) few_out_kernel(FewArgs a)
     for (int j = 0; j < NT; ++j)
         h[j] = static_cast<const S *>(a.h) + (FOLD ? (row16 >> 3) * a.h_array : 0) + min(FOLD ? row16 & 7 : j * 16 + row16, a.n - 1) * a.h_stride;
     f32x4 acc[MT][NT] = {};
-    few_sums<S, kOutWaves, MT, NT, FOLD ? 1 : FewTile<S>::kArrays>(w, h, a.h_array, a.inner, wave, lane, acc);
+    few_sums<S, kOutWaves, MT, NT>(w, h, a.inner, wave, lane, acc);
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
         f32x4 own[MT];
@@ -270,8 +261,8 @@ hipError_t few_tokens(const FewArgs &a, int compute_units, hipStream_t st)
     if (a.saved.kind == DEFT_SAVE_NONE) few_gate_kernel<S, 1, NT><<<(a.inner + 15) / 16, kGateWaves * kWave, 0, st>>>(a);
     else few_gate_kernel<S, 2, NT><<<(a.inner + 31) / 32, kGateWaves * kWave, 0, st>>>(a);
     const unsigned ones = (unsigned)(a.hidden + 15) / 16, twos = (unsigned)(a.hidden + 31) / 32;
-    if constexpr (NT == 1 && FewTile<S>::kArrays == 2)
-        if (a.n <= 8) {
+    if constexpr (NT == 1 && sizeof(S) == 2)
+        if (a.h_arrays == 2) {
             few_out_kernel<S, 1, 1, true><<<ones, kOutWaves * kWave, 0, st>>>(a);
             return hipGetLastError();
         }

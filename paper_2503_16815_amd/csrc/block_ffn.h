@@ -338,6 +338,7 @@ struct Ffn {
         f.h = s.h;
         f.h_stride = up(a.inner, 8);
         f.h_array = kFew * f.h_stride;   // (within the room for a tile's rows)
+        f.h_arrays = !kSplit && f.n <= 8 ? 2 : 1;
         f.saved = a.save;
         f.y = a.y;
         f.y_stride = a.y_stride;
