@@ -18,9 +18,14 @@
  * of 16 bytes are quicker.  Arrays may pass 2^31 elements.  Outputs must not overlap inputs.
  *
  * Sums are held in 32 bits, each in one fixed order (results do not change from call to call), and
- * outputs are rounded once to the handle's type.  In 16-bit types what one product leaves to the
- * next (the hidden activations, and the derivatives by the two projections) is rounded to the type
- * in between, as the matrix instructions take it; in 32 bits it is not.
+ * outputs are rounded once to the handle's type.  In 16-bit types of more than 64 rows what one
+ * product leaves to the next (the hidden activations, and the derivatives by the two projections) is
+ * rounded to the type in between, as the matrix instructions take it, so that an output's error is
+ * about sqrt 2 of its own rounding's; in 32 bits, and of fewer rows (but in y of 9 to 16), it is not.
+ * Hidden activations beyond the range of 16-bit floats are infinite there.
+ *
+ * Rows that stand for nothing (the padding of a batch) are rows of zeros, as deft_embed gives them
+ * for a token of -1: they add nothing to any gradient.
  */
 #ifndef DEFT_BLOCK_H
 #define DEFT_BLOCK_H
@@ -116,9 +121,10 @@ enum { DEFT_SILU = 0, DEFT_GELU = 1, DEFT_GELU_TANH = 2, DEFT_RELU = 3 };
 enum { DEFT_SAVE_NONE = 0, DEFT_SAVE_FULL = 1, DEFT_SAVE_PACKED = 2 };
 
 /* of width `inner`.  FULL: in 32 bits `codes` are the numbers themselves (float) and there are no
- * scales; in 16-bit types they are checkpoints whose codes are int16 (-32767 .. 32767, -32768 for what is
- * not finite), in 16.5 bits an element off by at most (1 + 2^-7) / 65534 of the group's largest:
- * so they are as good as the sums in 32 bits for what is rounded to the type afterwards. */
+ * scales; in 16-bit types they are checkpoints whose codes are int16 (-32767 .. 32767), in 16.5 bits an
+ * element off by at most (1 + 2^-7) / 65534 of the group's largest: as good as the sums in 32 bits for what
+ * is rounded to the type afterwards.  A sum within its own error of the middle between two codes may get
+ * either.  A group with a sum that is not finite has NaN as its scale, and comes back as NaN. */
 typedef struct {
     int32_t kind;          /* DEFT_SAVE_*                                                      */
     deft_checkpoint_t gate, up;
@@ -161,8 +167,8 @@ deft_status_t deft_ffn(deft_block_t *h, const deft_ffn_t *a);
  * checkpoint.  events (a HOST array of two hipEvent_t, or NULL) are recorded on the stream: the first once
  * grad_down is written, the second once grad_gate and grad_up are; grad_x comes last.  Such a call must
  * not be captured.
- * Where rows of x or grad_y hold infinities or NaN, so do the gradients that they have a part in (NaN
- * possibly in the place of an infinity).
+ * Where rows of x or grad_y hold infinities or NaN, so do their rows of grad_x and the matrices' gradients (NaN
+ * possibly in the place of an infinity); other rows of grad_x do not.
  * In 16-bit floats d_gate and d_up are held times a power of two that brings grad_y's largest magnitude to
  * 1 .. 2: elements below 2^-14 of that lose bits, one more than 2^15 times it is infinite.
  */

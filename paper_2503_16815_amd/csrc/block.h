@@ -12,6 +12,9 @@ struct FfnArgs {
     int64_t a2_ld, a2_plane;
     int64_t a_panel;                 // kOuter: elements between a's panels (256: rows as they are)
     int64_t d_half;                  // kInput: elements between b's halves
+    int arrays;                      // 16-bit types: 1, or 2 where h and d have a second array, what rounding took of the first
+    int64_t b_array;                 // kOut, kInput: elements between the two of b
+    int64_t a_step, b_step;          // kOuter: elements from a step's rows to the next one's (0: the second array's step takes the same)
     // kGate, kGateGrad
     int activation;
     int cols_up;                     // columns of the panels of h, and of each half of d's

@@ -211,9 +211,10 @@ __device__ __forceinline__ void use_saved(int kind, const Kept<O> &k, float (&x)
     }
 }
 
-// Eight elements of an operand in panels: one array of T, or three of bf16 whose sum they are.
+// Eight elements of an operand in panels: one array of T, two where the second has what rounding took of the first, or three of bf16
+// whose sum they are.
 template <typename T, bool SPLIT>
-__device__ __forceinline__ void store_operand(T *to, int64_t plane, const float (&x)[kEight])
+__device__ __forceinline__ void store_operand(T *to, int64_t plane, int arrays, const float (&x)[kEight])
 {
     typedef T T8 __attribute__((ext_vector_type(8)));
     if constexpr (SPLIT) {
@@ -232,6 +233,11 @@ __device__ __forceinline__ void store_operand(T *to, int64_t plane, const float 
 #pragma unroll
         for (int r = 0; r < kEight; ++r) y[r] = (T)x[r];
         *reinterpret_cast<T8 *>(to) = y;
+        if (arrays == 2) {
+#pragma unroll
+            for (int r = 0; r < kEight; ++r) y[r] = (T)(x[r] - (float)y[r]);
+            *reinterpret_cast<T8 *>(to + plane) = y;
+        }
     }
 }
 
@@ -360,7 +366,7 @@ struct Tile {
 };
 
 // Eight elements of both projections, of row n and from column `at` on; own_cols: the columns that the row has (0: no such row, zeros
-// in h).  h_at: where h has the column.
+// in h).  h_at: where h has the column.  kInside: the row and the group's columns are there, and operands are one array (or three).
 template <bool kInside, typename T, typename O, bool SPLIT, typename Act>
 __device__ __forceinline__ void use_gate(const FfnArgs &f, int n, int at, int own_cols, const float (&gate)[kEight], const float (&up)[kEight], T *h_at, Act act)
 {
@@ -373,7 +379,7 @@ __device__ __forceinline__ void use_gate(const FfnArgs &f, int n, int at, int ow
     act(gate, y, slope);
 #pragma unroll
     for (int r = 0; r < kEight; ++r) y[r] = kInside || at + r < own_cols ? y[r] * up[r] : 0.0f;
-    store_operand<T, SPLIT>(h_at + (int64_t)n * 256, f.h_plane, y);
+    store_operand<T, SPLIT>(h_at + (int64_t)n * 256, f.h_plane, kInside ? 1 : f.arrays, y);
 }
 
 template <typename O> struct Ahead {
@@ -399,10 +405,10 @@ __device__ __forceinline__ void use_gate_grad(const FfnArgs &f, int n, int at, i
         up[r] = here ? d * y[r] : 0.0f;
     }
     const int64_t from = (int64_t)n * 256;
-    if (f.h) store_operand<T, SPLIT>(h_at + from, f.h_plane, h);
+    if (f.h) store_operand<T, SPLIT>(h_at + from, f.h_plane, kInside ? 1 : f.arrays, h);
     if (f.d) {
-        store_operand<T, SPLIT>(d_at + from, f.d_plane, gate);
-        store_operand<T, SPLIT>(d_at + (f.cols_up >> 8) * f.panel + from, f.d_plane, up);
+        store_operand<T, SPLIT>(d_at + from, f.d_plane, kInside ? 1 : f.arrays, gate);
+        store_operand<T, SPLIT>(d_at + (f.cols_up >> 8) * f.panel + from, f.d_plane, kInside ? 1 : f.arrays, up);
     }
 }
 
@@ -461,7 +467,7 @@ template <bool kGrad, typename T, typename O, int MT, int NT, bool SPLIT>
 __device__ __forceinline__ void act_epilogue(const FfnArgs &f, const f32x4 (&acc)[MT][NT], const Tile &t)
 {
     static_assert(MT % 4 == 0);   // whole groups of 32
-    const bool inside = t.n + NT * 16 <= t.n_rows && t.m + MT * (kGrad ? 16 : 8) <= t.cols;
+    const bool inside = f.arrays == 1 && t.n + NT * 16 <= t.n_rows && t.m + MT * (kGrad ? 16 : 8) <= t.cols;
     if (!inside) return act_rows<kGrad, -1, false, T, O, MT, NT, SPLIT>(f, acc, t);
     if constexpr (SPLIT) {   // (32-bit operands are multiplied six times over: less of the whole, and twice the registers)
         act_rows<kGrad, -1, true, T, O, MT, NT, SPLIT>(f, acc, t);

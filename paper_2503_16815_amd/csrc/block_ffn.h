@@ -100,7 +100,7 @@ __global__ void __launch_bounds__(256) join_act_kernel(JoinArgs a)
     const RowPieces by(blockIdx.x, (a.n + kStep - 1) / kStep * kStep, (a.m + kStep - 1) / kStep * kStep);
     for (int i = threadIdx.x; i < by.count; i += 256) {
         const int n = by.row(i), at = by.piece(i) * kEight;
-        if (n < a.n && (at & -kGroup) + kGroup <= a.m) eight(std::true_type{}, n, at);   // (a group's four lanes go the same way)
+        if (f.arrays == 1 && n < a.n && (at & -kGroup) + kGroup <= a.m) eight(std::true_type{}, n, at);   // (a group's four lanes go the same way)
         else eight(std::false_type{}, n, at);
     }
 }
@@ -227,9 +227,12 @@ struct Ffn {
         FfnArgs f{};
         f.activation = activation;
         f.cols_up = (int)up(inner, 256);
-        f.panel = up(n, kTile) * 256;
-        f.h_plane = f.cols_up / 256 * f.panel;
-        f.d_plane = 2 * f.h_plane;
+        // Up to 64 rows the products are bound by reading and writing the matrices: what is rounded in between keeps what that took, in
+        // 64 more rows of each panel.
+        f.arrays = !kSplit && n <= kFew ? 2 : 1;
+        f.panel = up(n, n <= kFew ? kFew * f.arrays : kTile) * 256;
+        f.h_plane = f.arrays == 2 ? kFew * 256 : f.cols_up / 256 * f.panel;
+        f.d_plane = f.arrays == 2 ? kFew * 256 : 2 * f.h_plane;
         f.h = s.h;
         f.half = f.rows = INT32_MAX;
         f.a_panel = 256;
@@ -258,7 +261,7 @@ struct Ffn {
     static hipError_t parts(ProductArgs &p, int cols, const FfnScratch &s, int compute_units, hipStream_t st)
     {
         constexpr unsigned kWithout = E == kGate || E == kGateGrad ? kNoAct : kNoOther;
-        const int64_t steps = (int64_t)(p.k / kStep) * (kSplit ? 6 : 1) * (E == kInput ? 2 : 1);
+        const int64_t steps = (int64_t)(p.k / kStep) * (kSplit ? 6 : 1) * (E == kInput ? 2 : 1) * (E == kOut || E == kInput ? p.ffn.arrays : 1);
         p.splits = parts_of(cols, p.n, steps, compute_units, kWithout);
         p.sums = s.sums;
         p.sums_ld = up(cols, kEight);
@@ -377,6 +380,7 @@ struct Ffn {
         p.n = a.n_rows;
         p.k = (int)up(a.inner, kStep);
         p.ffn = f;
+        p.ffn.b_array = f.h_plane;
         p.ffn.out[0] = a.y;
         p.ffn.out_ld[0] = a.y_stride;
         return summed<kOut>(p, s, compute_units, st);
@@ -440,7 +444,7 @@ struct Ffn {
         }
         const bool weights = n > 0 || !a.accumulate;
         ProductArgs q{};   // of the matrices' gradients
-        q.k = (int)up(n, kStep);
+        q.k = (int)up(n, kStep) * f.arrays;
         q.add = a.accumulate;
         q.ffn = f;
         if (e == hipSuccess && a.grad_down && weights) {
@@ -450,6 +454,8 @@ struct Ffn {
             p.a_plane = f.h_plane;
             p.a_rows = p.k;
             p.ffn.a_panel = f.panel;
+            p.ffn.a_step = kStep * 256;
+            p.ffn.b_step = f.arrays == 2 ? 0 : kStep * grad_y.ld;
             p.b = grad_y.p;
             p.b_ld = grad_y.ld;
             p.b_plane = grad_y.plane;
@@ -474,6 +480,8 @@ struct Ffn {
             p.b_plane = f.d_plane;
             p.b_rows = p.k;
             p.d_panel = f.panel;
+            p.ffn.a_step = f.arrays == 2 ? 0 : kStep * x.ld;
+            p.ffn.b_step = kStep * 256;
             p.m = a.hidden;
             p.n = 2 * f.cols_up;
             p.ffn.out[0] = a.grad_gate;
@@ -502,7 +510,8 @@ struct Ffn {
             p.ffn.a2 = w_up.p;
             p.ffn.a2_ld = w_up.ld;
             p.ffn.a2_plane = w_up.plane;
-            p.ffn.d_half = f.h_plane;
+            p.ffn.d_half = f.cols_up / 256 * f.panel;
+            p.ffn.b_array = f.d_plane;
             p.ffn.out[0] = a.grad_x;
             p.ffn.out_ld[0] = a.grad_x_stride;
             e = summed<kInput>(p, s, compute_units, st);

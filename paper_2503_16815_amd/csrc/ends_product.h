@@ -154,6 +154,7 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
     constexpr bool kTurnedA = E == kSums || E == kGateGrad || E == kInput || E == kOuter;   // A's m elements are
     constexpr bool kPanels = E == kSums || E == kGradient || E == kOut || E == kInput;
     constexpr bool kAimed = kPanels || kTurned || kTurnedA;   // a step's place is not the last one's and 64 elements more
+    constexpr bool kTwo = !SPLIT && (E == kOut || E == kInput) && WM == 4 && TN == 64;   // b may have a second array (up to 64 rows)
     constexpr int kPanelSteps = 256 / kStep;
     constexpr int kColumns = E == kGate ? TM / 2 : TM;   // of C that a tile has
     constexpr int kPieces = TN / 8, kPiecesA = TM / 8;   // 16-byte pieces of a row of TN, of TM
@@ -177,7 +178,7 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
 
     const int steps_one = (p.k_dev ? *p.k_dev + kStep - 1 : p.k) / kStep, steps_all = E == kInput ? 2 * steps_one : steps_one;
     const int from = (int)((int64_t)steps_all * split / p.splits), to = (int)((int64_t)steps_all * (split + 1) / p.splits);
-    const int steps = to - from, total = SPLIT ? steps * 6 : E == kGradient ? steps * p.d_arrays : steps;
+    const int steps = to - from, total = SPLIT ? steps * 6 : E == kGradient ? steps * p.d_arrays : kTwo ? steps * p.ffn.arrays : steps;
 
     // where this thread's 16-byte pieces come from (rows past the operand's last one read that one)
     const bool second = E == kGate && ((wave >> 1) & 1);   // this wavefront loads rows of the other projection
@@ -243,7 +244,7 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
     const int64_t a_to_a2 = E == kInput ? (int64_t)((uintptr_t)p.ffn.a2 - (uintptr_t)p.a) : 0;
     const auto aim = [&]() {
         int64_t a_at = 0, b_at = 0;
-        if (E == kOuter) b_at = (int64_t)(from + at_step) * kStep * p.b_ld * 2;
+        if (E == kOuter) b_at = (from + at_step) * p.ffn.b_step * 2;
         else if (kTurned) b_at = (int64_t)(from + at_step) * kStep * 512;
         else if (kPanels) b_at = ((from + at_step) / kPanelSteps * p.d_panel + (from + at_step) % kPanelSteps * kStep) * 2;
         if constexpr (E == kInput) {   // (steps of the second product: its own weights, and the other half of b)
@@ -257,9 +258,12 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
             }
             if ((at_step == 0 || step_of == 0 || k + kStep > p.a_rows) && at_product == 0) turned_a(min(p.a_rows - k, kStep));
         } else if (kTurnedA) {
-            const int k = (from + at_step) * kStep;
-            a_at = (int64_t)k * p.a_ld * 2;
-            if (E == kOuter && ((at_step == 0 && at_product == 0) || k + kStep > p.b_rows)) turned_b(min(p.b_rows - k, kStep));
+            const int k = E == kOuter && p.ffn.a_step == 0 ? 0 : (from + at_step) * kStep;
+            a_at = E == kOuter ? (from + at_step) * p.ffn.a_step * 2 : (int64_t)k * p.a_ld * 2;
+            if (E == kOuter) {
+                const int k_b = p.ffn.b_step == 0 ? 0 : (from + at_step) * kStep;
+                if ((at_step == 0 && at_product == 0) || k_b + kStep > p.b_rows) turned_b(min(p.b_rows - k_b, kStep));
+            }
             if ((at_step == 0 && at_product == 0) || k + kStep > p.a_rows) turned_a(min(p.a_rows - k, kStep));
         }
         if (SPLIT) {
@@ -268,6 +272,8 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
             b_at += ((0x201100 >> (4 * (5 - at_product))) & 15) * p.b_plane * 2;
         } else if (E == kGradient) {
             b_at += at_product * p.d_plane * 2;
+        } else if (kTwo) {
+            b_at += at_product * p.ffn.b_array * 2;
         }
         a_from = descriptor(a_base + a_at);
         b_from = descriptor(b_base + b_at);
@@ -281,6 +287,8 @@ __global__ void __launch_bounds__(WM *WN *kWave, 2) product_kernel(ProductArgs p
             aim();
             return;
         }
+        if (kTwo && ++at_product < p.ffn.arrays) return aim();   // (a step's second array)
+        if (kTwo) at_product = 0;
         ++at_step;
         if (E == kGradient && at_step == steps) {
             at_step = 0;

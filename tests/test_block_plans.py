@@ -20,21 +20,22 @@ PROGRAM = r"""
 #include <cstdio>
 #include <cstdlib>
 using namespace deft;
-template <typename F, int E> void tell(int64_t m, int64_t n, int64_t k, bool split, int units)
+template <typename F, int E> void tell(int64_t m, int64_t n, int64_t k, int arrays, bool split, int units)
 {
     constexpr unsigned kWithout = E == kGate || E == kGateGrad ? kNoAct : kNoOther;
-    const int64_t steps = up(k, kStep) / kStep * (split ? 6 : 1) * (E == kInput ? 2 : 1);
+    const int64_t steps = up(k, kStep) / kStep * (split ? 6 : 1) * (E == kInput ? 2 : 1) * arrays;
     const int parts = F::parts_of(m, n, steps, units, kWithout);
     printf("%d %d ", shape_of(m, n, steps, parts, units, kWithout, F::kAlone), parts);
 }
 template <typename F> void all(int64_t n, int64_t hidden, int64_t inner, bool split, int units)
 {
-    tell<F, kGate>(up(inner, 16) * 2, n, hidden, split, units);
-    tell<F, kOut>(hidden, n, inner, split, units);
-    tell<F, kGateGrad>(inner, n, hidden, split, units);
-    tell<F, kOuter>(inner, hidden, n, split, units);
-    tell<F, kOuter>(hidden, 2 * up(inner, 256), n, split, units);
-    tell<F, kInput>(hidden, n, inner, split, units);
+    const int arrays = F::panels(FfnScratch(FfnPlan{}, nullptr), (int)n, (int)inner, 0).arrays;
+    tell<F, kGate>(up(inner, 16) * 2, n, hidden, 1, split, units);
+    tell<F, kOut>(hidden, n, inner, arrays, split, units);
+    tell<F, kGateGrad>(inner, n, hidden, 1, split, units);
+    tell<F, kOuter>(inner, hidden, n, arrays, split, units);
+    tell<F, kOuter>(hidden, 2 * up(inner, 256), n, arrays, split, units);
+    tell<F, kInput>(hidden, n, inner, arrays, split, units);
     printf("\n");
 }
 int main(int argc, char **argv)   // whether in 32 bits, units; rows, hidden, inner ...
