@@ -32,29 +32,32 @@ constexpr int kGroup = DEFT_CHECKPOINT_GROUP;
 constexpr int kFactorParts = 256;
 
 // How workgroups of 256 threads go through rows' pieces of eight elements, a piece each: as many whole rows as a workgroup has
-// threads for, or a part of one.
+// threads for, or a part of one.  (Worked out on the host: divisions by a thread would be half of a checkpoint's instructions.)
 struct RowPieces {
-    int pieces, first, from, count;    // of a row; its first row, and piece of that; pieces in all
+    int rows, pieces, rows_each, parts;    // pieces and parts of a row
     float one_by;
-    static __host__ __device__ int pieces_of(int cols) { return (cols + 7) / 8; }
-    static __host__ __device__ int rows_each(int cols) { return pieces_of(cols) < 256 ? 256 / pieces_of(cols) : 1; }
-    static __host__ __device__ int parts(int cols) { return (pieces_of(cols) + 255) / 256; }   // of a row
-    static __host__ __device__ unsigned blocks(int64_t rows, int cols)
+    RowPieces() = default;
+    RowPieces(int64_t n, int64_t cols)
+        : rows((int)n), pieces((int)((cols + 7) / 8)), rows_each(pieces < 256 ? 256 / pieces : 1), parts((pieces + 255) / 256), one_by(1.0f / (float)pieces)
     {
-        return (unsigned)((rows + rows_each(cols) - 1) / rows_each(cols) * parts(cols));
     }
-    __device__ RowPieces(unsigned block, int rows, int cols) : pieces(pieces_of(cols))
+    __host__ __device__ unsigned blocks() const { return (unsigned)(((int64_t)rows + rows_each - 1) / rows_each) * (unsigned)parts; }
+
+    // The row and piece of this thread, or false.
+    __device__ bool own(unsigned block, int *row, int *piece) const
     {
-        const int of = parts(cols);
-        first = (int)(block / of) * rows_each(cols);
-        from = (int)(block % of) * 256;
-        count = of > 1 ? min(pieces - from, 256) : min(rows - first, rows_each(cols)) * pieces;
-        one_by = 1.0f / (float)pieces;
+        const int i = threadIdx.x;
+        if (parts == 1) {   // (a whole number less than 256 and a half, divided: never within the error of a whole number)
+            const int in_block = (int)(((float)i + 0.5f) * one_by);
+            *row = (int)block * rows_each + in_block;
+            *piece = i - in_block * pieces;
+            return in_block < rows_each && *row < rows;
+        }
+        const unsigned of = block / (unsigned)parts;
+        *row = (int)of;
+        *piece = (int)(block - of * (unsigned)parts) * 256 + i;
+        return *piece < pieces;
     }
-    // (a whole number less than 256 and a half, divided: never within the error of a whole number)
-    __device__ int in_block(int i) const { return from > 0 ? 0 : (int)(((float)i + 0.5f) * one_by); }
-    __device__ int row(int i) const { return first + in_block(i); }
-    __device__ int piece(int i) const { return from + i - in_block(i) * pieces; }
 };
 
 constexpr float kCodes8 = 127.0f, kCodes16 = 32767.0f;   // the largest codes
@@ -88,6 +91,7 @@ struct RestoreArgs {
     deft_checkpoint_t from;
     void *out;
     int64_t out_ld, out_plane;
+    RowPieces by;
 };
 hipError_t checkpoint_launch(int dtype, const deft_checkpoint_call_t &a, hipStream_t st);
 hipError_t restore_launch(int dtype, const deft_restore_call_t &a, hipStream_t st);
@@ -99,6 +103,7 @@ struct LargestArgs {
     const f16 *x;
     int64_t x_stride;
     float *largest;    // [kFactorParts]
+    RowPieces by;
 };
 hipError_t ffn_largest_launch(const LargestArgs &a, hipStream_t st);
 

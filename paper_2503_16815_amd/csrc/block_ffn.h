@@ -29,6 +29,7 @@ struct JoinArgs {
     int m, n, splits, add;
     const float *sums;               // [splits][n][sums_ld]
     int64_t sums_ld, sums_split;
+    RowPieces by;
 };
 
 // The sums of all parts, eight columns from `from` on.
@@ -56,16 +57,15 @@ __device__ __forceinline__ void joined(const JoinArgs &a, const float *from, flo
 template <typename O>
 __global__ void __launch_bounds__(256) join_out_kernel(JoinArgs a)
 {
-    const RowPieces by(blockIdx.x, a.n, a.m);
     const float alpha = __is_same(O, f16) && a.ffn.largest ? factor_of(a.ffn.largest, threadIdx.x & 63).y : 1.0f;
-    for (int i = threadIdx.x; i < by.count; i += 256) {
-        const int n = by.row(i), m = by.piece(i) * kEight;
-        O *row = out_row<O>(a.ffn, n);
-        if (!row) continue;
-        float x[kEight];
-        joined(a, a.sums + n * a.sums_ld + m, x);
-        store_out<false>(row, m, a.m, x, alpha, a.add);
-    }
+    int n, piece;
+    if (!a.by.own(blockIdx.x, &n, &piece)) return;
+    O *row = out_row<O>(a.ffn, n);
+    if (!row) return;
+    const int m = piece * kEight;
+    float x[kEight];
+    joined(a, a.sums + n * a.sums_ld + m, x);
+    store_out<false>(row, m, a.m, x, alpha, a.add);
 }
 
 // What the products of the projections and of the derivative by h do with their sums, of sums that were cut into parts: m columns
@@ -97,12 +97,11 @@ __global__ void __launch_bounds__(256) join_act_kernel(JoinArgs a)
             use_gate<kInside, T, O, SPLIT>(f, n, at, own_cols, x, up, h_at, act);
         }
     };
-    const RowPieces by(blockIdx.x, (a.n + kStep - 1) / kStep * kStep, (a.m + kStep - 1) / kStep * kStep);
-    for (int i = threadIdx.x; i < by.count; i += 256) {
-        const int n = by.row(i), at = by.piece(i) * kEight;
-        if (f.arrays == 1 && n < a.n && (at & -kGroup) + kGroup <= a.m) eight(std::true_type{}, n, at);   // (a group's four lanes go the same way)
-        else eight(std::false_type{}, n, at);
-    }
+    int n, piece;
+    if (!a.by.own(blockIdx.x, &n, &piece)) return;
+    const int at = piece * kEight;
+    if (f.arrays == 1 && n < a.n && (at & -kGroup) + kGroup <= a.m) eight(std::true_type{}, n, at);   // (a group's four lanes go the same way)
+    else eight(std::false_type{}, n, at);
 }
 
 // One call's view of the scratch memory.
@@ -269,9 +268,10 @@ struct Ffn {
         return product<E>(p, shape_of(cols, p.n, steps, p.splits, compute_units, kWithout, kAlone), st);
     }
 
-    static JoinArgs join(const ProductArgs &p)
+    static JoinArgs join(const ProductArgs &p, const RowPieces &by)
     {
         JoinArgs j{};
+        j.by = by;
         j.ffn = p.ffn;
         j.m = p.m;
         j.n = p.n;
@@ -289,7 +289,8 @@ struct Ffn {
     {
         const hipError_t e = parts<E>(p, E == kGate ? (int)up(p.m, 16) * 2 : p.m, s, compute_units, st);
         if (e != hipSuccess || p.splits == 1) return e;
-        join_act_kernel<E == kGateGrad, T, S, kSplit><<<RowPieces::blocks(up(p.n, kStep), (int)up(p.m, kStep)), 256, 0, st>>>(join(p));
+        const JoinArgs j = join(p, RowPieces(up(p.n, kStep), up(p.m, kStep)));
+        join_act_kernel<E == kGateGrad, T, S, kSplit><<<j.by.blocks(), 256, 0, st>>>(j);
         return hipGetLastError();
     }
 
@@ -319,7 +320,8 @@ struct Ffn {
     {
         const hipError_t e = parts<E>(p, p.m, s, compute_units, st);
         if (e != hipSuccess || p.splits == 1) return e;
-        join_out_kernel<S><<<RowPieces::blocks(p.n, p.m), 256, 0, st>>>(join(p));
+        const JoinArgs j = join(p, RowPieces(p.n, p.m));
+        join_out_kernel<S><<<j.by.blocks(), 256, 0, st>>>(j);
         return hipGetLastError();
     }
 
@@ -420,7 +422,7 @@ struct Ffn {
             }
             if constexpr (kHalf16) {
                 if (e == hipSuccess && by_projections) {
-                    e = ffn_largest_launch({n, a.hidden, static_cast<const f16 *>(a.grad_y), a.grad_y_stride, s.largest}, st);
+                    e = ffn_largest_launch({n, a.hidden, static_cast<const f16 *>(a.grad_y), a.grad_y_stride, s.largest, RowPieces(n, a.hidden)}, st);
                     f.largest = s.largest;
                 }
             }

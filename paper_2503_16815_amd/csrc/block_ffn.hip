@@ -11,14 +11,13 @@ __global__ void __launch_bounds__(256) largest_kernel(LargestArgs a)
     __shared__ float of_wave[4];
     float top = 0.0f;
     for (unsigned block = blockIdx.x;; block += kFactorParts) {
-        if (block >= RowPieces::blocks(a.rows, a.cols)) break;
-        const RowPieces by(block, a.rows, a.cols);
-        for (int i = threadIdx.x; i < by.count; i += 256) {
-            const int at = by.piece(i) * kEight;
-            const Eight<f16>::type x = load_eight<false>(a.x + by.row(i) * a.x_stride + at, at, a.cols);
+        if (block >= a.by.blocks()) break;
+        int row, piece;
+        if (!a.by.own(block, &row, &piece)) continue;
+        const int at = piece * kEight;
+        const Eight<f16>::type x = load_eight<false>(a.x + row * a.x_stride + at, at, a.cols);
 #pragma unroll
-            for (int r = 0; r < kEight; ++r) top = fmaxf(top, is_finite((float)x[r]) ? fabsf((float)x[r]) : 0.0f);
-        }
+        for (int r = 0; r < kEight; ++r) top = fmaxf(top, is_finite((float)x[r]) ? fabsf((float)x[r]) : 0.0f);
     }
     top = wave_max(top);
     if ((threadIdx.x & 63) == 0) of_wave[threadIdx.x >> 6] = top;
