@@ -1,6 +1,7 @@
 // The feed-forward block of up to 64 tokens, as a program that generates them calls it.
 //
-// Bound by reading the three matrices once.  Nothing is packed: a wavefront takes sixteen rows of a matrix at a time, 16 bytes a
+// Bound by reading the three matrices once (13 tokens of 4096 x 12288 bf16 61 us in both launches, 5.0 TB/s; one of 1600 x 6400 18, of which
+// a third is latency).  Nothing is packed: a wavefront takes sixteen rows of a matrix at a time, 16 bytes a
 // lane from memory to the matrix instructions, and eight or sixteen wavefronts share a workgroup's rows along their length (an
 // inner product's terms may come in any order, as long as both operands' do in the same; a tile of 32-bit operands takes
 // four instructions, one for each element of a lane's 16 bytes).  The wavefronts' sums meet in LDS.
