@@ -29,7 +29,7 @@ __device__ __forceinline__ void act_of(float a, float &y, float &slope)
         // (what x log2 e loses by its rounding, times ln 2; limits beyond which 1 + exp x is 1 or the gate's share of it 0)
         const float within = fminf(fmaxf(x, -104.0f), 88.0f), power = within * kLog2e;
         const float rest = fmaf(within, kLog2e, -power) + within * kLog2eRest, y = __builtin_amdgcn_exp2f(power);
-        return fmaf(y, 0.693147181f * rest, y);
+        return x == x ? fmaf(y, 0.693147181f * rest, y) : x;   // (the limits would make a number of NaN)
     };
     const auto inverse = [](float x) {
         const float y = __builtin_amdgcn_rcpf(x);
@@ -63,9 +63,9 @@ __device__ __forceinline__ void act_of(float a, float &y, float &slope)
         const float rest = p - p * p;   // (0 where the square may be infinite)
         y = a * p;
         slope = p + (rest == 0.0f ? 0.0f : rest * 1.595769122f * a * fmaf(0.134145f, square, 1.0f));
-    } else {   // (NaN stays)
+    } else {   // (NaN stays, in both)
         y = a < 0.0f ? 0.0f : a;
-        slope = a > 0.0f ? 1.0f : 0.0f;
+        slope = a > 0.0f ? 1.0f : a == a ? 0.0f : a;
     }
 }
 

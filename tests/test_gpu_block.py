@@ -321,6 +321,42 @@ def test_a_row_of_nan_or_infinities_stays_a_row(block, n, dtype):
                     assert not torch.isfinite(g).all()
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("n", [5, 70, 600])
+def test_nan_in_a_row_is_seen_in_every_gradient(block, n, act, dtype):
+    hidden, inner = 64, 96
+    x, wg, wu, wd, gy = inputs(n, hidden, inner, dtype)
+    x[n - 1] = math.nan
+    with block.DeftBlock(("ffn", "ffn_grad"), dtype, n, hidden, inner) as b:
+        for save in (None, "full", "packed"):
+            y = b.ffn(x, wg, wu, wd, activation=act, save=save)
+            y, saved = y if save else (y, None)
+            gx, gg, gu, gd = b.ffn_grad(gy, x, wg, wu, wd, saved=saved, activation=act)
+            torch.cuda.synchronize()
+            assert torch.isnan(y[n - 1]).all() and torch.isnan(gx[n - 1]).all() and torch.isfinite(gx[:n - 1]).all()
+            assert torch.isnan(gu).all() and torch.isnan(gd).all() and torch.isnan(gg).all(), (act, save)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("n", [5, 70, 600])
+def test_nan_in_the_gate_alone_is_seen_in_its_gradient(block, n, act, dtype):
+    hidden, inner, bad = 64, 96, 40
+    x, wg, wu, wd, gy = inputs(n, hidden, inner, dtype)
+    wg[bad] = math.nan
+    others = [i for i in range(inner) if i // R.GROUP != bad // R.GROUP]   # (a kept group with a NaN is one of NaN)
+    with block.DeftBlock(("ffn", "ffn_grad"), dtype, n, hidden, inner) as b:
+        for save in (None, "full", "packed"):
+            y = b.ffn(x, wg, wu, wd, activation=act, save=save)
+            y, saved = y if save else (y, None)
+            gx, gg, gu, gd = b.ffn_grad(gy, x, wg, wu, wd, saved=saved, activation=act)
+            torch.cuda.synchronize()
+            assert torch.isnan(y).all() and torch.isnan(gx).all() and torch.isnan(gd[:, bad]).all()
+            assert torch.isnan(gu[bad]).all() and torch.isnan(gg[bad]).all(), save
+            assert torch.isfinite(gu[others]).all() and torch.isfinite(gg[others]).all() and torch.isfinite(gd[:, others]).all()
+
+
 def test_small_gradients_of_16_bit_floats_keep_their_bits(block):
     """Gradients of a mean over many tokens, far below the range of 16-bit floats but for their common factor."""
     for grad in (2.0 ** -20, 2.0 ** -14, 1.0, 2.0 ** 12):
