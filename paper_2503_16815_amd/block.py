@@ -256,7 +256,7 @@ class DeftBlock(Marshalling):
 
     @staticmethod
     def _choice(name, value, choices):
-        if value not in choices:
+        if not isinstance(value, (str, type(None))) or value not in choices:
             raise ValueError(f"{name} is one of {list(choices)}: got {value!r}")
         return choices[value]
 

@@ -105,6 +105,12 @@ def _args(dtype=torch.float32, n=4, hidden=6, inner=10):
     return [torch.zeros(s, dtype=dtype) for s in ((n, hidden), (inner, hidden), (inner, hidden), (hidden, inner))]
 
 
+@pytest.mark.parametrize("kw", [dict(activation=["silu"]), dict(activation={}), dict(activation=None), dict(save=[]), dict(save=True)])
+def test_binding_refuses_choices_of_other_types(block, kw):
+    with pytest.raises(ValueError):
+        Stub(block).ffn(*_args(), **kw)
+
+
 def test_binding_refuses_what_the_kernels_do_not_take(block):
     b = Stub(block)
     x, wg, wu, wd = _args()
