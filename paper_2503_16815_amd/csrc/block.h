@@ -109,9 +109,6 @@ hipError_t ffn_largest_launch(const LargestArgs &a, hipStream_t st);
 
 struct FfnPlan {
     int64_t scratch_bytes = 0;
-    int max_rows = 0, max_hidden = 0, max_inner = 0;
-    int planes = 1;                  // 16-bit arrays that an operand is held in: 1, or 3 for 32-bit types
-    bool grad = false;
     // offsets into the scratch memory
     int64_t largest, x, grad_y, w_gate, w_up, w_down, h, d, gate, up, sums;
 };

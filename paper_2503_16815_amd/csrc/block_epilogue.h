@@ -296,11 +296,11 @@ __device__ __forceinline__ void by_rows(const f32x4 (&acc)[MT][NT], float *lds, 
     }
 }
 
-// The same piece by piece of eight columns, rows of any number of pieces, nothing fetched.
-template <int kEach, int MT, int NT, typename Use>
+// The same piece by piece of eight columns, rows of any number of pieces (a tile of 192 columns has 24), nothing fetched.
+template <int MT, int NT, typename Use>
 __device__ __forceinline__ void by_pieces(const f32x4 (&acc)[MT][NT], float *lds, int lane, Use use)
 {
-    constexpr int kPitch = epilogue_pitch(MT), kLanes = MT * 16 / kEach;   // kEach columns of sums make eight
+    constexpr int kPitch = epilogue_pitch(MT), kLanes = MT * 2;
     const int row16 = lane & 15, part = lane >> 4;
 #pragma clang loop unroll(disable)
     for (int j = 0; j < NT; ++j) {
@@ -509,7 +509,7 @@ __device__ __forceinline__ void store_out(O *row, int at, int cols, const float 
 template <int MT, int NT>
 __device__ __forceinline__ void sums_epilogue(float *sums, int64_t ld, const f32x4 (&acc)[MT][NT], const Tile &t)
 {
-    by_pieces<8>(acc, t.lds, t.lane, [&](int row, int col, const float *from) __attribute__((always_inline)) {
+    by_pieces(acc, t.lds, t.lane, [&](int row, int col, const float *from) __attribute__((always_inline)) {
         const int n = t.n + row, at = t.m + col;
         if (n >= t.n_rows || at >= t.cols) return;
         float x[kEight];
@@ -523,7 +523,7 @@ template <typename O, int MT, int NT>
 __device__ __forceinline__ void out_epilogue(const FfnArgs &f, const f32x4 (&acc)[MT][NT], const Tile &t, int add)
 {
     const float alpha = __is_same(O, f16) && f.largest ? factor_of(f.largest, t.lane).y : 1.0f;
-    by_pieces<8>(acc, t.lds, t.lane, [&](int row, int col, const float *from) __attribute__((always_inline)) {
+    by_pieces(acc, t.lds, t.lane, [&](int row, int col, const float *from) __attribute__((always_inline)) {
         const int n = t.n + row, at = t.m + col;
         if (n >= t.n_rows || at >= t.cols) return;
         float x[kEight];

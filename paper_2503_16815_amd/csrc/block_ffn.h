@@ -356,7 +356,7 @@ struct Ffn {
         return few_tokens<S, 4>(f, compute_units, st);
     }
 
-    static hipError_t forward(const FfnPlan &, const deft_ffn_t &a, const FfnScratch &s, int compute_units, hipStream_t st)
+    static hipError_t forward(const deft_ffn_t &a, const FfnScratch &s, int compute_units, hipStream_t st)
     {
         // Up to 16 tokens; up to 64 where the matrices would have to be packed.  16 of 4096 x 12288 bf16: 78 us for 86 by the products
         // below, 24: 99 for 86; 48 of 1021 x 2731 f16 41 for 44; 64 of 1024 x 4096 f32 62 for 96.
@@ -392,7 +392,7 @@ struct Ffn {
         return summed<kOut>(p, s, compute_units, st);
     }
 
-    static hipError_t backward(const FfnPlan &, const deft_ffn_grad_t &a, const FfnScratch &s, int compute_units, hipStream_t st)
+    static hipError_t backward(const deft_ffn_grad_t &a, const FfnScratch &s, int compute_units, hipStream_t st)
     {
         const int n = a.n_rows;
         const bool of_gate = a.grad_gate || a.grad_up, by_projections = of_gate || a.grad_x;

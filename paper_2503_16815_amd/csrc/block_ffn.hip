@@ -44,18 +44,13 @@ DEFT_FFN_TYPE(f32)
 void ffn_plan(int dtype, int max_rows, int max_hidden, int max_inner, bool grad, int compute_units, FfnPlan *plan)
 {
     const int64_t n = up(max_rows, kTile), hidden = up(max_hidden, kTile), inner = up(max_inner, kTile);
-    plan->max_rows = max_rows;
-    plan->max_hidden = max_hidden;
-    plan->max_inner = max_inner;
-    plan->grad = grad;
-    plan->planes = dtype == DEFT_F32 ? 3 : 1;
     int64_t at = 0;
     const auto take = [&](int64_t bytes) {
         const int64_t here = at;
         at += up(bytes, 256);
         return here;
     };
-    const int64_t element = 2 * plan->planes, own = dtype == DEFT_F32 ? 4 : 2;
+    const int64_t element = dtype == DEFT_F32 ? 6 : 2, own = dtype == DEFT_F32 ? 4 : 2;   // of an operand (three 16-bit arrays), of the type
     plan->largest = take(kFactorParts * 4);
     // (whether a call's rows can be read in place is known when it is made)
     plan->x = take(n * up(max_hidden, kStep) * element);
