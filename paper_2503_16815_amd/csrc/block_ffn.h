@@ -358,11 +358,17 @@ struct Ffn {
 
     static hipError_t forward(const deft_ffn_t &a, const FfnScratch &s, int compute_units, hipStream_t st)
     {
-        // Up to 16 tokens; up to 64 where the matrices would have to be packed.  16 of 4096 x 12288 bf16: 78 us for 86 by the products
-        // below, 24: 99 for 86; 48 of 1021 x 2731 f16 41 for 44; 64 of 1024 x 4096 f32 62 for 96.
+        // A few tokens go to kernels that read the matrices once as they lie.  32-bit types: up to 64 (64 of 1024 x 4096 62 us for 74 by
+        // the products below, 32 of 4096 x 12288 189 for 532).  16-bit types: up to 16 (of 4096 x 12288 67 us for 80, of 1600 x 6400 24 for
+        // 29), and where operands would have to be packed, as many as that is worth, by the matrices' size (64 of 515 x 1030 18 for 24; 32
+        // of 1021 x 2731 24 for 29, 64 of it 35 for 32; 32 of 2047 x 8191 97 for 79).  Beyond 8 these kernels round what is between the
+        // products once more, which the products below do not: so where nothing is packed no more than 16 take them, though up to 32 of
+        // 1024 x 4096 (20 us for 24) and 64 of 768 x 2048 (20 for 21) would be faster.
         const bool whole = Packing::as_is(a.x, a.x_stride, a.hidden, true) && Packing::as_is(a.w_gate, a.w_gate_stride, a.hidden, true) &&
                            Packing::as_is(a.w_up, a.w_up_stride, a.hidden, true) && Packing::as_is(a.w_down, a.w_down_stride, a.inner, true);
-        if (a.n_rows <= (whole ? 16 : kFew)) return few(a, s, compute_units, st);
+        const int64_t size = (int64_t)a.hidden * a.inner;
+        const int most = kSplit ? kFew : whole ? 16 : size <= 2 << 20 ? kFew : size <= 6 << 20 ? 32 : 16;
+        if (a.n_rows <= most) return few(a, s, compute_units, st);
         Packing pack;
         const Operand x = pack.operand(a.x, a.x_stride, a.n_rows, a.hidden, true, s.x);
         const Operand w_gate = pack.operand(a.w_gate, a.w_gate_stride, a.inner, a.hidden, true, s.w_gate);

@@ -149,6 +149,23 @@ def test_norms_of_the_roundings(block, n, save, dtype):
         assert off <= limit, (i, off, limit)
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("n", [16, 17, 32, 33, 64, 65])
+@pytest.mark.parametrize("hidden,inner,most", [(1021, 2053, 64), (1023, 2055, 32), (2051, 3061, 32), (2051, 3079, 16)])
+def test_few_rows_of_odd_matrices(block, hidden, inner, most, n, dtype):
+    """Either side of the sizes up to which rows that cannot be read in place go to the kernels for few: the bounds, and once or twice
+    rounded (as above: a tenth for finite samples)."""
+    x, wg, wu, wd, _ = inputs(n, hidden, inner, dtype, seed=n)
+    with block.DeftBlock(("ffn",), dtype, n, hidden, inner) as b:
+        y = b.ffn(x, wg, wu, wd)
+        torch.cuda.synchronize()
+    want = R.forward(x, wg, wu, wd, "silu", dtype)[0]
+    want.holds(y, "y")
+    if dtype != torch.float32:
+        off = float((y.double() - want.value).norm() / want.value.norm())
+        assert off <= 1.1 * R.UNIT[dtype] * math.sqrt((2 if n <= most or n > 64 else 1) / 3)
+
+
 # ---- checkpoints ---------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
