@@ -15,7 +15,8 @@
  * a memset node and read no device data on the host, so they may be recorded into a HIP graph
  * (ffn_grad without events).  Rows are `stride` ELEMENTS apart (at least as many as a row has);
  * pointers need no more than their element's own alignment, though rows whose starts are multiples
- * of 16 bytes are quicker.  Arrays may pass 2^31 elements.  Outputs must not overlap inputs.
+ * of 16 bytes are quicker.  Arrays may pass 2^31 elements.  Outputs overlap neither inputs
+ * nor each other.
  *
  * Sums are held in 32 bits, each in one fixed order (results do not change from call to call), and
  * outputs are rounded once to the handle's type.  In 16-bit types of more than 64 rows what one
