@@ -22,9 +22,10 @@
  * outputs are rounded once to the handle's type.  In 16-bit types of more than 64 rows what one
  * product leaves to the next (the hidden activations, and the derivatives by the two projections) is
  * rounded to the type in between, as the matrix instructions take it, so that an output's error is
- * about sqrt 2 of its own rounding's; in 32 bits, and of fewer rows, it is not, but in y of 9 to 16 rows
- * and, where a matrix's or x's rows do not all start at multiples of 16 bytes, of up to 64 (hidden x inner
- * up to 2^21) or 32 (up to 6 x 2^20).
+ * about sqrt 2 of its own rounding's.  In 32 bits, and of fewer rows, it is not, but in y of 9 to 16 rows
+ * and, unless hidden and inner are multiples of 64 and all rows of x and the matrices start at multiples
+ * of 16 bytes and at most 2^22 elements apart, of up to 64 rows (hidden x inner up to 2^21) or 32 (up to
+ * 6 x 2^20).
  * Hidden activations beyond the range of 16-bit floats are infinite there.
  *
  * Rows that stand for nothing (the padding of a batch) are rows of zeros, as deft_embed gives them

@@ -7,8 +7,8 @@
 // four instructions, one for each element of a lane's 16 bytes).  The wavefronts' sums meet in LDS.
 //
 // Of up to 8 tokens the hidden activations go from the first launch to the second as two numbers of the type, the rounded one and
-// what the rounding took, which are the two halves of a tile's sixteen rows: so y is rounded once.  (Of more they would be a second
-// tile: 16 tokens of 1600 x 6400 bf16 30 us.)
+// what the rounding took, which are the two halves of a tile's sixteen rows: so y is rounded once.  Of more they are a second
+// tile: of 9 to 16 that costs more than it is worth (16 tokens of 1600 x 6400 bf16 30 us for 24), of 17 to 32 it is done where asked.
 #pragma once
 #include "block_epilogue.h"
 #include "ends_shapes.h"
@@ -226,25 +226,28 @@ __global__ void __launch_bounds__(kGateWaves *kWave, 4) few_gate_kernel(FewArgs 
     }
 }
 
-// Workgroup b: columns MT * 16 b .. of y.  FOLD: up to 8 tokens, whose two arrays are one tile's sixteen rows.
-template <typename S, int MT, int NT, bool FOLD>
+// Workgroup b: columns MT * 16 b .. of y.  FOLD: up to 8 tokens, whose two arrays are one tile's sixteen rows.  TWO: the second array
+// is as many tiles again, whose sums are added before the wavefronts' meet.
+template <typename S, int MT, int NT, bool FOLD, bool TWO = false>
 __global__ void __launch_bounds__(kOutWaves *kWave) few_out_kernel(FewArgs a)
 {
     __shared__ __align__(16) float lds[kOutWaves * 16 * (MT * 16 + 4)];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, row16 = lane & 15, first = blockIdx.x * MT * 16;
-    const S *w[MT], *h[NT];
+    constexpr int kTiles = TWO ? 2 * NT : NT;
+    const S *w[MT], *h[kTiles];
 #pragma unroll
     for (int i = 0; i < MT; ++i) w[i] = static_cast<const S *>(a.w_down) + min(first + i * 16 + row16, a.hidden - 1) * a.w_down_stride;
 #pragma unroll
-    for (int j = 0; j < NT; ++j)
-        h[j] = static_cast<const S *>(a.h) + (FOLD ? (row16 >> 3) * a.h_array : 0) + min(FOLD ? row16 & 7 : j * 16 + row16, a.n - 1) * a.h_stride;
-    f32x4 acc[MT][NT] = {};
-    few_sums<S, kOutWaves, MT, NT>(w, h, a.inner, wave, lane, acc);
+    for (int j = 0; j < kTiles; ++j)
+        h[j] = static_cast<const S *>(a.h) + (FOLD ? (row16 >> 3) * a.h_array : j / NT * a.h_array) +
+               min(FOLD ? row16 & 7 : j % NT * 16 + row16, a.n - 1) * a.h_stride;
+    f32x4 acc[MT][kTiles] = {};
+    few_sums<S, kOutWaves, MT, kTiles>(w, h, a.inner, wave, lane, acc);
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
         f32x4 own[MT];
 #pragma unroll
-        for (int i = 0; i < MT; ++i) own[i] = acc[i][j];
+        for (int i = 0; i < MT; ++i) own[i] = TWO ? acc[i][j] + acc[i][kTiles - NT + j] : acc[i][j];
         few_meet<MT>(own, lds, wave, lane);
         for (int at = tid; at < (FOLD ? 8 : 16) * MT * 16; at += kOutWaves * kWave) {
             const int token = at / (MT * 16), row = at % (MT * 16), n = j * 16 + token;
@@ -265,6 +268,11 @@ hipError_t few_tokens(const FewArgs &a, int compute_units, hipStream_t st)
     if constexpr (NT == 1 && sizeof(S) == 2)
         if (a.h_arrays == 2) {
             few_out_kernel<S, 1, 1, true><<<ones, kOutWaves * kWave, 0, st>>>(a);
+            return hipGetLastError();
+        }
+    if constexpr (NT == 2 && sizeof(S) == 2)
+        if (a.h_arrays == 2) {
+            few_out_kernel<S, 1, NT, false, true><<<ones, kOutWaves * kWave, 0, st>>>(a);
             return hipGetLastError();
         }
     // (rows two tiles at a time read the activations half as often)

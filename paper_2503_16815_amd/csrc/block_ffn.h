@@ -329,7 +329,7 @@ struct Ffn {
         return hipGetLastError();
     }
 
-    static hipError_t few(const deft_ffn_t &a, const FfnScratch &s, int compute_units, hipStream_t st)
+    static hipError_t few(const deft_ffn_t &a, const FfnScratch &s, int h_arrays, int compute_units, hipStream_t st)
     {
         FewArgs f{};
         f.n = a.n_rows;
@@ -347,7 +347,7 @@ struct Ffn {
         f.h = s.h;
         f.h_stride = up(a.inner, 8);
         f.h_array = kFew * f.h_stride;   // (within the room for a tile's rows)
-        f.h_arrays = !kSplit && f.n <= 8 ? 2 : 1;
+        f.h_arrays = h_arrays;
         f.saved = a.save;
         f.y = a.y;
         f.y_stride = a.y_stride;
@@ -362,13 +362,15 @@ struct Ffn {
         // the products below, 32 of 4096 x 12288 189 for 532).  16-bit types: up to 16 (of 4096 x 12288 67 us for 80, of 1600 x 6400 24 for
         // 29), and where operands would have to be packed, as many as that is worth, by the matrices' size (64 of 515 x 1030 18 for 24; 32
         // of 1021 x 2731 24 for 29, 64 of it 35 for 32; 32 of 2047 x 8191 97 for 79).  Beyond 8 these kernels round what is between the
-        // products once more, which the products below do not: so where nothing is packed no more than 16 take them, though up to 32 of
-        // 1024 x 4096 (20 us for 24) and 64 of 768 x 2048 (20 for 21) would be faster.
+        // products once more, which the products below do not: so where nothing is packed 17 to 32 take them with what that takes beside it,
+        // as a second array, which pays for small matrices only (32 of 768 x 2048 17 us for 20.6, without the array 13.5; 24 of 1024 x
+        // 4096 24.0 for 23.4), and more do not, though 48 of 768 x 2048 would be quicker without (18 for 21).
         const bool whole = Packing::as_is(a.x, a.x_stride, a.hidden, true) && Packing::as_is(a.w_gate, a.w_gate_stride, a.hidden, true) &&
                            Packing::as_is(a.w_up, a.w_up_stride, a.hidden, true) && Packing::as_is(a.w_down, a.w_down_stride, a.inner, true);
         const int64_t size = (int64_t)a.hidden * a.inner;
-        const int most = kSplit ? kFew : whole ? 16 : size <= 2 << 20 ? kFew : size <= 6 << 20 ? 32 : 16;
-        if (a.n_rows <= most) return few(a, s, compute_units, st);
+        const int most = kSplit ? kFew : size <= 2 << 20 ? (whole ? 32 : kFew) : size <= 6 << 20 && !whole ? 32 : 16;
+        const bool two = !kSplit && (a.n_rows <= 8 || (a.n_rows > 16 && whole));
+        if (a.n_rows <= most) return few(a, s, two ? 2 : 1, compute_units, st);
         Packing pack;
         const Operand x = pack.operand(a.x, a.x_stride, a.n_rows, a.hidden, true, s.x);
         const Operand w_gate = pack.operand(a.w_gate, a.w_gate_stride, a.inner, a.hidden, true, s.w_gate);

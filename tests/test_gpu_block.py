@@ -150,6 +150,29 @@ def test_norms_of_the_roundings(block, n, save, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("act,save", [("silu", None), ("gelu", "packed"), ("gelu_tanh", "full"), ("relu", None)])
+@pytest.mark.parametrize("n", [17, 25, 31, 32, 33])
+@pytest.mark.parametrize("hidden,inner", [(64, 64), (768, 2048), (1024, 2048), (1088, 2048)])
+def test_17_to_32_rows_read_in_place(block, hidden, inner, n, act, save, dtype):
+    """Either side of the sizes and lengths at which these go to the kernels for few: the bounds, y rounded once (as above: a tenth
+    for finite samples), and the rows behind the last as they were."""
+    x, wg, wu, wd, _ = inputs(n, hidden, inner, dtype, seed=n)
+    wide = torch.full((n + 3, hidden), 7.0, dtype=dtype, device="cuda")
+    with block.DeftBlock(("ffn",), dtype, n, hidden, inner) as b:
+        y = b.ffn(x, wg, wu, wd, activation=act, save=save, out=wide[:n])
+        y, saved = y if save else (y, None)
+        torch.cuda.synchronize()
+    want, gate, up = R.forward(x, wg, wu, wd, act, dtype)
+    want.holds(y, "y")
+    if save:
+        check_saved(block, saved, gate, up, dtype)
+    assert (wide[n:] == 7.0).all()
+    if dtype != torch.float32 and hidden > 64:
+        off = float((y.double() - want.value).norm() / want.value.norm())
+        assert off <= 1.1 * R.UNIT[dtype] * math.sqrt(1 / 3)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
 @pytest.mark.parametrize("n", [16, 17, 32, 33, 64, 65])
 @pytest.mark.parametrize("hidden,inner,most", [(1021, 2053, 64), (1023, 2055, 32), (2051, 3061, 32), (2051, 3079, 16)])
 def test_few_rows_of_odd_matrices(block, hidden, inner, most, n, dtype):
