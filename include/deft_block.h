@@ -128,7 +128,8 @@ enum { DEFT_SAVE_NONE = 0, DEFT_SAVE_FULL = 1, DEFT_SAVE_PACKED = 2 };
  * scales; in 16-bit types they are checkpoints whose codes are int16 (-32767 .. 32767), in 16.5 bits an
  * element off by at most (1 + 2^-7) / 65534 of the group's largest: as good as the sums in 32 bits for what
  * is rounded to the type afterwards.  A sum within its own error of the middle between two codes may get
- * either.  A group with a sum that is not finite has NaN as its scale, and comes back as NaN. */
+ * either; with relu, whose derivative changes there, a positive sum of the gate gets 1 at least (and may be
+ * off by the step).  A group with a sum that is not finite has NaN as its scale, and comes back as NaN. */
 typedef struct {
     int32_t kind;          /* DEFT_SAVE_*                                                      */
     deft_checkpoint_t gate, up;

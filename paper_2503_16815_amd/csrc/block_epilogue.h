@@ -125,8 +125,10 @@ __device__ __forceinline__ unsigned pack_bytes(unsigned a, unsigned b, unsigned 
 
 // Sums as codes C of a checkpoint, whose group this and three neighbouring lanes hold.  A group with a sum that is not finite
 // gets NaN as its scale.  Codes are the low bits of x / s + 3 2^22, rounded once (a sum in 32 bits is itself unsure of a half).
-template <bool kInside, typename C>
-__device__ __forceinline__ void store_codes(deft_checkpoint_t to, int n, int at, int cols, const float (&x)[kEight])
+// kStaySigned: of 16 bits, positive sums get codes of at least `least`, 0 or 1 (relu's derivative is 1 down to 0: with a code of 0 for what
+// is below half a step 2e-5 of a gate's elements lose theirs, 5e-3 of the derivative's norm, 25 times what 16-bit floats round).
+template <bool kInside, typename C, bool kStaySigned>
+__device__ __forceinline__ void store_codes(deft_checkpoint_t to, int n, int at, int cols, const float (&x)[kEight], float least = 0.0f)
 {
     constexpr bool k8 = sizeof(C) == 1;
     constexpr float kLargest = k8 ? kCodes8 : kCodes16;
@@ -138,7 +140,10 @@ __device__ __forceinline__ void store_codes(deft_checkpoint_t to, int n, int at,
     const float inverse = __builtin_amdgcn_rcpf(s);
     unsigned c[kEight];
 #pragma unroll
-    for (int r = 0; r < kEight; ++r) c[r] = __float_as_uint(fmaf(x[r], inverse, kShift));
+    for (int r = 0; r < kEight; ++r) {
+        const float code = fmaf(x[r], inverse, kShift);
+        c[r] = __float_as_uint(kStaySigned && !k8 && x[r] > 0.0f ? fmaxf(code, kShift + least) : code);
+    }
     typename Eight<C>::type y;
     if constexpr (k8) {
         uint2 all;
@@ -159,12 +164,12 @@ __device__ __forceinline__ void store_codes(deft_checkpoint_t to, int n, int at,
 }
 
 // A projection as it is kept: in 8 bits, or in as many as O has.
-template <bool kInside, typename O>
-__device__ __forceinline__ void store_saved(int kind, deft_checkpoint_t to, int n, int at, int cols, const float (&x)[kEight])
+template <bool kInside, typename O, bool kStaySigned>
+__device__ __forceinline__ void store_saved(int kind, deft_checkpoint_t to, int n, int at, int cols, const float (&x)[kEight], float least = 0.0f)
 {
-    if (kind == DEFT_SAVE_PACKED) store_codes<kInside, int8_t>(to, n, at, cols, x);
+    if (kind == DEFT_SAVE_PACKED) store_codes<kInside, int8_t, false>(to, n, at, cols, x);
     else if constexpr (sizeof(O) == 4) store_eight<kInside>(static_cast<float *>(to.codes) + n * to.codes_stride + at, at, cols, rounded<float>(x));
-    else store_codes<kInside, int16_t>(to, n, at, cols, x);
+    else store_codes<kInside, int16_t, kStaySigned>(to, n, at, cols, x, least);
 }
 
 // Eight elements of it as they come from memory: codes of 8 bits in the first two words, of 16 in four, or floats.
@@ -374,8 +379,8 @@ __device__ __forceinline__ void use_gate(const FfnArgs &f, int n, int at, int ow
 {
     float y[kEight], slope[kEight];
     if (f.saved.kind != DEFT_SAVE_NONE) {
-        store_saved<kInside, O>(f.saved.kind, f.saved.gate, n, at, own_cols, gate);
-        store_saved<kInside, O>(f.saved.kind, f.saved.up, n, at, own_cols, up);
+        store_saved<kInside, O, true>(f.saved.kind, f.saved.gate, n, at, own_cols, gate, f.activation == DEFT_RELU ? 1.0f : 0.0f);
+        store_saved<kInside, O, false>(f.saved.kind, f.saved.up, n, at, own_cols, up);
     }
     if (!f.h || (!kInside && at >= f.cols_up)) return;
     act(gate, y, slope);

@@ -152,9 +152,9 @@ __device__ __forceinline__ float few_sum(const float *lds, int token, int row)
     return x;
 }
 
-// A sum as its part of a checkpoint's group, which 32 neighbouring lanes hold.
+// A sum as its part of a checkpoint's group, which 32 neighbouring lanes hold.  `least`: of positive sums' codes.
 template <typename C>
-__device__ __forceinline__ void few_code(deft_checkpoint_t to, int n, int at, bool in, float x)
+__device__ __forceinline__ void few_code(deft_checkpoint_t to, int n, int at, bool in, float x, float least)
 {
     constexpr float kLargest = sizeof(C) == 1 ? kCodes8 : kCodes16;
     unsigned top = in ? __float_as_uint(x) & 0x7fffffffu : 0u;
@@ -162,20 +162,20 @@ __device__ __forceinline__ void few_code(deft_checkpoint_t to, int n, int at, bo
     for (int d = 16; d > 0; d >>= 1) top = max(top, (unsigned)__shfl_xor((int)top, d));
     const float s = checkpoint_scale(__uint_as_float(top), kLargest, 1.0f / kLargest);
     if (!in) return;
-    static_cast<C *>(to.codes)[n * to.codes_stride + at] = (C)(int)__builtin_rintf(fminf(fmaxf(x / s, -kLargest), kLargest));
+    static_cast<C *>(to.codes)[n * to.codes_stride + at] = (C)(int)__builtin_rintf(fminf(fmaxf(x / s, x > 0.0f ? least : -kLargest), kLargest));
     if (at % kGroup == 0)
         static_cast<unsigned short *>(to.scales)[n * to.scales_stride + at / kGroup] = top < 0x7f800000u ? __float_as_uint(s) >> 16 : 0x7fc0;
 }
 
 template <typename S>
-__device__ __forceinline__ void few_save(int kind, deft_checkpoint_t to, int n, int at, bool in, float x)
+__device__ __forceinline__ void few_save(int kind, deft_checkpoint_t to, int n, int at, bool in, float x, float least = 0.0f)
 {
     if (kind == DEFT_SAVE_PACKED) {
-        few_code<int8_t>(to, n, at, in, x);
+        few_code<int8_t>(to, n, at, in, x, 0.0f);
     } else if constexpr (sizeof(S) == 4) {
         if (in) static_cast<float *>(to.codes)[n * to.codes_stride + at] = x;
     } else {
-        few_code<int16_t>(to, n, at, in, x);
+        few_code<int16_t>(to, n, at, in, x, least);
     }
 }
 
@@ -209,7 +209,7 @@ __global__ void __launch_bounds__(kGateWaves *kWave, 4) few_gate_kernel(FewArgs 
         const float gate = few_sum<kGateWaves, MT>(lds, token, col), up = few_sum<kGateWaves, MT>(lds, token, kCols + col);
         const bool in = n < a.n && at < a.inner;
         if (TILES == 2 && a.saved.kind != DEFT_SAVE_NONE) {
-            few_save<S>(a.saved.kind, a.saved.gate, n, at, in, gate);
+            few_save<S>(a.saved.kind, a.saved.gate, n, at, in, gate, a.activation == DEFT_RELU ? 1.0f : 0.0f);
             few_save<S>(a.saved.kind, a.saved.up, n, at, in, up);
         }
         if (!in) continue;

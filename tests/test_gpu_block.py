@@ -45,7 +45,7 @@ def inputs(n, hidden, inner, dtype, seed=1, pad=0, shift=0, grad=1.0):
     return [rows(t.to(dtype), pad, shift) for t in (x, wg, wu, wd, gy)]
 
 
-def check_saved(block, saved, gate, up, dtype):
+def check_saved(block, saved, gate, up, dtype, act="silu"):
     """What is kept of the projections is as near to them as its format has it."""
     for c, z in ((saved.gate, gate), (saved.up, up)):
         if c.scales is None:
@@ -54,7 +54,10 @@ def check_saved(block, saved, gate, up, dtype):
         most = 127.0 if c.codes.dtype == torch.int8 else 32767.0
         s = c.scales.double().repeat_interleave(R.GROUP, dim=1)[:, :z.value.shape[1]]
         # half a step, and the step that a group's largest may be taken for; the scale itself within its own rounding
-        R.Range(z.value, z.off + s * (0.5 + 2.0 ** -8)).holds(R.kept(c), "kept")
+        half = torch.full_like(s, 0.5)
+        if act == "relu" and z is gate and most > 127:   # (what is in (0, s / 2) is held as s: off by less than s, where the value may be there)
+            half = torch.where((z.value > -z.off) & (z.value < s / 2 + z.off), 1.0, half)
+        R.Range(z.value, z.off + s * (half + 2.0 ** -8)).holds(R.kept(c), "kept")
         n, w = z.value.shape
         top = torch.nn.functional.pad(z.value.abs() + z.off, (0, -w % R.GROUP)).view(n, -1, R.GROUP).amax(dim=2)
         assert (c.scales.double() <= R.scale_of(top * (1 + 2.0 ** -20), most) * (1 + 2.0 ** -20)).all()
@@ -75,7 +78,7 @@ def step(block, n, hidden, inner, dtype, act="silu", save=None, x_packed=False, 
         if save is None:
             _, gate, up = R.forward(x, wg, wu, wd, act, dtype)
     if save:
-        check_saved(block, saved, *R.forward(inputs(n, hidden, inner, dtype, seed, pad, shift, grad)[0], wg, wu, wd, act, dtype)[1:], dtype)
+        check_saved(block, saved, *R.forward(inputs(n, hidden, inner, dtype, seed, pad, shift, grad)[0], wg, wu, wd, act, dtype)[1:], dtype, act)
         gate, up = R.Range(R.kept(saved.gate)), R.Range(R.kept(saved.up))
     elif dtype != torch.float32:   # (kept in 16 bits within the call)
         gate, up = (R.Range(z.value, z.off + z.value.abs().max() / 32767 + 2.0 ** -100) for z in (gate, up))
@@ -165,7 +168,7 @@ def test_17_to_32_rows_read_in_place(block, hidden, inner, n, act, save, dtype):
     want, gate, up = R.forward(x, wg, wu, wd, act, dtype)
     want.holds(y, "y")
     if save:
-        check_saved(block, saved, gate, up, dtype)
+        check_saved(block, saved, gate, up, dtype, act)
     assert (wide[n:] == 7.0).all()
     if dtype != torch.float32 and hidden > 64:
         off = float((y.double() - want.value).norm() / want.value.norm())
@@ -395,6 +398,35 @@ def test_nan_in_the_gate_alone_is_seen_in_its_gradient(block, n, act, dtype):
             assert torch.isnan(y).all() and torch.isnan(gx).all() and torch.isnan(gd[:, bad]).all()
             assert torch.isnan(gu[bad]).all() and torch.isnan(gg[bad]).all(), save
             assert torch.isfinite(gu[others]).all() and torch.isfinite(gg[others]).all() and torch.isfinite(gd[:, others]).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("n,hidden,inner", [(5, 64, 96), (30, 65, 100), (40, 128, 4096), (700, 128, 4096), (1003, 101, 515)])
+def test_relu_keeps_the_sign_of_small_sums(block, n, hidden, inner, dtype):
+    """Gates down to 2^-40 of their group's largest: what is kept of a positive one is positive, and of others it is not."""
+    _, wg, wu, wd, gy = inputs(n, hidden, inner, dtype)
+    g = gen(9)
+    wg.zero_()
+    wg[:, 0] = (torch.randn(inner, generator=g, device="cuda").sign() * torch.exp2(-torch.randint(0, 13, (inner,), generator=g, device="cuda").float())).to(dtype)
+    x = torch.randn((n, hidden), generator=g, device="cuda").to(dtype)
+    x[:, 0] = 2.0 ** -8
+    wg[0::32, 0] = 256.0   # (a group's largest, 2^21 times its least)
+    with block.DeftBlock(("ffn", "ffn_grad"), dtype, n, hidden, inner) as b:
+        y, saved = b.ffn(x, wg, wu, wd, activation="relu", save="full")
+        kept = b.ffn_grad(gy, x, wg, wu, wd, saved=saved, activation="relu")
+        again = b.ffn_grad(gy, x, wg, wu, wd, activation="relu")
+        torch.cuda.synchronize()
+    gate = x.double() @ wg.double().t()
+    assert torch.equal(R.kept(saved.gate) > 0, gate > 0)
+    off = wu.double()   # (grad_gate of a positive gate is d * up, whatever the gate: each row against the definition's)
+    d = gy.double() @ wd.double()
+    want = ((d * (x.double() @ off.t()) * (gate > 0)).t() @ x.double())
+    for grads in (kept, again):
+        on = (gate > 0).any(dim=0)
+        assert (grads[1][~on] == 0).all()
+        far = (grads[1].double() - want).norm(dim=1) / want.norm(dim=1).clamp(min=1e-300)
+        # roundings of d_gate and of the sum, and of up as kept (2^-16 of its group's largest, about three times its size): a step each
+        assert (far[on] <= 4 * max(R.UNIT[dtype], 2.0 ** -14 if dtype != torch.float32 else 2.0 ** -18)).all(), float(far[on].max())
 
 
 def test_small_gradients_of_16_bit_floats_keep_their_bits(block):
