@@ -80,8 +80,8 @@ deft_status_t deft_block_get_info(const deft_block_t *h, deft_block_info_t *info
  *   codes = the whole number nearest to x / s, ties to the even one (-127 .. 127),
  * and it stands for codes * s: off by at most s / 2, which is at most (1 + 2^-7) max |x| / 254, in
  * 8.5 bits an element.  An element that is not finite has code -128, takes no part in the largest
- * and comes back as NaN.  Scales are the upper halves of 32-bit floats (bfloat16).  What lies beyond
- * the type's largest number comes back as that.
+ * and comes back as NaN, as all of a group does whose scale is NaN (deft_ffn writes such ones).  Scales are the
+ * upper halves of 32-bit floats (bfloat16).  What lies beyond the type's largest number comes back as that.
  */
 #define DEFT_CHECKPOINT_GROUP 32
 

@@ -76,10 +76,11 @@ __device__ __forceinline__ float checkpoint_scale(float top, float most, float o
 
 __device__ __forceinline__ bool is_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
 
-// What a code stands for, up to `most`, the largest number of its type: the nearest multiple of s may lie beyond.
+// What a code stands for, up to `most`, the largest number of its type: the nearest multiple of s may lie beyond.  (A projection's group
+// with a sum that is not finite has NaN as its scale, whatever its codes are: the limits alone would make a number of it.)
 __device__ __forceinline__ float checkpoint_value(int code, float s, float most)
 {
-    return code == -128 ? __builtin_nanf("") : fminf(fmaxf((float)code * s, -most), most);
+    return code == -128 || s != s ? __builtin_nanf("") : fminf(fmaxf((float)code * s, -most), most);
 }
 
 // ---- launches (each returns hipGetLastError() of its launches) ------------------------------
