@@ -26,7 +26,7 @@
  * and, unless hidden and inner are multiples of 64 and all rows of x and the matrices start at multiples
  * of 16 bytes and at most 2^22 elements apart, of up to 64 rows (hidden x inner up to 2^21) or 32 (up to
  * 6 x 2^20).
- * Hidden activations beyond the range of 16-bit floats are infinite there.
+ * Hidden activations beyond the type's range are infinite there, of few rows too.
  *
  * Rows that stand for nothing (the padding of a batch) are rows of zeros, as deft_embed gives them
  * for a token of -1: they add nothing to any gradient.
@@ -139,7 +139,8 @@ typedef struct {
  * deft_ffn, with the matrices stored as [outputs][inputs]:
  *   gate = x w_gate^T,  up = x w_up^T,  y = (act(gate) * up) w_down^T,
  * and gate and up kept as `save` says, from their sums in 32 bits.
- * A row of y depends on its own row of x alone.
+ * A row of y depends on its own row of x alone.  Where that or a matrix holds infinities or NaN, so does what is made of them (NaN
+ * possibly in the place of an infinity).
  */
 typedef struct {
     int32_t n_rows;

@@ -218,6 +218,11 @@ __device__ __forceinline__ void use_saved(int kind, const Kept<O> &k, float (&x)
     }
 }
 
+// What rounding x to y took; of one that the rounding made infinite nothing (x less infinity would be the opposite one, and both
+// arrays' products NaN together).
+template <typename T>
+__device__ __forceinline__ float taken(float x, T y) { return is_finite((float)y) ? x - (float)y : 0.0f; }
+
 // Eight elements of an operand in panels: one array of T, two where the second has what rounding took of the first, or three of bf16
 // whose sum they are.
 template <typename T, bool SPLIT>
@@ -242,7 +247,7 @@ __device__ __forceinline__ void store_operand(T *to, int64_t plane, int arrays, 
         *reinterpret_cast<T8 *>(to) = y;
         if (arrays == 2) {
 #pragma unroll
-            for (int r = 0; r < kEight; ++r) y[r] = (T)(x[r] - (float)y[r]);
+            for (int r = 0; r < kEight; ++r) y[r] = (T)taken(x[r], y[r]);
             *reinterpret_cast<T8 *>(to + plane) = y;
         }
     }

@@ -220,9 +220,9 @@ __global__ void __launch_bounds__(kGateWaves *kWave, 4) few_gate_kernel(FewArgs 
         else if (a.activation == DEFT_GELU_TANH) act_of<DEFT_GELU_TANH, kExact>(gate, y, slope);
         else act_of<DEFT_RELU, kExact>(gate, y, slope);
         S *h = static_cast<S *>(a.h) + n * a.h_stride + at;
-        float rest = y * up;
-        *h = (S)rest;
-        if (a.h_arrays == 2) h[a.h_array] = (S)(rest - (float)(S)rest);
+        const float of_both = y * up;
+        *h = (S)of_both;
+        if (a.h_arrays == 2) h[a.h_array] = (S)taken(of_both, (S)of_both);
     }
 }
 
