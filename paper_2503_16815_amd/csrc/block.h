@@ -42,6 +42,8 @@ struct RowPieces {
     {
     }
     __host__ __device__ unsigned blocks() const { return (unsigned)(((int64_t)rows + rows_each - 1) / rows_each) * (unsigned)parts; }
+    // Rows that a launch can have, whose threads have to be fewer than 2^32.
+    int64_t most_rows() const { return (int64_t)(((1 << 24) - 1) / parts) * rows_each; }
 
     // The row and piece of this thread, or false.
     __device__ bool own(unsigned block, int *row, int *piece) const
@@ -59,6 +61,17 @@ struct RowPieces {
         return *piece < pieces;
     }
 };
+
+// As many launches as n rows of `cols` take (one, but of about a million rows of more than 30720 columns): launch(its first row,
+// RowPieces of its rows).
+template <typename F>
+hipError_t by_launches(int64_t n, int64_t cols, F launch)
+{
+    const int64_t most = RowPieces(n, cols).most_rows();
+    hipError_t e = hipSuccess;
+    for (int64_t first = 0; first < n && e == hipSuccess; first += most) e = launch(first, RowPieces(n - first < most ? n - first : most, cols));
+    return e;
+}
 
 constexpr float kCodes8 = 127.0f, kCodes16 = 32767.0f;   // the largest codes
 constexpr float kShift = 12582912.0f;   // 3 2^22: a sum with it is a whole number, in the low bits

@@ -72,6 +72,13 @@ __global__ void __launch_bounds__(256) store_kernel(StoreArgs a)
     if ((at & (kGroup - 1)) == 0) static_cast<unsigned short *>(a.out.scales)[row * a.out.scales_stride + at / kGroup] = __float_as_uint(s) >> 16;
 }
 
+// A checkpoint's rows from `first` on.
+deft_checkpoint_t rows_from(const deft_checkpoint_t &c, int64_t first)
+{
+    return {static_cast<int8_t *>(c.codes) + first * c.codes_stride, c.codes_stride,
+            static_cast<unsigned short *>(c.scales) + first * c.scales_stride, c.scales_stride};
+}
+
 template <typename S> constexpr float kMost = 3.402823466e38f;
 template <> constexpr float kMost<f16> = 65504.0f;
 template <> constexpr float kMost<bf16> = 3.38953139e38f;
@@ -107,24 +114,38 @@ __global__ void __launch_bounds__(256) restore_kernel(RestoreArgs a)
     for (int k = 0; k < P; ++k) store_eight<false>(static_cast<T *>(a.out) + k * a.out_plane + row * a.out_ld + at, at, a.cols_to, y[k]);
 }
 
-template <typename S, typename T, int P>
-hipError_t restore(RestoreArgs a, hipStream_t st)
+template <typename S>
+hipError_t store(const deft_checkpoint_call_t &c, hipStream_t st)
 {
-    a.by = RowPieces(a.rows_to, a.cols_to);
-    restore_kernel<S, T, P><<<a.by.blocks(), 256, 0, st>>>(a);
-    return hipGetLastError();
+    return by_launches(c.n_rows, ((int64_t)c.width + kGroup - 1) / kGroup * kGroup, [&](int64_t first, const RowPieces &by) {
+        const StoreArgs a = {by.rows, c.width, static_cast<const S *>(c.x) + first * c.x_stride, c.x_stride, rows_from(c.out, first), by};
+        store_kernel<S><<<by.blocks(), 256, 0, st>>>(a);
+        return hipGetLastError();
+    });
+}
+
+template <typename S, typename T, int P>
+hipError_t restore(const RestoreArgs &c, hipStream_t st)
+{
+    return by_launches(c.rows_to, c.cols_to, [&](int64_t first, const RowPieces &by) {
+        RestoreArgs a = c;
+        a.rows = (int)(c.rows - first);   // (fewer than none where all of them are zeros)
+        a.rows_to = by.rows;
+        a.from = rows_from(c.from, first);
+        a.out = static_cast<T *>(c.out) + first * c.out_ld;
+        a.by = by;
+        restore_kernel<S, T, P><<<by.blocks(), 256, 0, st>>>(a);
+        return hipGetLastError();
+    });
 }
 
 }  // namespace
 
 hipError_t checkpoint_launch(int dtype, const deft_checkpoint_call_t &c, hipStream_t st)
 {
-    const StoreArgs a = {c.n_rows, c.width, c.x, c.x_stride, c.out, RowPieces(c.n_rows, ((int64_t)c.width + kGroup - 1) / kGroup * kGroup)};
-    const unsigned blocks = a.by.blocks();
-    if (dtype == DEFT_F32) store_kernel<float><<<blocks, 256, 0, st>>>(a);
-    else if (dtype == DEFT_F16) store_kernel<f16><<<blocks, 256, 0, st>>>(a);
-    else store_kernel<bf16><<<blocks, 256, 0, st>>>(a);
-    return hipGetLastError();
+    if (dtype == DEFT_F32) return store<float>(c, st);
+    if (dtype == DEFT_F16) return store<f16>(c, st);
+    return store<bf16>(c, st);
 }
 
 hipError_t restore_launch(int dtype, const deft_restore_call_t &c, hipStream_t st)
