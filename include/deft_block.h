@@ -44,7 +44,8 @@ extern "C" {
 
 typedef struct deft_block deft_block_t; /* opaque */
 
-/* operators that a handle serves; they size its scratch memory (checkpoint and restore need none) */
+/* operators that a handle serves; they size its scratch memory (checkpoint and restore need none; ffn alone of up to 16
+ * rows, or 32 of max_hidden x max_inner up to 2^21, or 64 in 32 bits, none for operands and parts of sums) */
 #define DEFT_BLOCK_FFN 1u
 #define DEFT_BLOCK_FFN_GRAD 2u
 #define DEFT_BLOCK_CHECKPOINT 4u

@@ -2,7 +2,7 @@
 // device code, and the launch interface between the C ABI (block_api.hip) and the kernels.
 #pragma once
 #include "../../include/deft_block.h"
-#include "ends.h"
+#include "ends_shapes.h"
 
 namespace deft {
 
@@ -127,6 +127,12 @@ struct FfnPlan {
     int64_t largest, x, grad_y, w_gate, w_up, w_down, h, d, gate, up, sums;
 };
 void ffn_plan(int dtype, int max_rows, int max_hidden, int max_inner, bool grad, int compute_units, FfnPlan *plan);
+// Rows up to which the forward pass goes to the kernels for few (block_ffn.h has the reasons), of matrices of `size` elements; `whole`: all
+// that it reads can be read in place.  The fewest are those of the largest matrices, read in place.
+inline int few_rows(bool f32, int64_t size, bool whole)
+{
+    return f32 ? kFew : size <= 2 << 20 ? (whole ? 32 : kFew) : size <= 6 << 20 && !whole ? 32 : 16;
+}
 hipError_t ffn_prepare();            // kernel attributes, on the current device
 hipError_t ffn_launch(const FfnPlan &plan, int dtype, const deft_ffn_t &a, void *scratch, int compute_units, hipStream_t st);
 hipError_t ffn_grad_launch(const FfnPlan &plan, int dtype, const deft_ffn_grad_t &a, void *scratch, int compute_units, hipStream_t st);

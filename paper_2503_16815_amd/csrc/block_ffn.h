@@ -367,10 +367,8 @@ struct Ffn {
         // 4096 24.0 for 23.4), and more do not, though 48 of 768 x 2048 would be quicker without (18 for 21).
         const bool whole = Packing::as_is(a.x, a.x_stride, a.hidden, true) && Packing::as_is(a.w_gate, a.w_gate_stride, a.hidden, true) &&
                            Packing::as_is(a.w_up, a.w_up_stride, a.hidden, true) && Packing::as_is(a.w_down, a.w_down_stride, a.inner, true);
-        const int64_t size = (int64_t)a.hidden * a.inner;
-        const int most = kSplit ? kFew : size <= 2 << 20 ? (whole ? 32 : kFew) : size <= 6 << 20 && !whole ? 32 : 16;
         const bool two = !kSplit && (a.n_rows <= 8 || (a.n_rows > 16 && whole));
-        if (a.n_rows <= most) return few(a, s, two ? 2 : 1, compute_units, st);
+        if (a.n_rows <= few_rows(kSplit, (int64_t)a.hidden * a.inner, whole)) return few(a, s, two ? 2 : 1, compute_units, st);
         Packing pack;
         const Operand x = pack.operand(a.x, a.x_stride, a.n_rows, a.hidden, true, s.x);
         const Operand w_gate = pack.operand(a.w_gate, a.w_gate_stride, a.inner, a.hidden, true, s.w_gate);

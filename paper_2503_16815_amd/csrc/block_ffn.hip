@@ -51,6 +51,11 @@ void ffn_plan(int dtype, int max_rows, int max_hidden, int max_inner, bool grad,
         return here;
     };
     const int64_t element = dtype == DEFT_F32 ? 6 : 2, own = dtype == DEFT_F32 ? 4 : 2;   // of an operand (three 16-bit arrays), of the type
+    if (!grad && max_rows <= few_rows(dtype == DEFT_F32, (int64_t)max_hidden * max_inner, true)) {   // (the kernels for few alone: two arrays of h)
+        plan->h = take(2 * kFew * up(max_inner, 8) * own);
+        plan->scratch_bytes = at;
+        return;
+    }
     plan->largest = take(kFactorParts * 4);
     // (whether a call's rows can be read in place is known when it is made)
     plan->x = take(n * up(max_hidden, kStep) * element);
