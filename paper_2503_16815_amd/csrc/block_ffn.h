@@ -243,7 +243,8 @@ struct Ffn {
     }
 
     // Parts of a sum, as splits_of has them, with the time that it takes to write and join them: a launch and 8 bytes an element
-    // at 5 TB/s, in the time of a large tile's step.
+    // at 5 TB/s, in the time of a large tile's step.  (`steps` counts a 32-bit step's six products one by one, which the kernel does not
+    // part: there may be more parts than steps, as 4 of 3.  Those without a step have sums of zero.)
     static int parts_of(int64_t m, int64_t n, int64_t steps, int64_t units, unsigned without)
     {
         const int64_t tiles = up(m, kTile) / kTile * (n <= kFew ? 1 : up(n, kTile) / kTile);
