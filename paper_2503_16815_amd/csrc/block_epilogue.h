@@ -6,7 +6,7 @@
 // checkpoint's group of 32 is four lanes'.  What the derivatives' epilogue reads of the rows ahead is on its way meanwhile.
 //
 // Bound by memory, which is idle while the sums are made: the derivatives by both projections of 8192 x 6400 bf16 read 216 MB and write
-// 315 after a product of 140 us, 270 in all (without the writes 175, without the reads 226; with tiles two to a compute unit, one's
+// 315 after a product of 140 us, 270 to 280 in all (without the writes 175, without the reads 226; with tiles two to a compute unit, one's
 // epilogue beside the other's sums, the same).
 #pragma once
 #include <type_traits>

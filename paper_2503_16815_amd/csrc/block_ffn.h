@@ -16,9 +16,9 @@
 // 16-bit floats hold d_gate and d_up times a power of two that brings the largest of dy to 1 .. 2: the gradient of a mean over many
 // tokens is far below 1, and so out of their range's reach of 2^-14.
 //
-// Forward 8192 x 1600 x 6400 bf16 0.42 ms (1200 TFLOP/s in both products; a library's products of those sizes 1000 and 1230), with gradient 1.43 ms
-// (1060 over all nine; the derivative by h, bound by the 530 MB around its sums, 0.27 of it), 16384 x 4096 x 12288 kept in 8 bits 11.0 ms
-// (1350; 1550 to 1580), 1024 x 640 x 1728 f32 0.245 ms.
+// Forward 8192 x 1600 x 6400 bf16 0.42 ms (1200 TFLOP/s in both products; a library's products of those sizes 1000 and 1230), with gradient 1.42 to 1.47 ms
+// (1030 to 1060 over all nine; the derivative by h, bound by the 530 MB around its sums, 0.28 of it), 16384 x 4096 x 12288 kept in 8 bits 10.9 to 11.2 ms
+// (1320 to 1370; 1550 to 1580), 1024 x 640 x 1728 f32 0.242 to 0.248 ms.
 #pragma once
 #include "block_few.h"
 #include "ends_operands.h"
