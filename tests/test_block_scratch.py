@@ -30,7 +30,7 @@ int main(int argc, char **argv)   // dtype, rows, hidden, inner, grad ...
 """
 
 ROWS = [1, 8, 9, 16, 17, 32, 33, 64, 65, 1000]
-MATRICES = [(1, 1), (64, 96), (768, 2048), (1024, 2048), (1024, 2049), (1600, 6400), (2048, 3071), (2048, 3073), (4096, 12288), (16384, 65536)]
+MATRICES = [(1, 1), (64, 96), (768, 2048), (1024, 2048), (1024, 2049), (1600, 6400), (2051, 3061), (2051, 3079), (4096, 12288), (16384, 65536)]
 
 
 @pytest.fixture(scope="module")
